@@ -28,6 +28,12 @@ def lib_path() -> str:
     return _LIB_PATH
 
 
+class TmRopeParams(ctypes.Structure):
+    _fields_ = [("rot_dim", ctypes.c_int), ("layout", ctypes.c_int), ("scaling", ctypes.c_int), ("base", ctypes.c_double),
+                ("factor", ctypes.c_double), ("original_len", ctypes.c_double), ("low", ctypes.c_double), ("high", ctypes.c_double),
+                ("amplitude", ctypes.c_double), ("frequencies", ctypes.POINTER(ctypes.c_double))]
+
+
 class TmEpilogue(ctypes.Structure):
     _fields_ = [("bias", ctypes.c_void_p), ("residual", ctypes.c_void_p), ("act", ctypes.c_int)]
 
@@ -132,6 +138,18 @@ def load_library():
     lib.tm_bench_mfma.argtypes = [vp, i, i, i, i, vp]
     lib.tm_bench_read_shape.restype = i
     lib.tm_bench_read_shape.argtypes = [vp, sz, vp, i, i, i, i, vp]
+    lib.tm_rope_create.restype = vp
+    lib.tm_rope_create.argtypes = [c.POINTER(TmRopeParams)]
+    lib.tm_rope_free.restype = None
+    lib.tm_rope_free.argtypes = [vp]
+    lib.tm_rope_frequencies.restype = i
+    lib.tm_rope_frequencies.argtypes = [vp, c.POINTER(c.c_double), c.POINTER(c.c_double)]
+    lib.tm_paged_workspace_bytes.restype = sz
+    lib.tm_paged_workspace_bytes.argtypes = []
+    lib.tm_paged_create.restype = vp
+    lib.tm_paged_create.argtypes = [vp, vp, vp, i, i, i, i, vp, sz]
+    lib.tm_paged_free.restype = None
+    lib.tm_paged_free.argtypes = [vp]
     lib.tm_last_error.restype = c.c_char_p
     lib.tm_last_error.argtypes = []
     lib.tm_version.restype = c.c_char_p
@@ -585,3 +603,146 @@ def tm_kv_upload(cache: KvCache, kbuf, vbuf, szbuf):
             raise ValueError("buffer size does not match the cache")
         _check(lib.tm_bench_copy(ctypes.c_void_p(ptr), ctypes.c_void_p(t.data_ptr()), nbytes, _stream_ptr(None)))
     torch.cuda.synchronize()
+
+
+# ------------------------------------------------------------------ rotary positions and the paged cache (tm_paged.h)
+
+TM_ROPE_HALF, TM_ROPE_INTERLEAVED = 0, 1
+TM_ROPE_PLAIN, TM_ROPE_LINEAR, TM_ROPE_BASE, TM_ROPE_WAVELENGTH, TM_ROPE_RAMP = 0, 1, 2, 3, 4
+
+
+class Rope:
+    """Owner of a tm_rope handle."""
+
+    def __init__(self, handle: int, rot_dim: int):
+        self._h = handle
+        self.rot_dim = rot_dim
+
+    @property
+    def handle(self):
+        if not self._h:
+            raise ValueError("rope already freed")
+        return ctypes.c_void_p(self._h)
+
+    def close(self):
+        if self._h:
+            import torch
+            torch.cuda.synchronize()
+            load_library().tm_rope_free(ctypes.c_void_p(self._h))
+            self._h = 0
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+def tm_rope_create(rot_dim: int = 128, layout: int = TM_ROPE_HALF, base: float = 10000.0, scaling: int = TM_ROPE_PLAIN, factor: float = 1.0,
+                   original_len: float = 0.0, low: float = 0.0, high: float = 0.0, amplitude: float = 0.0, frequencies=None) -> Rope:
+    """Rotary positions over the first rot_dim dimensions of a head (see include/tm_paged.h); `frequencies`: rot_dim / 2 numbers,
+    radians per position, instead of those that base and scaling give."""
+    p = TmRopeParams(rot_dim, layout, scaling, base, factor, original_len, low, high, amplitude, None)
+    if frequencies is not None:
+        f = [float(x) for x in frequencies]
+        if len(f) != rot_dim // 2:
+            raise ValueError(f"need {rot_dim // 2} frequencies, got {len(f)}")
+        p.frequencies = (ctypes.c_double * len(f))(*f)
+    h = load_library().tm_rope_create(ctypes.byref(p))
+    if not h:
+        raise TmError(-1, tm_last_error())
+    return Rope(h, rot_dim)
+
+
+def tm_rope_frequencies(rope: Rope):
+    """(radians per position of every pair, amplitude)."""
+    f, amp = (ctypes.c_double * (rope.rot_dim // 2))(), ctypes.c_double()
+    _check(load_library().tm_rope_frequencies(rope.handle, f, ctypes.byref(amp)))
+    return list(f), amp.value
+
+
+def tm_rope_apply(X, positions, rope: Rope, Y, stream=None):
+    """X, Y float16 [tokens, heads, dim] (rows may lie apart, Y may be X), positions int32 [tokens], all on the device -> Y."""
+    return (_calls or _native()).rope_apply(X, positions, rope, Y, stream)
+
+
+def tm_paged_workspace(device="cuda"):
+    """A workspace for the caches of layers that run one after another on one stream."""
+    import torch
+    return torch.zeros(int(load_library().tm_paged_workspace_bytes()), dtype=torch.uint8, device=device)
+
+
+class PagedCache:
+    """Owner of a tm_paged_cache handle; keeps the pool's tensors and the workspace alive."""
+
+    def __init__(self, k, v, pairs, workspace=None):
+        import torch
+        if pairs.dim() != 5 or tuple(pairs.shape[3:]) != (2, 2) or k.dim() != 4 or tuple(k.shape[:2]) != tuple(pairs.shape[:2]) or \
+                k.shape[2] * 32 != pairs.shape[2] or k.shape[3] not in (2048, 4096) or v.shape != k.shape:
+            raise ValueError("need k, v [pages][kv_heads][page_tokens / 32][512 * bits], pairs [pages][kv_heads][page_tokens][2][2]")
+        ptrs = [_dev_ptr(k, torch.uint8, "k"), _dev_ptr(v, torch.uint8, "v"), _dev_ptr(pairs, torch.float16, "pairs")]
+        if workspace is None:
+            workspace = tm_paged_workspace(pairs.device)
+        ptrs.append(_dev_ptr(workspace, torch.uint8, "workspace"))
+        self._h = 0
+        self.k, self.v, self.pairs, self.workspace = k, v, pairs, workspace
+        if any(t.device.index != torch.cuda.current_device() for t in (k, v, pairs, workspace)):
+            raise ValueError("the pool and the workspace must lie on the current device")
+        self.pages, self.kv_heads, self.page_tokens, self.bits = k.shape[0], k.shape[1], pairs.shape[2], k.shape[3] // 512
+        h = load_library().tm_paged_create(*ptrs[:3], self.pages, self.kv_heads, self.page_tokens, self.bits, ptrs[3], workspace.numel())
+        if not h:
+            raise TmError(-1, tm_last_error())
+        self._h = h
+
+    @property
+    def handle(self):
+        if not self._h:
+            raise ValueError("paged cache already freed")
+        return ctypes.c_void_p(self._h)
+
+    def close(self):
+        if self._h:
+            import torch
+            torch.cuda.synchronize()
+            load_library().tm_paged_free(ctypes.c_void_p(self._h))
+            self._h = 0
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+def tm_paged_pool(pages: int, kv_heads: int, page_tokens: int, bits: int = 8, device="cuda"):
+    """Tensors of a pool: (k, v, pairs) for tm_paged_create."""
+    import torch
+    k, v = (torch.zeros(pages, kv_heads, page_tokens // 32, 512 * bits, dtype=torch.uint8, device=device) for _ in range(2))
+    return k, v, torch.zeros(pages, kv_heads, page_tokens, 2, 2, dtype=torch.float16, device=device)
+
+
+def tm_paged_create(k, v, pairs, workspace=None) -> PagedCache:
+    """A paged cache over the caller's tensors (layout: include/tm_paged.h); workspace: one of tm_paged_workspace, or None for its own."""
+    return PagedCache(k, v, pairs, workspace)
+
+
+class PagedBatch:
+    """The sequences of a call: table int32 [batch][max_pages], offsets int32 [batch + 1] of their rows in the packed token arrays,
+    positions int32 [batch] of their first new tokens; max_count and max_len are hints (0 = unknown), see include/tm_paged.h.  The tensors may be
+    updated in place between calls and between replays of a captured graph."""
+
+    __slots__ = ("table", "offsets", "positions", "max_count", "max_len")
+
+    def __init__(self, table, offsets, positions, max_count: int = 0, max_len: int = 0):
+        self.table, self.offsets, self.positions, self.max_count, self.max_len = table, offsets, positions, max_count, max_len
+
+
+def tm_paged_append(cache: PagedCache, batch: PagedBatch, K, V, rope: Rope = None, Q=None, Q_out=None, stream=None):
+    """Store the new tokens' K, V float16 [tokens, kv_heads, 128] (rows may lie apart) in their pages; with a rope keys are rotated first, and
+    Q [tokens, q_heads, 128] -> Q_out along with them.  -> Q_out"""
+    return (_calls or _native()).paged_append(cache, batch, K, V, rope, Q, Q_out, stream)
+
+
+def tm_paged_read(cache: PagedCache, batch: PagedBatch, K, V, stream=None):
+    """The cached keys and values of the batch's tokens into K, V float16 [tokens, kv_heads, 128]."""
+    return (_calls or _native()).paged_read(cache, batch, K, V, stream)

@@ -10,17 +10,20 @@
 // call.
 #include <torch/csrc/DynamicTypes.h>
 #include <torch/csrc/autograd/python_variable.h>
+#include <c10/hip/HIPFunctions.h>
 #include <c10/hip/HIPStream.h>
 
 #include <initializer_list>
 
 #include "tm_attn.h"
+#include "tm_paged.h"
 #include "tm_w4.h"
 
 namespace {
 
 PyObject* g_tm_error = nullptr;                          // binding.TmError
-PyObject *s_h, *s_K, *s_N, *s_experts, *s_batch, *s_kv_heads, *s_stream;      // attribute names, interned
+PyObject *s_h, *s_K, *s_N, *s_experts, *s_batch, *s_kv_heads, *s_stream, *s_table, *s_offsets, *s_positions,
+    *s_max_count, *s_max_len;                            // attribute names, interned
 
 struct Failed {};                                        // a Python exception is set
 
@@ -316,6 +319,149 @@ PyObject* attn_prefill(PyObject*, PyObject* const* a, Py_ssize_t n)  // Q, cache
     });
 }
 
+// ---- paged cache and rotary positions.  Tensors have to lie on the current device; rows of token arrays may lie apart (a part of a fused
+// projection's output is taken as it lies), heads and dimensions may not.
+
+constexpr const char* kRopeFreed = "rope already freed";
+constexpr const char* kPagedFreed = "paged cache already freed";
+
+void on_current_device(const at::Tensor& t, const char* what)
+{
+    if (t.get_device() != c10::hip::current_device()) {
+        PyErr_Format(PyExc_ValueError, "%s is on device %d, the current device is %d", what, (int)t.get_device(), (int)c10::hip::current_device());
+        throw Failed{};
+    }
+}
+
+const int32_t* int_ptr(const at::Tensor& t, const char* what)
+{
+    const auto* p = (const int32_t*)device_ptr(t, at::kInt, what);
+    on_current_device(t, what);
+    return p;
+}
+
+// fp16 [tokens][heads][dim]
+struct TokenRows {
+    uint16_t* p;
+    int64_t stride;
+    TokenRows(const at::Tensor& t, const char* what)
+    {
+        if (!t.is_cuda() || t.scalar_type() != at::kHalf) device_ptr(t, at::kHalf, what);          // raises what it raises for the other entry points
+        on_current_device(t, what);
+        const int64_t heads = t.size(1), dim = t.size(2);
+        if ((dim > 1 && t.stride(2) != 1) || (heads > 1 && t.stride(1) != dim) || (t.size(0) > 1 && t.stride(0) < heads * dim)) {
+            PyErr_Format(PyExc_ValueError, "%s must have contiguous heads and rows that do not overlap", what);
+            throw Failed{};
+        }
+        p = (uint16_t*)t.data_ptr();
+        stride = t.size(0) > 1 ? t.stride(0) : heads * dim;
+    }
+};
+
+// The sequences of a call: a binding.PagedBatch.  It keeps the tensors; their addresses are read here.
+struct Sequences {
+    tm_paged_batch b{};
+    Sequences(PyObject* batch, int64_t tokens)
+    {
+        PyObject* held[3] = {nullptr, nullptr, nullptr};
+        try {
+            held[0] = attr(batch, s_table), held[1] = attr(batch, s_offsets), held[2] = attr(batch, s_positions);
+            const at::Tensor &table = tensor(held[0], "table"), &offsets = tensor(held[1], "offsets"), &positions = tensor(held[2], "positions");
+            if (table.dim() != 2 || offsets.numel() != table.size(0) + 1 || positions.numel() != table.size(0))
+                raise(PyExc_ValueError, "need table [batch][max_pages], offsets [batch + 1], positions [batch]");
+            b.table = int_ptr(table, "table");
+            b.offsets = int_ptr(offsets, "offsets");
+            b.positions = int_ptr(positions, "positions");
+            b.batch = whole(table.size(0), "batch");
+            b.max_pages = whole(table.size(1), "max_pages");
+            b.tokens = whole(tokens, "tokens");
+            b.max_count = whole(int_attr(batch, s_max_count), "max_count");
+            b.max_len = whole(int_attr(batch, s_max_len), "max_len");
+        } catch (...) {
+            for (PyObject* o : held) Py_XDECREF(o);
+            throw;
+        }
+        for (PyObject* o : held) Py_DECREF(o);
+    }
+    static int whole(int64_t v, const char* what)
+    {
+        if (v < 0 || v > 0x7fffffff) {
+            PyErr_Format(PyExc_ValueError, "%s = %lld out of range", what, (long long)v);
+            throw Failed{};
+        }
+        return (int)v;
+    }
+};
+
+PyObject* rope_apply(PyObject*, PyObject* const* a, Py_ssize_t n)    // X, positions, rope, Y, stream
+{
+    return entry(n, 5, n > 3 ? a[3] : Py_None, [&] {
+        const at::Tensor &X = tensor(a[0], "X"), &pos = tensor(a[1], "positions"), &Y = tensor(a[3], "Y");
+        if (X.dim() != 3 || Y.sizes() != X.sizes() || pos.dim() != 1 || pos.numel() != X.size(0)) raise(PyExc_ValueError, "need X and Y [tokens][heads][dim], positions [tokens]");
+        const TokenRows x(X, "X"), y(Y, "Y");
+        const int32_t* p = int_ptr(pos, "positions");
+        const auto* h = (const tm_rope*)handle_of(a[2], kRopeFreed);
+        const int tokens = Sequences::whole(X.size(0), "tokens"), heads = Sequences::whole(X.size(1), "heads"), dim = Sequences::whole(X.size(2), "dim");
+        const tm_stream st = stream_of(a[4]);
+        call([&] { return tm_rope_apply(x.p, x.stride, p, h, y.p, y.stride, tokens, heads, dim, st); });
+    });
+}
+
+void check_tokens(const at::Tensor& t, int64_t tokens, int64_t heads, const char* what)
+{
+    if (!shape_is(t, {tokens, heads, 128})) {
+        PyErr_Format(PyExc_ValueError, "%s must be [%lld][%lld][128]", what, (long long)tokens, (long long)heads);
+        throw Failed{};
+    }
+}
+
+PyObject* paged_append(PyObject*, PyObject* const* a, Py_ssize_t n)  // cache, batch, K, V, rope, Q, Q_out, stream
+{
+    return entry(n, 8, n > 6 ? a[6] : Py_None, [&] {
+        const at::Tensor &K = tensor(a[2], "K"), &V = tensor(a[3], "V");
+        const int64_t tokens = K.dim() ? K.size(0) : 0, heads = int_attr(a[0], s_kv_heads);
+        check_tokens(K, tokens, heads, "K");
+        check_tokens(V, tokens, heads, "V");
+        const Sequences seqs(a[1], tokens);
+        const TokenRows k(K, "K"), v(V, "V");
+        auto* h = (tm_paged_cache*)handle_of(a[0], kPagedFreed);
+        const auto* rope = a[4] == Py_None ? nullptr : (const tm_rope*)handle_of(a[4], kRopeFreed);
+        const uint16_t* q = nullptr;
+        uint16_t* q_out = nullptr;
+        int64_t q_stride = 0, q_out_stride = 0;
+        int q_heads = 0;
+        if ((a[5] == Py_None) != (a[6] == Py_None)) raise(PyExc_ValueError, "Q and Q_out go together");
+        if (a[5] != Py_None) {
+            const at::Tensor &Q = tensor(a[5], "Q"), &Q_out = tensor(a[6], "Q_out");
+            if (Q.dim() != 3) raise(PyExc_ValueError, "Q must be [tokens][q_heads][128]");
+            check_tokens(Q, tokens, Q.size(1), "Q");
+            check_tokens(Q_out, tokens, Q.size(1), "Q_out");
+            const TokenRows in(Q, "Q"), out(Q_out, "Q_out");
+            q = in.p, q_stride = in.stride, q_out = out.p, q_out_stride = out.stride;
+            q_heads = Sequences::whole(Q.size(1), "q_heads");
+        }
+        const tm_stream st = stream_of(a[7]);
+        call([&] { return tm_paged_append(h, &seqs.b, k.p, k.stride, v.p, v.stride, rope, q, q_stride, q_out, q_out_stride, q_heads, st); });
+    });
+}
+
+PyObject* paged_read(PyObject*, PyObject* const* a, Py_ssize_t n)    // cache, batch, K, V, stream
+{
+    return entry(n, 5, Py_None, [&] {
+        const at::Tensor &K = tensor(a[2], "K"), &V = tensor(a[3], "V");
+        const int64_t tokens = K.dim() ? K.size(0) : 0, heads = int_attr(a[0], s_kv_heads);
+        check_tokens(K, tokens, heads, "K");
+        check_tokens(V, tokens, heads, "V");
+        const Sequences seqs(a[1], tokens);
+        uint16_t *k = half_ptr(K, "K"), *v = half_ptr(V, "V");
+        on_current_device(K, "K");
+        on_current_device(V, "V");
+        const auto* h = (const tm_paged_cache*)handle_of(a[0], kPagedFreed);
+        const tm_stream st = stream_of(a[4]);
+        call([&] { return tm_paged_read(h, &seqs.b, k, v, st); });
+    });
+}
+
 PyObject* set_error(PyObject*, PyObject* type)
 {
     Py_INCREF(type);
@@ -338,6 +484,9 @@ PyMethodDef g_methods[] = {fast<gemm>("gemm"),
                            fast<kv_append>("kv_append"),
                            fast<attn_decode>("attn_decode"),
                            fast<attn_prefill>("attn_prefill"),
+                           fast<rope_apply>("rope_apply"),
+                           fast<paged_append>("paged_append"),
+                           fast<paged_read>("paged_read"),
                            {"set_error", set_error, METH_O, nullptr},
                            {nullptr, nullptr, 0, nullptr}};
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "tm_calls", nullptr, -1, g_methods, nullptr, nullptr, nullptr, nullptr};
@@ -346,9 +495,9 @@ PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "tm_calls", nullptr, -1, g_method
 
 extern "C" __attribute__((visibility("default"))) PyObject* PyInit_tm_calls()
 {
-    PyObject** names[] = {&s_h, &s_K, &s_N, &s_experts, &s_batch, &s_kv_heads, &s_stream};
-    const char* texts[] = {"_h", "K", "N", "experts", "batch", "kv_heads", "cuda_stream"};
-    for (int i = 0; i < 7; ++i)
+    PyObject** names[] = {&s_h, &s_K, &s_N, &s_experts, &s_batch, &s_kv_heads, &s_stream, &s_table, &s_offsets, &s_positions, &s_max_count, &s_max_len};
+    const char* texts[] = {"_h", "K", "N", "experts", "batch", "kv_heads", "cuda_stream", "table", "offsets", "positions", "max_count", "max_len"};
+    for (int i = 0; i < 12; ++i)
         if (!(*names[i] = PyUnicode_InternFromString(texts[i]))) return nullptr;
     return PyModule_Create(&g_module);
 }

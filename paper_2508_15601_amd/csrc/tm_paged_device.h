@@ -1,0 +1,104 @@
+// Device-side view of a paged cache and of the sequences a call works on, and how a wave finds its sequence.
+#pragma once
+#include "tm_w4_device.h"
+
+namespace tmw4 {
+
+constexpr int kRun = 32;                 // tokens of a run: the unit in which codes are laid out
+
+// Pool of pages.  Page p, KV head h, run r of the page: codes at ((p * heads + h) << run_log | r) runs, scale / zero-point words of
+// token t of the page at word ((p * heads + h) << (run_log + 5) | t) * 2 (key, value).
+struct PagedPool {
+    uint8_t* k;
+    uint8_t* v;
+    uint32_t* pairs;
+    int pages, heads, run_log;           // runs of a page = 1 << run_log
+    int bits;
+};
+
+// The sequences of a call.  Rows offsets[b] .. offsets[b+1] - 1 of the packed arrays are the new tokens of sequence b; row i of it sits
+// at position positions[b] + i.
+struct PagedSeqs {
+    const int32_t* table;                // [batch][max_pages] page numbers; one outside the pool holds no tokens
+    const int32_t* offsets;              // [batch + 1]
+    const int32_t* positions;            // [batch]
+    int batch, max_pages, tokens, cap;   // cap = tokens a row of the table can hold
+};
+
+struct PagedSeq {
+    int row, count, pos;                 // first row, new tokens, position of the first
+    __device__ __forceinline__ int first() const { return max(pos, 0); }             // cached positions of the new tokens: [first, last)
+    __device__ __forceinline__ int last(int cap) const { return (int)min((long)pos + count, (long)cap); }
+};
+
+__device__ __forceinline__ PagedSeq paged_seq(const PagedSeqs& s, int b)
+{
+    const int o0 = min(max(s.offsets[b], 0), s.tokens), o1 = min(max(s.offsets[b + 1], 0), s.tokens);
+    return PagedSeq{o0, max(o1 - o0, 0), s.positions[b]};
+}
+
+// Inclusive sum over the lanes of a wave: rows of sixteen lanes, then the rows' totals to the rows behind them.
+__device__ __forceinline__ uint32_t wave_sums(uint32_t v)
+{
+    auto add = [&](auto CTRL, auto ROWS) {
+        v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, decltype(CTRL)::value, decltype(ROWS)::value, 0xf, false);
+    };
+    add(std::integral_constant<int, 0x111>{}, std::integral_constant<int, 0xf>{});   // row_shr by 1, 2, 4, 8
+    add(std::integral_constant<int, 0x112>{}, std::integral_constant<int, 0xf>{});
+    add(std::integral_constant<int, 0x114>{}, std::integral_constant<int, 0xf>{});
+    add(std::integral_constant<int, 0x118>{}, std::integral_constant<int, 0xf>{});
+    add(std::integral_constant<int, 0x142>{}, std::integral_constant<int, 0xa>{});   // row_bcast 15: last lane of a row to the next row
+    add(std::integral_constant<int, 0x143>{}, std::integral_constant<int, 0xc>{});   // row_bcast 31: to the upper half
+    return v;
+}
+
+// Work laid out sequence after sequence: units_of(b) units belong to sequence b.  Every wave sums them up by itself (a lane takes
+// ceil(batch / 64) neighbouring sequences; three loads each, all of them in the L2), so that no plan has to be made by another launch and
+// nothing about the lengths has to be known on the host.  The total has to stay below 2^32; whatever the offsets hold, find() names a
+// sequence that there is, and its callers check the unit against that sequence.
+template <class F>
+struct SeqFinder {
+    F units_of;
+    int per, batch;
+    uint32_t mine, incl;                 // units of the lane's sequences; with those of the lanes before
+    uint32_t total;
+
+    __device__ __forceinline__ SeqFinder(F f, int sequences, int lane) : units_of(f), per((sequences + 63) / 64), batch(sequences), mine(0)
+    {
+        for (int j = 0; j < per; ++j) {
+            const int b = lane * per + j;
+            if (b < batch) mine += units_of(b);
+        }
+        incl = wave_sums(mine);
+        total = (uint32_t)__builtin_amdgcn_readlane((int)incl, 63);
+    }
+    // The sequence that unit u < total belongs to, and its first unit (both wave-uniform).
+    __device__ __forceinline__ int find(uint32_t u, uint32_t& base) const
+    {
+        const int l = __builtin_popcountll(__builtin_amdgcn_ballot_w64(incl <= u));
+        base = (uint32_t)__builtin_amdgcn_readlane((int)(incl - mine), l);
+        int b = l * per;
+        for (int j = 1; j < per && b < batch; ++j) {
+            const uint32_t n = units_of(b);
+            if (u - base < n) break;
+            base += n;
+            ++b;
+        }
+        return min(b, batch - 1);
+    }
+};
+
+// Page number of run `run` (counted over the sequence) of sequence b, -1 where the table names none of the pool's.  The run must lie within
+// the table's row.
+__device__ __forceinline__ int paged_page(const PagedPool& p, const PagedSeqs& s, int b, int run)
+{
+    const int id = s.table[(size_t)b * s.max_pages + (run >> p.run_log)];
+    return (uint32_t)id < (uint32_t)p.pages ? id : -1;
+}
+// Number of a run in the pool.
+__device__ __forceinline__ size_t paged_run(const PagedPool& p, int page, int head, int run)
+{
+    return (((size_t)page * p.heads + head) << p.run_log) + (run & ((1 << p.run_log) - 1));
+}
+
+}  // namespace tmw4

@@ -1,0 +1,39 @@
+// Rotary positions of packed tokens (tm_rope_apply).
+#include "tm_rope_device.h"
+#include "tm_paged_host.h"
+
+namespace tmw4 {
+
+namespace {
+
+// A wave takes `per_wave` heads of one token: it works out the token's sines and cosines once (a lane a pair) and reads them back from LDS for every head.
+__global__ __launch_bounds__(256) void rope_kernel(const uint16_t* __restrict__ X, long x_stride, const int32_t* __restrict__ positions, RopePlan r,
+                                                   uint16_t* Y, long y_stride, int tokens, int heads, int dim, int per_wave)
+{
+    __shared__ CosSin cs[4][kRopeMaxPairs];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int parts = (heads + per_wave - 1) / per_wave;
+    const long job = (long)blockIdx.x * 4 + wave;
+    const long token = job / parts;
+    const int h0 = (int)(job - token * parts) * per_wave;
+    if (token < tokens) rope_angles(cs[wave], r, positions[token], lane);
+    __syncthreads();
+    if (token >= tokens) return;
+    rope_heads(X + token * x_stride, Y + token * y_stride, h0, min(h0 + per_wave, heads), dim, r, cs[wave], lane);
+}
+
+}  // namespace
+
+hipError_t launch_rope(const uint16_t* X, long x_stride, const int32_t* positions, const RopePlan& r, uint16_t* Y, long y_stride, int tokens, int heads,
+                       int dim, hipStream_t stream)
+{
+    // one round of a wave's lanes at a time where tokens are few
+    const int round = 64 / ((dim + 15) / 16);
+    const int per_wave = (long)tokens * heads >= 16384L * round ? heads : round;
+    const long jobs = (long)tokens * ((heads + per_wave - 1) / per_wave);
+    if (jobs <= 0 || jobs > 4 * 0x7fffffffL) return hipErrorInvalidValue;
+    hipLaunchKernelGGL(rope_kernel, dim3((unsigned)((jobs + 3) / 4)), dim3(256), 0, stream, X, x_stride, positions, r, Y, y_stride, tokens, heads, dim, per_wave);
+    return hipGetLastError();
+}
+
+}  // namespace tmw4

@@ -1,4 +1,5 @@
 // C ABI of libtm_w4: argument checking, handle and workspace management, kernel selection.
+#include <math.h>
 #include <stdarg.h>
 #include <stdio.h>
 #include <string.h>
@@ -8,6 +9,8 @@
 #include <vector>
 
 #include "tm_attn.h"
+#include "tm_paged.h"
+#include "tm_paged_host.h"
 #include "tm_w4.h"
 #include "tm_w4_host.h"
 
@@ -1917,6 +1920,272 @@ int tm_kv_raw(const tm_kv_cache* cache, void** k_codes, void** v_codes, void** p
     if (pairs) *pairs = cache->kv.sz;
     if (code_bytes) *code_bytes = cache->code_bytes;
     if (pair_bytes) *pair_bytes = cache->pair_bytes;
+    return TM_OK;
+}
+
+// --------------------------------------------------------------------------------- rotary positions and the paged cache
+
+struct tm_rope {
+    uint32_t magic;
+    int device, rot, interleaved;
+    double amp;
+    double f[kRopeMaxPairs];
+    uint64_t* turns;
+};
+
+struct tm_paged_cache {
+    uint32_t magic;
+    int device;
+    PagedPool pool;
+    void* workspace;
+};
+
+static bool valid_rope(const tm_rope* r) { return r && r->magic == 0x746D5250u; }
+static bool valid_paged(const tm_paged_cache* c) { return c && c->magic == 0x746D5047u; }
+
+// The frequencies of the header's table; false if a parameter is out of range.
+static bool rope_frequencies(const tm_rope_params& p, double* f, double* amp)
+{
+    const int n = p.rot_dim, pairs = n / 2;
+    const bool stretched = p.scaling != TM_ROPE_PLAIN, bounded = p.scaling == TM_ROPE_WAVELENGTH || p.scaling == TM_ROPE_RAMP;
+    *amp = p.amplitude;
+    if (!p.frequencies) {
+        if (!(p.base > 1.0) || !isfinite(p.base)) return false;
+        if (stretched && (!(p.factor >= 1.0) || !isfinite(p.factor))) return false;
+        if (bounded && (!(p.original_len > 0.0) || !isfinite(p.original_len) || !(p.low > 0.0) || !(p.high > p.low) || !isfinite(p.high))) return false;
+    } else if (p.scaling == TM_ROPE_RAMP && *amp == 0.0 && (!(p.factor >= 1.0) || !isfinite(p.factor))) {
+        return false;
+    }
+    if (*amp == 0.0) *amp = p.scaling == TM_ROPE_RAMP ? 0.1 * log(p.factor) + 1.0 : 1.0;
+    if (!isfinite(*amp) || !(fabs(*amp) <= 1e4)) return false;
+    const double pi2 = 6.283185307179586476925286766559;
+    auto at = [&](double turns) { return n * log(p.original_len / (turns * pi2)) / (2.0 * log(p.base)); };
+    const double base = p.scaling == TM_ROPE_BASE ? p.base * pow(p.factor, (double)n / (n - 2)) : p.base;
+    for (int i = 0; i < pairs; ++i) {
+        if (p.frequencies) {
+            f[i] = p.frequencies[i];
+        } else {
+            const double g = pow(base, -2.0 * i / n);
+            double w = p.scaling == TM_ROPE_LINEAR ? 0.0 : 1.0;
+            if (p.scaling == TM_ROPE_WAVELENGTH) w = (p.original_len * g / pi2 - p.low) / (p.high - p.low);
+            if (p.scaling == TM_ROPE_RAMP) {
+                const double a = fmax(floor(at(p.high)), 0.0), b = fmin(ceil(at(p.low)), n - 1.0);
+                w = 1.0 - (i - a) / fmax(b - a, 0.001);
+            }
+            w = fmin(fmax(w, 0.0), 1.0);
+            f[i] = stretched && p.scaling != TM_ROPE_BASE ? g / p.factor * (1.0 - w) + g * w : g;
+        }
+        if (!isfinite(f[i]) || fabs(f[i]) > 1e6) return false;
+    }
+    return true;
+}
+
+tm_rope* tm_rope_create(const tm_rope_params* params)
+{
+    if (!params) {
+        fail(TM_EINVAL, "params is null");
+        return nullptr;
+    }
+    const tm_rope_params& p = *params;
+    if (p.rot_dim < 16 || p.rot_dim > 2 * kRopeMaxPairs || p.rot_dim % 16 || p.layout < TM_ROPE_HALF || p.layout > TM_ROPE_INTERLEAVED ||
+        p.scaling < TM_ROPE_PLAIN || p.scaling > TM_ROPE_RAMP) {
+        fail(TM_EINVAL, "need rot_dim a multiple of 16 in 16 .. %d, a known layout and scaling (got %d, %d, %d)", 2 * kRopeMaxPairs, p.rot_dim, p.layout, p.scaling);
+        return nullptr;
+    }
+    tm_rope* r = new (std::nothrow) tm_rope();
+    if (!r) {
+        fail(TM_ENOMEM, "host allocation failed");
+        return nullptr;
+    }
+    if (!rope_frequencies(p, r->f, &r->amp)) {
+        fail(TM_EINVAL, "base, factor, original_len, low, high, amplitude or a frequency out of range");
+        delete r;
+        return nullptr;
+    }
+    if (check_device(&r->device) != TM_OK) {
+        delete r;
+        return nullptr;
+    }
+    r->rot = p.rot_dim;
+    r->interleaved = p.layout == TM_ROPE_INTERLEAVED;
+    uint64_t turns[kRopeMaxPairs];
+    for (int i = 0; i < r->rot / 2; ++i) {
+        // the fraction of a turn per position in units of 2^-64 (extended precision: 64 bits of mantissa)
+        long double t = (long double)r->f[i] / 6.283185307179586476925286766559L;
+        t = ldexpl(t - floorl(t), 64);
+        turns[i] = t >= ldexpl(1.0L, 64) ? 0u : (uint64_t)t;
+    }
+    hipError_t e = hipMalloc((void**)&r->turns, sizeof(uint64_t) * (size_t)(r->rot / 2));
+    if (e == hipSuccess) {
+        e = hipMemcpy(r->turns, turns, sizeof(uint64_t) * (size_t)(r->rot / 2), hipMemcpyHostToDevice);
+        if (e != hipSuccess) (void)hipFree(r->turns);
+    }
+    if (e != hipSuccess) {
+        fail_hip(e, "hipMalloc(rope)");
+        delete r;
+        return nullptr;
+    }
+    r->magic = 0x746D5250u;
+    return r;
+}
+
+void tm_rope_free(tm_rope* rope)
+{
+    if (!valid_rope(rope)) return;
+    rope->magic = 0;
+    (void)hipFree(rope->turns);
+    delete rope;
+}
+
+int tm_rope_frequencies(const tm_rope* rope, double* frequencies, double* amplitude)
+{
+    if (!valid_rope(rope)) return fail(TM_EINVAL, "rope handle is null or invalid");
+    if (frequencies) memcpy(frequencies, rope->f, sizeof(double) * (size_t)(rope->rot / 2));
+    if (amplitude) *amplitude = rope->amp;
+    return TM_OK;
+}
+
+static RopePlan rope_plan(const tm_rope* r) { return RopePlan{r->turns, r->amp, r->rot, r->interleaved}; }
+
+// A packed array of [rows][values]: alignment and stride.
+static int check_rows(const char* what, const void* p, int64_t stride, int64_t values)
+{
+    if (!p) return fail(TM_EINVAL, "%s is null", what);
+    if ((uintptr_t)p & 15) return fail(TM_EINVAL, "%s must be 16-byte aligned", what);
+    if (stride % 8 || stride < values || stride >= (int64_t(1) << 31)) return fail(TM_EINVAL, "%s: stride %lld must be a multiple of 8, at least %lld and below 2^31",
+                                                                                   what, (long long)stride, (long long)values);
+    return TM_OK;
+}
+
+int tm_rope_apply(const uint16_t* X, int64_t x_stride, const int32_t* positions, const tm_rope* rope, uint16_t* Y, int64_t y_stride, int tokens, int heads,
+                  int head_dim, tm_stream stream)
+{
+    if (!valid_rope(rope)) return fail(TM_EINVAL, "rope handle is null or invalid");
+    if (tokens < 0 || heads <= 0 || heads > 65535) return fail(TM_EINVAL, "need tokens >= 0 and 1 <= heads <= 65535 (got %d, %d)", tokens, heads);
+    if (head_dim % 8 || head_dim < rope->rot || head_dim > 256) return fail(TM_EINVAL, "head_dim = %d must be a multiple of 8 from %d to 256", head_dim, rope->rot);
+    if (tokens == 0) return TM_OK;
+    if (!positions || ((uintptr_t)positions & 3)) return fail(TM_EINVAL, "positions is null or misaligned");
+    int rc = check_rows("X", X, x_stride, (int64_t)heads * head_dim);
+    if (rc == TM_OK) rc = check_rows("Y", Y, y_stride, (int64_t)heads * head_dim);
+    if (rc != TM_OK) return rc;
+    if (X == Y && x_stride != y_stride) return fail(TM_EINVAL, "in place needs equal strides (got %lld, %lld)", (long long)x_stride, (long long)y_stride);
+    int dev;
+    rc = check_device(&dev);
+    if (rc != TM_OK) return rc;
+    if (dev != rope->device) return fail(TM_EINVAL, "rope lives on device %d, current device is %d", rope->device, dev);
+    const hipError_t e = launch_rope(X, x_stride, positions, rope_plan(rope), Y, y_stride, tokens, heads, head_dim, (hipStream_t)stream);
+    if (e != hipSuccess) return fail_hip(e, "rope launch");
+    return TM_OK;
+}
+
+size_t tm_paged_workspace_bytes(void) { return kPagedWorkspaceBytes; }
+
+tm_paged_cache* tm_paged_create(uint8_t* k, uint8_t* v, uint16_t* pairs, int pages, int kv_heads, int page_tokens, int bits, void* workspace, size_t workspace_bytes)
+{
+    if (!k || !v || !pairs || !workspace) {
+        fail(TM_EINVAL, "k, v, pairs or workspace is null");
+        return nullptr;
+    }
+    if (((uintptr_t)k | (uintptr_t)v | (uintptr_t)pairs) & 15 || ((uintptr_t)workspace & 255)) {
+        fail(TM_EINVAL, "misaligned pool (16 bytes) or workspace (256 bytes)");
+        return nullptr;
+    }
+    if (pages <= 0 || kv_heads <= 0 || kv_heads > 4096 || page_tokens < kRun || page_tokens > 1024 || (page_tokens & (page_tokens - 1)) || (bits != 8 && bits != 4)) {
+        fail(TM_EINVAL, "need pages > 0, 1 <= kv_heads <= 4096, page_tokens a power of two from 32 to 1024, bits 8 or 4 (got %d, %d, %d, %d)", pages, kv_heads,
+             page_tokens, bits);
+        return nullptr;
+    }
+    if (workspace_bytes < kPagedWorkspaceBytes) {
+        fail(TM_EINVAL, "workspace of %zu bytes, need %zu", workspace_bytes, (size_t)kPagedWorkspaceBytes);
+        return nullptr;
+    }
+    int dev;
+    if (check_device(&dev) != TM_OK) return nullptr;
+    tm_paged_cache* c = new (std::nothrow) tm_paged_cache();
+    if (!c) {
+        fail(TM_ENOMEM, "host allocation failed");
+        return nullptr;
+    }
+    c->device = dev;
+    c->pool = PagedPool{k, v, (uint32_t*)pairs, pages, kv_heads, __builtin_ctz((unsigned)page_tokens) - 5, bits};
+    c->workspace = workspace;
+    c->magic = 0x746D5047u;
+    return c;
+}
+
+void tm_paged_free(tm_paged_cache* cache)
+{
+    if (!valid_paged(cache)) return;
+    cache->magic = 0;
+    delete cache;
+}
+
+// Checks what every call on a paged cache shares; *seqs receives the kernels' view of the batch.
+static int check_paged(const tm_paged_cache* cache, const tm_paged_batch* b, PagedSeqs* seqs)
+{
+    if (!valid_paged(cache)) return fail(TM_EINVAL, "cache handle is null or invalid");
+    if (!b || !b->table || !b->offsets || !b->positions) return fail(TM_EINVAL, "batch, table, offsets or positions is null");
+    if (((uintptr_t)b->table | (uintptr_t)b->offsets | (uintptr_t)b->positions) & 3) return fail(TM_EINVAL, "misaligned table, offsets or positions");
+    const int page_log = cache->pool.run_log + 5;
+    if (b->batch <= 0 || b->batch > 65535 || b->max_pages <= 0 || ((int64_t)b->max_pages << page_log) >= (int64_t(1) << 30) || b->tokens < 0 || b->max_count < 0 ||
+        b->max_len < 0)
+        return fail(TM_EINVAL, "need 1 <= batch <= 65535, max_pages > 0, max_pages * %d < 2^30, tokens, max_count, max_len >= 0 (got %d, %d, %d, %d, %d)", 1 << page_log,
+                    b->batch, b->max_pages, b->tokens, b->max_count, b->max_len);
+    *seqs = PagedSeqs{b->table, b->offsets, b->positions, b->batch, b->max_pages, b->tokens, b->max_pages << page_log};
+    return TM_OK;
+}
+
+static int check_paged_device(const tm_paged_cache* cache, int* dev)
+{
+    const int rc = check_device(dev);
+    if (rc != TM_OK) return rc;
+    if (*dev != cache->device) return fail(TM_EINVAL, "cache lives on device %d, current device is %d", cache->device, *dev);
+    return TM_OK;
+}
+
+int tm_paged_append(tm_paged_cache* cache, const tm_paged_batch* batch, const uint16_t* K, int64_t k_stride, const uint16_t* V, int64_t v_stride, const tm_rope* rope,
+                    const uint16_t* Q, int64_t q_stride, uint16_t* Q_out, int64_t q_out_stride, int q_heads, tm_stream stream)
+{
+    PagedSeqs seqs;
+    int rc = check_paged(cache, batch, &seqs);
+    if (rc != TM_OK) return rc;
+    if (rope && !valid_rope(rope)) return fail(TM_EINVAL, "rope handle is invalid");
+    if (rope && rope->rot > 128) return fail(TM_EINVAL, "rot_dim = %d, the cache's heads have 128 dimensions", rope->rot);
+    if (Q && !rope) return fail(TM_EINVAL, "Q without a rope");
+    if (seqs.tokens == 0) return TM_OK;
+    const int64_t values = (int64_t)cache->pool.heads * 128;
+    rc = check_rows("K", K, k_stride, values);
+    if (rc == TM_OK) rc = check_rows("V", V, v_stride, values);
+    if (rc == TM_OK && Q) {
+        if (q_heads <= 0 || q_heads > 65535) return fail(TM_EINVAL, "q_heads = %d out of range", q_heads);
+        rc = check_rows("Q", Q, q_stride, (int64_t)q_heads * 128);
+        if (rc == TM_OK) rc = check_rows("Q_out", Q_out, q_out_stride, (int64_t)q_heads * 128);
+        if (rc == TM_OK && Q == Q_out && q_stride != q_out_stride) return fail(TM_EINVAL, "in place needs equal strides");
+    }
+    int dev;
+    if (rc == TM_OK) rc = check_paged_device(cache, &dev);
+    if (rc != TM_OK) return rc;
+    if (rope && rope->device != dev) return fail(TM_EINVAL, "rope lives on device %d, current device is %d", rope->device, dev);
+    RopePlan plan{};
+    if (rope) plan = rope_plan(rope);
+    const hipError_t e = launch_paged_append(cache->pool, seqs, PagedRows{K, (long)k_stride}, PagedRows{V, (long)v_stride}, rope ? &plan : nullptr,
+                                             PagedRows{Q, (long)q_stride}, Q_out, (long)q_out_stride, q_heads, (hipStream_t)stream);
+    if (e != hipSuccess) return fail_hip(e, "paged append launch");
+    return TM_OK;
+}
+
+int tm_paged_read(const tm_paged_cache* cache, const tm_paged_batch* batch, uint16_t* K, uint16_t* V, tm_stream stream)
+{
+    PagedSeqs seqs;
+    int rc = check_paged(cache, batch, &seqs);
+    if (rc != TM_OK) return rc;
+    if (seqs.tokens == 0) return TM_OK;
+    if (!K || !V || (((uintptr_t)K | (uintptr_t)V) & 15)) return fail(TM_EINVAL, "K or V is null or not 16-byte aligned");
+    int dev;
+    rc = check_paged_device(cache, &dev);
+    if (rc != TM_OK) return rc;
+    const hipError_t e = launch_paged_read(cache->pool, seqs, K, V, (hipStream_t)stream);
+    if (e != hipSuccess) return fail_hip(e, "paged read launch");
     return TM_OK;
 }
 
