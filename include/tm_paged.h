@@ -9,6 +9,7 @@
  *     tm_rope_apply    rotary positions of packed tokens
  *     tm_paged_append  (rotates and) quantises new keys and values into their pages, rotates the queries along
  *     tm_paged_read    the cached keys and values back as fp16
+ *     tm_paged_attn    causal attention of every sequence's new tokens over its pages
  *
  * Conventions as in tm_w4.h: plain C ABI, DEVICE pointers unless marked host, fp16 as uint16_t bit patterns, nothing synchronises or
  * allocates except the create calls, work is enqueued on the given stream, negative tm_status codes with tm_last_error().
@@ -124,6 +125,24 @@ TM_API int tm_paged_append(tm_paged_cache* cache, const tm_paged_batch* batch, c
  * position positions[b] + i.  Rows whose position lies outside [0, max_pages * page_tokens) are left untouched.
  */
 TM_API int tm_paged_read(const tm_paged_cache* cache, const tm_paged_batch* batch, uint16_t* K, uint16_t* V, tm_stream stream);
+
+/*
+ * Attention of the new tokens.  Q fp16 [tokens][q_heads][128] (row r at Q + r * q_stride, as for tm_rope_apply), O fp16 [tokens][q_heads][128] contiguous,
+ * both 16-byte aligned, not overlapping: row offsets[b] + i, the query at position p = positions[b] + i of its sequence, attends over the cached tokens 0 .. p, its own
+ * included, so its key and value have to be stored first (tm_paged_append, on the same stream):
+ *     O = softmax(scale * K^ q) V^,   query head h with KV head h / (q_heads / kv_heads),   q_heads = 1 .. 128 times kv_heads.
+ * Tokens on pages that the pool does not have are not attended over; a row that is left with none gets O = 0.  Rows whose position lies outside
+ * [0, max_pages * page_tokens) are left untouched.  One token a sequence is a decoding step, a few are drafted tokens to be verified, hundreds a prompt; a call takes any mix.
+ * Never allocates.  Partial results go through the cache's workspace.  Results are bit-identical from run to run (same arguments and hints).
+ */
+TM_API int tm_paged_attn(const uint16_t* Q, int64_t q_stride, const tm_paged_cache* cache, const tm_paged_batch* batch, uint16_t* O, int q_heads, float scale,
+                         tm_stream stream);
+
+/*
+ * Query hook: how tm_paged_attn divides such a call (host out-pointers, any may be NULL).  Sequences with up to *column_rows (token, query head of a KV head) rows, *columns of
+ * them at a time (8 or 16; 0 = no such launch), the others in CTAs of *rows rows (128 or 256; 0 = no such launch), their contexts in up to *pieces.
+ */
+TM_API int tm_get_paged_plan(const tm_paged_cache* cache, const tm_paged_batch* batch, int q_heads, int* columns, int* column_rows, int* rows, int* pieces);
 
 #ifdef __cplusplus
 }

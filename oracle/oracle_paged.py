@@ -92,13 +92,14 @@ def gather(arrays, table_row, n):
 
 
 def attention(Q, arrays, table, offsets, positions, scale: float):
-    """O fp64 [tokens][q_heads][128], NaN in rows that are not to be written.  Row offsets[b] + i at position positions[b] + i attends over the tokens
-    0 .. positions[b] + i that lie on a page of the pool; a row with none of them is 0."""
+    """(O, A) fp64 [tokens][q_heads][128], NaN in rows that are not to be written.  Row offsets[b] + i at position positions[b] + i attends over the tokens
+    0 .. positions[b] + i that lie on a page of the pool; a row with none of them is 0.  A is the same sum over |V^|: what rounding errors of the probabilities are
+    measured against."""
     Q = np.asarray(Q, np.float64)
     tokens, Hq, D = Q.shape
     heads, page = arrays[0].shape[1], arrays[0].shape[2]
     cap = table.shape[1] * page
-    O = np.full(Q.shape, np.nan)
+    O, A = np.full(Q.shape, np.nan), np.full(Q.shape, np.nan)
     for b in range(len(positions)):
         n = int(offsets[b + 1]) - int(offsets[b])
         last = min(int(positions[b]) + n, cap)
@@ -107,16 +108,17 @@ def attention(Q, arrays, table, offsets, positions, scale: float):
         with np.errstate(invalid="ignore", over="ignore"):
             K, V, ok = gather(arrays, table[b], last)
         for i in range(n):
-            p = int(positions[b]) + i
+            p, row = int(positions[b]) + i, int(offsets[b]) + i
             if not 0 <= p < cap:
                 continue
             use = np.nonzero(ok[:p + 1])[0]
             for h in range(Hq):
                 hk = h // (Hq // heads)
                 if not len(use):
-                    O[offsets[b] + i, h] = 0.0
+                    O[row, h] = A[row, h] = 0.0
                     continue
-                x = (K[use, hk] @ Q[offsets[b] + i, h]) * float(scale)
+                x = (K[use, hk] @ Q[row, h]) * float(scale)
                 e = np.exp(x - x.max())
-                O[offsets[b] + i, h] = (e / e.sum()) @ V[use, hk]
-    return O
+                e /= e.sum()
+                O[row, h], A[row, h] = e @ V[use, hk], e @ np.abs(V[use, hk])
+    return O, A

@@ -746,3 +746,13 @@ def tm_paged_append(cache: PagedCache, batch: PagedBatch, K, V, rope: Rope = Non
 def tm_paged_read(cache: PagedCache, batch: PagedBatch, K, V, stream=None):
     """The cached keys and values of the batch's tokens into K, V float16 [tokens, kv_heads, 128]."""
     return (_calls or _native()).paged_read(cache, batch, K, V, stream)
+
+
+def tm_paged_attn(Q, cache: PagedCache, batch: PagedBatch, O, scale: float, stream=None):
+    """Causal attention of the batch's new tokens over their pages: Q (rows may lie apart), O float16 [tokens, q_heads, 128] -> O."""
+    return (_calls or _native()).paged_attn(Q, cache, batch, O, scale, stream)
+
+
+def tm_get_paged_plan(cache: PagedCache, batch: PagedBatch, tokens: int, q_heads: int):
+    """(columns, column_rows, rows, pieces) of such a tm_paged_attn call, see include/tm_paged.h."""
+    return (_calls or _native()).paged_plan(cache, batch, tokens, q_heads)

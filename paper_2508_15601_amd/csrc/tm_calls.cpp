@@ -462,6 +462,37 @@ PyObject* paged_read(PyObject*, PyObject* const* a, Py_ssize_t n)    // cache, b
     });
 }
 
+PyObject* paged_attn(PyObject*, PyObject* const* a, Py_ssize_t n)    // Q, cache, batch, O, scale, stream
+{
+    return entry(n, 6, n > 3 ? a[3] : Py_None, [&] {
+        const at::Tensor &Q = tensor(a[0], "Q"), &O = tensor(a[3], "O");
+        if (Q.dim() != 3 || Q.size(2) != 128 || O.sizes() != Q.sizes()) raise(PyExc_ValueError, "Q and O must be [tokens][q_heads][128]");
+        const Sequences seqs(a[2], Q.size(0));
+        const TokenRows q(Q, "Q");
+        uint16_t* o = half_ptr(O, "O");
+        on_current_device(O, "O");
+        const auto* h = (const tm_paged_cache*)handle_of(a[1], kPagedFreed);
+        const int q_heads = Sequences::whole(Q.size(1), "q_heads");
+        const float scale = (float)as_double(a[4]);
+        const tm_stream st = stream_of(a[5]);
+        call([&] { return tm_paged_attn(q.p, q.stride, h, &seqs.b, o, q_heads, scale, st); });
+    });
+}
+
+PyObject* paged_plan(PyObject*, PyObject* const* a, Py_ssize_t n)    // cache, batch, tokens, q_heads -> (columns, column_rows, rows, pieces)
+{
+    int v[4] = {0, 0, 0, 0};
+    PyObject* none = entry(n, 4, Py_None, [&] {
+        const Sequences seqs(a[1], as_int(a[2]));
+        const auto* h = (const tm_paged_cache*)handle_of(a[0], kPagedFreed);
+        const int q_heads = Sequences::whole(as_int(a[3]), "q_heads");
+        call([&] { return tm_get_paged_plan(h, &seqs.b, q_heads, &v[0], &v[1], &v[2], &v[3]); });
+    });
+    if (!none) return nullptr;
+    Py_DECREF(none);
+    return Py_BuildValue("(iiii)", v[0], v[1], v[2], v[3]);
+}
+
 PyObject* set_error(PyObject*, PyObject* type)
 {
     Py_INCREF(type);
@@ -487,6 +518,8 @@ PyMethodDef g_methods[] = {fast<gemm>("gemm"),
                            fast<rope_apply>("rope_apply"),
                            fast<paged_append>("paged_append"),
                            fast<paged_read>("paged_read"),
+                           fast<paged_attn>("paged_attn"),
+                           fast<paged_plan>("paged_plan"),
                            {"set_error", set_error, METH_O, nullptr},
                            {nullptr, nullptr, 0, nullptr}};
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "tm_calls", nullptr, -1, g_methods, nullptr, nullptr, nullptr, nullptr};

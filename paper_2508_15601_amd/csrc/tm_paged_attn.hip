@@ -1,0 +1,331 @@
+// Attention of few new tokens per sequence over a paged cache: decoding steps and the verification of drafted tokens (tm_paged_attn; many tokens per sequence run
+// on tm_paged_rows.hip).
+//
+// Arithmetic and loading pipeline are those of decode attention over the contiguous cache (tm_attn.hip): a wave multiplies blocks of 4 KiB of key codes and as many of value
+// codes with sixteen (or eight) query columns, two blocks ahead in flight, four waves take blocks in turn and meet in LDS.  New here:
+//   - Columns are (token, query head) pairs of a sequence and KV head, numbered token by token, each with its own causal length.
+//   - The work of the call - (sequence, KV head, column tile) segments of `quads` of four blocks, the length known on the device only - is laid out in one row and cut into
+//     equal pieces, one per CTA.  A CTA works through the end of one segment, whole ones, and the beginning of another, so a call takes as long as its work
+//     and not as long as its longest sequence; a server's contexts differ by factors of ten.
+//   - A segment that several CTAs share is put together by the one that arrives last, in the order of the pieces, so results do not depend on who that is; above sixteen pieces in
+//     two levels, groups of sixteen first, which keeps the chain of loads short without another launch.
+//   - A block is one run of 32 tokens (8-bit codes) or two (4-bit); every run has its own address, from a page number that is requested three blocks ahead.  A run on a
+//     page that the pool does not have is not read and its tokens are masked.
+#include "tm_attn_device.h"
+#include "tm_paged_host.h"
+
+namespace tmw4 {
+
+namespace {
+
+constexpr int kGroupPieces = 16;         // pieces merged at a time
+constexpr int kMergeLoads = 8;           // of them in flight at once
+
+// Page numbers of a block's runs.
+template <int BITS>
+struct BlockPages {
+    int id[BITS == 8 ? 1 : 2];
+};
+
+template <int BITS, bool PACK>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) void paged_columns_kernel(
+    PagedPool pool, PagedSeqs seqs, const uint16_t* __restrict__ Q, long q_stride, uint16_t* __restrict__ O, int q_heads, float scale_log2e, int most_rows,
+    int min_quads, float* __restrict__ partial, uint32_t* __restrict__ counters)
+{
+    constexpr int TOK = 256 / BITS, RUNS = TOK / kRun;       // tokens and runs of a block
+    constexpr int COLS = PACK ? 8 : 16;
+    constexpr int kPartial = COLS * (2 + kHeadDim);          // m, l, unnormalised outputs of every column
+    __shared__ float sm_ml[4][2][16];
+    __shared__ float sm_out[4][8][4][64];
+    __shared__ __attribute__((aligned(16))) uint32_t sz_ring0[4][2 * TOK];
+    __shared__ __attribute__((aligned(16))) uint32_t sz_ring1[4][2 * TOK];
+    __shared__ __attribute__((aligned(16))) uint32_t sz_ring2[4][2 * TOK];
+    __shared__ uint32_t s_last;
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int c = lane & 15, h = lane >> 4;
+    const int G = q_heads / pool.heads;
+
+    // ---- this CTA's piece of the work
+    auto tiles_of = [&](const PagedSeq& s) { return s.count * G <= most_rows ? (s.count * G + COLS - 1) / COLS : 0; };
+    auto quads_of = [&](const PagedSeq& s) { return (max(s.last(seqs.cap), 0) + 4 * TOK - 1) / (4 * TOK); };
+    const SeqFinder finder(
+        [&](int b) {
+            const PagedSeq s = paged_seq(seqs, b);
+            return (uint32_t)(tiles_of(s) * pool.heads) * (uint32_t)quads_of(s);
+        },
+        seqs.batch, lane);
+    const uint32_t total = finder.total;
+    const uint32_t piece = max((total + gridDim.x - 1) / gridDim.x, (uint32_t)min_quads);
+    uint32_t at = blockIdx.x * piece;
+    if (at >= total) return;
+    const uint32_t end = min(at + piece, total);
+    uint32_t* const z0 = sz_ring0[wave];
+    uint32_t* const z1 = sz_ring1[wave];
+    uint32_t* const z2 = sz_ring2[wave];
+    const Magic mg = make_magic();
+
+    while (at < end) {
+        uint32_t base;
+        const int b = finder.find(at, base);
+        const PagedSeq s = paged_seq(seqs, b);
+        const uint32_t quads = (uint32_t)max(quads_of(s), 1), tiles = (uint32_t)max(tiles_of(s), 1);
+        const uint32_t segment = (at - base) / quads, qa = (at - base) - segment * quads;
+        const uint32_t seg_first = at - qa, qb = min(quads, qa + (end - at));
+        const int tile = (int)(segment % tiles), hk = min((int)(segment / tiles), pool.heads - 1);
+        at += qb - qa;
+
+        // ---- columns
+        const int rows = s.count * G, r0 = tile * COLS;
+        const int row = r0 + (PACK ? c & 7 : c);
+        int tok = row / G;
+        int head = row - tok * G;
+        const long pos = (long)s.pos + tok;
+        const bool real = row < rows && pos >= 0 && pos < seqs.cap;
+        const int len = real ? (int)pos + 1 : 0;
+        const int last_tok = (min(r0 + COLS, rows) - 1) / G;
+        const int len_all = (int)min(max((long)s.pos + last_tok + 1, 0L), (long)seqs.cap);
+        if (!real) tok = 0, head = 0;                        // an address that exists
+        f16x8 qraw[4];
+        {
+            const uint16_t* qp = Q + (size_t)(s.row + tok) * q_stride + ((size_t)hk * G + head) * kHeadDim + 32 * h;
+#pragma unroll
+            for (int tt = 0; tt < 4; ++tt) qraw[tt] = *(const f16x8*)(qp + 8 * tt);
+        }
+        const int blk1 = min((int)qb * 4, (len_all + TOK - 1) / TOK);
+        int blk = (int)qa * 4 + wave;
+
+        auto pages_of = [&](int k) {
+            BlockPages<BITS> p;
+#pragma unroll
+            for (int n = 0; n < RUNS; ++n) {
+                p.id[n] = -1;
+                if (k < blk1 && (k * RUNS + n) * kRun < len_all) p.id[n] = paged_page(pool, seqs, b, k * RUNS + n);
+            }
+            return p;
+        };
+        // Requests a block; a run that is not there is a buffer of no bytes, whose loads return zeros without memory traffic.  Returns which runs are there.
+        auto load = [&](BlockRegs& r, uint32_t* slot, int k, const BlockPages<BITS>& p) {
+            uint32_t present = 0;
+#pragma unroll
+            for (int n = 0; n < RUNS; ++n) {
+                constexpr uint32_t bytes = 512 * BITS;
+                const bool ok = p.id[n] >= 0;
+                present |= (uint32_t)ok << n;
+                const size_t run = paged_run(pool, ok ? p.id[n] : 0, hk, k * RUNS + n);
+                const __amdgpu_buffer_rsrc_t rk = make_rsrc(pool.k + run * bytes, ok ? bytes : 0u), rv = make_rsrc(pool.v + run * bytes, ok ? bytes : 0u),
+                                             rz = make_rsrc(pool.pairs + run * kRun * 2, ok ? kRun * 8u : 0u);
+#if defined(__HIP_DEVICE_COMPILE__)
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(rz, (__attribute__((address_space(3))) void*)(slot + 64 * n), 4, lane * 4, 0, 0, 0);
+#else
+                (void)rz, (void)slot;
+#endif
+#pragma unroll
+                for (int j = 0; j < 2; ++j)
+#pragma unroll
+                    for (int i = 0; i < 2 / RUNS; ++i)
+                        r.k[RUNS == 1 ? j : n][RUNS == 1 ? i : j] = __builtin_amdgcn_raw_buffer_load_b128(rk, lane * 16 + (RUNS == 1 ? j * 2 + i : j) * 1024, 0, kNonTemporal);
+#pragma unroll
+                for (int i = 0; i < 4 / RUNS; ++i) r.v[4 / RUNS * n + i] = __builtin_amdgcn_raw_buffer_load_b128(rv, lane * 16 + i * 1024, 0, kNonTemporal);
+            }
+            return present;
+        };
+
+        BlockRegs g0, g1, g2;
+        BlockPages<BITS> next = pages_of(blk);
+        BlockPages<BITS> after = pages_of(blk + 4);
+        uint32_t there0 = load(g0, z0, blk, next);
+        next = pages_of(blk + 8);
+        uint32_t there1 = load(g1, z1, blk + 4, after), there2 = 0;
+
+        f16x8 qf[4];
+        float qsum = 0.f, qbias = 0.f;
+#pragma unroll
+        for (int tt = 0; tt < 4; ++tt) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) qf[tt][e] = real ? qraw[tt][e] : (_Float16)0.0f;
+            u32x4 bits = __builtin_bit_cast(u32x4, qf[tt]);
+            asm volatile("" : "+v"(bits.x), "+v"(bits.y), "+v"(bits.z), "+v"(bits.w));            // (keeps this arithmetic behind the requests above)
+            qf[tt] = __builtin_bit_cast(f16x8, bits);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                qsum += (float)qf[tt][e];
+                qbias += ((e & 2) ? 64.0f : 1024.0f) * (float)qf[tt][e];
+            }
+        }
+        qsum = xor_add(xor_add(qsum, 16), 32);
+        qbias = BITS == 8 ? 1024.0f * qsum : xor_add(xor_add(qbias, 16), 32);
+        const f32x4 neg_qbias = {-qbias, -qbias, -qbias, -qbias};
+
+        // The reference starts above the mask value: a wave may meet blocks in which a column has no live token.
+        SoftmaxState st{kMaskFloor, 0.f, 0.f, f32x4{0.f, 0.f, 0.f, 0.f}};
+        f32x4 acc[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) acc[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+        auto step = [&](BlockRegs& use, uint32_t* zu, uint32_t there, BlockRegs& fill, uint32_t* zf, uint32_t& filled) {
+            filled = load(fill, zf, blk + 8, next);
+            next = pages_of(blk + 12);
+            process_block<BITS, PACK, true>(use, zu, qf, scale_log2e, qsum, neg_qbias, mg, blk, len, len_all, lane, st, acc, there);
+            blk += 4;
+            return blk < blk1;
+        };
+        if (blk < blk1)
+            while (step(g0, z0, there0, g2, z2, there2) && step(g1, z1, there1, g0, z0, there0) && step(g2, z2, there2, g1, z1, there1)) {
+            }
+
+        // ---- the four lanes of a column add their partial sums; the waves meet in LDS
+        float l_w = xor_add(xor_add(st.l_run, 16), 32);
+        float corr_w = xor_add(xor_add(st.corr, 16), 32);
+        if constexpr (PACK) {
+            l_w = xor_add(l_w, 8);
+            corr_w = xor_add(corr_w, 8);
+        }
+        if (h == 0) {
+            sm_ml[wave][0][c] = st.m_run;
+            sm_ml[wave][1][c] = l_w;
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+#pragma unroll
+            for (int rr = 0; rr < 4; ++rr) sm_out[wave][i][rr][lane] = (BITS == 8 ? acc[i][rr] + st.bias[rr] : acc[i][rr]) - corr_w;
+        __syncthreads();
+        float M = kNegBig;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) M = fmaxf(M, sm_ml[w][0][c]);
+        float L = 0.f, f[4];
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            f[w] = exp2f(sm_ml[w][0][c] - M);
+            L += sm_ml[w][1][c] * f[w];
+        }
+        // thread (wave w, lane) has dimensions 16 * (2w + ii) + 4h + rr of its column
+        float o[2][4];
+#pragma unroll
+        for (int ii = 0; ii < 2; ++ii)
+#pragma unroll
+            for (int rr = 0; rr < 4; ++rr) {
+                o[ii][rr] = 0.f;
+#pragma unroll
+                for (int w = 0; w < 4; ++w) o[ii][rr] += sm_out[w][2 * wave + ii][rr][lane] * f[w];
+            }
+        const bool writes = real && (!PACK || c < 8);
+        auto finish = [&](float m_l) {
+            const float inv = m_l > 0.f ? 1.0f / m_l : 0.f;
+#pragma unroll
+            for (int ii = 0; ii < 2; ++ii) {
+                const float v[4] = {o[ii][0] * inv, o[ii][1] * inv, o[ii][2] * inv, o[ii][3] * inv};
+                if (writes) store_out4(O, s.row + tok, q_heads, hk * G + head, 16 * (2 * wave + ii) + 4 * h, v);
+            }
+        };
+        if (qa == 0 && qb == quads) {                        // (uniform) the whole segment was this CTA's
+            finish(L);
+            __syncthreads();
+            continue;
+        }
+
+        // ---- a piece of a segment.  Its slot: 2k + 1 for the segment that begins in CTA k, 2k for one that began before it.
+        const bool column = c < COLS && (PACK ? c & 7 : c) + r0 < rows;
+        auto where = [&](int ii, int rr) { return 2 * COLS + ((4 * (2 * wave + ii) + rr) * 4 + h) * COLS + c; };
+        auto put = [&](uint32_t slot) {
+            float* const p = partial + (size_t)slot * kPartial;
+            if (!column) return;
+            if (wave == 0 && h == 0) {
+                st_partial(p + c, M);
+                st_partial(p + COLS + c, L);
+            }
+#pragma unroll
+            for (int ii = 0; ii < 2; ++ii)
+#pragma unroll
+                for (int rr = 0; rr < 4; ++rr) st_partial(p + where(ii, rr), o[ii][rr]);
+        };
+        // Bumps a counter once all of this CTA's stores have arrived; true in every thread of the CTA that is the last of n, which also resets it.
+        auto arrive = [&](uint32_t* counter, uint32_t n) {
+            wait_stores_done();
+            __syncthreads();
+            if (tid == 0) {
+                const uint32_t prev = atomicAdd(counter, 1u);
+                s_last = prev == n - 1u;
+                if (prev == n - 1u) __hip_atomic_store(counter, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            }
+            __syncthreads();
+            return s_last != 0u;
+        };
+        const uint32_t k0 = seg_first / piece, pieces = (seg_first + quads - 1) / piece - k0 + 1;
+        auto slot_of = [&](uint32_t j) { return j == 0 ? 2 * k0 + 1 : 2 * (k0 + j); };
+        // M, L, o := pieces j0, j0 + step, ... (n of them), in that order
+        auto merge = [&](uint32_t j0, uint32_t stride, uint32_t n) {
+            M = kNegBig, L = 0.f;
+#pragma unroll
+            for (int ii = 0; ii < 2; ++ii)
+#pragma unroll
+                for (int rr = 0; rr < 4; ++rr) o[ii][rr] = 0.f;
+            if (!column) return;
+            for (uint32_t i0 = 0; i0 < n; i0 += kMergeLoads) {
+                float ms[kMergeLoads], ls[kMergeLoads], v[kMergeLoads][2][4];
+#pragma unroll
+                for (int i = 0; i < kMergeLoads; ++i) {
+                    const float* const p = partial + (size_t)slot_of(j0 + stride * (i0 + i < n ? i0 + i : 0)) * kPartial;
+                    ms[i] = ld_partial(p + c);
+                    ls[i] = ld_partial(p + COLS + c);
+#pragma unroll
+                    for (int ii = 0; ii < 2; ++ii)
+#pragma unroll
+                        for (int rr = 0; rr < 4; ++rr) v[i][ii][rr] = ld_partial(p + where(ii, rr));
+                }
+                float up = M;
+#pragma unroll
+                for (int i = 0; i < kMergeLoads; ++i) up = fmaxf(up, i0 + i < n ? ms[i] : kNegBig);
+                const float old = exp2f(M - up);
+                M = up;
+                L *= old;
+#pragma unroll
+                for (int ii = 0; ii < 2; ++ii)
+#pragma unroll
+                    for (int rr = 0; rr < 4; ++rr) o[ii][rr] *= old;
+#pragma unroll
+                for (int i = 0; i < kMergeLoads; ++i) {
+                    const float fi = i0 + i < n ? exp2f(ms[i] - M) : 0.f;
+                    L += ls[i] * fi;
+#pragma unroll
+                    for (int ii = 0; ii < 2; ++ii)
+#pragma unroll
+                        for (int rr = 0; rr < 4; ++rr) o[ii][rr] += v[i][ii][rr] * fi;
+                }
+            }
+        };
+        const uint32_t mine = (at - 1) / piece - k0;         // this piece's number
+        const uint32_t groups = (pieces + kGroupPieces - 1) / kGroupPieces, g = mine / kGroupPieces;
+        const uint32_t in_group = min((uint32_t)kGroupPieces, pieces - g * kGroupPieces);
+        put(slot_of(mine));
+        // Counters: of the first group, [CTA in which the segment begins]; of a later one, [CTA of its first piece] - only one segment enters a CTA from before; of the
+        // groups of a segment, [CTA in which it begins].
+        if (!arrive(counters + (g == 0 ? k0 : gridDim.x + k0 + g * kGroupPieces), in_group)) continue;
+        merge(g * kGroupPieces, 1, in_group);
+        if (groups > 1) {
+            __syncthreads();                                 // all of the group has been read before its first slot is written
+            put(slot_of(g * kGroupPieces));
+            if (!arrive(counters + 2 * gridDim.x + k0, groups)) continue;
+            merge(0, kGroupPieces, groups);
+        }
+        finish(L);
+    }
+}
+
+}  // namespace
+
+hipError_t launch_paged_columns(const PagedPool& pool, const PagedSeqs& seqs, const uint16_t* Q, long q_stride, uint16_t* O, int q_heads, float scale, bool pack,
+                                int most_rows, int grid, int min_quads, void* workspace, hipStream_t stream)
+{
+    static_assert(3 * kPagedMostCtas * sizeof(uint32_t) <= kPagedCounterBytes, "three counters a CTA");
+    static_assert(2 * kPagedMostCtas * 16 * (2 + kHeadDim) * sizeof(float) <= kPagedPartialBytes, "two slots a CTA");
+    if (grid < 1 || grid > kPagedMostCtas) return hipErrorInvalidValue;
+    uint32_t* const counters = (uint32_t*)workspace;
+    float* const partial = (float*)((char*)workspace + kPagedCounterBytes);
+    const float s = scale * 1.4426950408889634f;
+    const auto kernel = pool.bits == 8 ? (pack ? paged_columns_kernel<8, true> : paged_columns_kernel<8, false>)
+                                       : (pack ? paged_columns_kernel<4, true> : paged_columns_kernel<4, false>);
+    hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(256), 0, stream, pool, seqs, Q, q_stride, O, q_heads, s, most_rows, min_quads, partial, counters);
+    return hipGetLastError();
+}
+
+}  // namespace tmw4

@@ -49,6 +49,7 @@ struct DeviceState {
     void* workspace = nullptr;
     void* xperm = nullptr;     // kXpermBytes, allocated with the first activation-order handle
     bool attn_ready = false;   // LDS limits of the prompt attention kernels raised, with the first cache
+    bool paged_ready = false;  // the same for the paged ones
     void* static_ws = nullptr; // this device's copy of the static scratch array, resolved at the first static call
     int num_cu = 256;
 };
@@ -2101,6 +2102,17 @@ tm_paged_cache* tm_paged_create(uint8_t* k, uint8_t* v, uint16_t* pairs, int pag
     }
     int dev;
     if (check_device(&dev) != TM_OK) return nullptr;
+    {
+        std::lock_guard<std::mutex> lock(g_mutex);
+        if (!g_dev[dev].paged_ready) {
+            const hipError_t e = paged_rows_setup();
+            if (e != hipSuccess) {
+                fail_hip(e, "paged attention set-up");
+                return nullptr;
+            }
+            g_dev[dev].paged_ready = true;
+        }
+    }
     tm_paged_cache* c = new (std::nothrow) tm_paged_cache();
     if (!c) {
         fail(TM_ENOMEM, "host allocation failed");
@@ -2186,6 +2198,51 @@ int tm_paged_read(const tm_paged_cache* cache, const tm_paged_batch* batch, uint
     if (rc != TM_OK) return rc;
     const hipError_t e = launch_paged_read(cache->pool, seqs, K, V, (hipStream_t)stream);
     if (e != hipSuccess) return fail_hip(e, "paged read launch");
+    return TM_OK;
+}
+
+static int check_paged_attn(const tm_paged_cache* cache, const tm_paged_batch* batch, int q_heads, PagedSeqs* seqs)
+{
+    const int rc = check_paged(cache, batch, seqs);
+    if (rc != TM_OK) return rc;
+    const int hk = cache->pool.heads;
+    if (q_heads <= 0 || q_heads % hk || q_heads / hk > 128) return fail(TM_EINVAL, "q_heads = %d must be 1..128 times the cache's %d heads", q_heads, hk);
+    // row numbers and pieces of work are counted in 32 bits
+    const int64_t G = q_heads / hk, tiles = seqs->tokens * G / 8 + seqs->batch, quads = seqs->cap / 128 + 1;
+    if (seqs->tokens * G >= (int64_t(1) << 30)) return fail(TM_EINVAL, "tokens * query heads of a KV head = %lld, at most 2^30", (long long)(seqs->tokens * G));
+    if (tiles * hk >= (int64_t(1) << 31) / quads)
+        return fail(TM_EINVAL, "%d tokens of %d sequences with %d heads over tables of %d tokens: too much work for one call", seqs->tokens, seqs->batch, q_heads, seqs->cap);
+    return TM_OK;
+}
+
+int tm_paged_attn(const uint16_t* Q, int64_t q_stride, const tm_paged_cache* cache, const tm_paged_batch* batch, uint16_t* O, int q_heads, float scale, tm_stream stream)
+{
+    PagedSeqs seqs;
+    int rc = check_paged_attn(cache, batch, q_heads, &seqs);
+    if (rc != TM_OK) return rc;
+    if (!(scale > 0.0f) || !(scale < 1.0e6f)) return fail(TM_EINVAL, "scale out of range");
+    if (seqs.tokens == 0) return TM_OK;
+    rc = check_rows("Q", Q, q_stride, (int64_t)q_heads * 128);
+    if (rc == TM_OK) rc = check_rows("O", O, (int64_t)q_heads * 128, (int64_t)q_heads * 128);
+    int dev;
+    if (rc == TM_OK) rc = check_paged_device(cache, &dev);
+    if (rc != TM_OK) return rc;
+    const hipError_t e = launch_paged_attn(cache->pool, seqs, Q, (long)q_stride, O, q_heads, scale, batch->max_count, batch->max_len, g_dev[dev].num_cu, cache->workspace,
+                                           (hipStream_t)stream);
+    if (e != hipSuccess) return fail_hip(e, "paged attention launch");
+    return TM_OK;
+}
+
+int tm_get_paged_plan(const tm_paged_cache* cache, const tm_paged_batch* batch, int q_heads, int* columns, int* column_rows, int* rows, int* pieces)
+{
+    PagedSeqs seqs;
+    const int rc = check_paged_attn(cache, batch, q_heads, &seqs);
+    if (rc != TM_OK) return rc;
+    const PagedForm f = paged_form(cache->pool, seqs, q_heads, batch->max_count, batch->max_len, g_dev[cache->device].num_cu);
+    if (columns) *columns = !f.column_rows ? 0 : f.pack ? 8 : 16;
+    if (column_rows) *column_rows = f.column_rows;
+    if (rows) *rows = 32 * f.row_waves;
+    if (pieces) *pieces = f.row_waves ? f.pieces : 0;
     return TM_OK;
 }
 

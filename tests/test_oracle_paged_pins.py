@@ -70,11 +70,11 @@ def test_paged_attention_is_the_contiguous_one(bits):
             for i in range(3):
                 p[table[b, i]] = a[b, :, i * page:(i + 1) * page]
         arrays.append(p)
-    got = op.attention(Qc.reshape(B * n, Hq, 128), arrays, table, [0, n, 2 * n], [T - n, 40], 0.1)
+    got = op.attention(Qc.reshape(B * n, Hq, 128), arrays, table, [0, n, 2 * n], [T - n, 40], 0.1)[0]
     assert np.abs(got.reshape(want.shape) - want).max() <= 2 ** -11 * np.abs(want).max()
     # a page that does not exist holds no tokens
     table[0, 1] = 99
-    holes = op.attention(Qc[0], arrays, table[:1], [0, n], [T - n], 0.1)
+    holes = op.attention(Qc[0], arrays, table[:1], [0, n], [T - n], 0.1)[0]
     keep = np.r_[0:32, 64:96]
     less = oa.attn_decode(Qc[:1, 2], *[a[:1, :, keep] for a in (*kq, *vq)], [64], 0.1)
     assert np.abs(holes[2] - less[0]).max() <= 2 ** -11 * np.abs(less).max()
