@@ -6,7 +6,8 @@
 //   - Columns are (token, query head) pairs of a sequence and KV head, numbered token by token, each with its own causal length.
 //   - The work of the call - (sequence, KV head, column tile) segments of `quads` of four blocks, the length known on the device only - is laid out in one row and cut into
 //     equal pieces, one per CTA.  A CTA works through the end of one segment, whole ones, and the beginning of another, so a call takes as long as its work
-//     and not as long as its longest sequence; a server's contexts differ by factors of ten.
+//     and not as long as its longest sequence; a server's contexts differ by factors of ten.  Beginning a segment costs as much as kSegmentStart quads, which counts as work.  Where
+//     there is little of it, pieces are cut so that every one begins a CTA and no short segment is cut at all.
 //   - A segment that several CTAs share is put together by the one that arrives last, in the order of the pieces, so results do not depend on who that is; above sixteen pieces in
 //     two levels, groups of sixteen first, which keeps the chain of loads short without another launch.
 //   - A block is one run of 32 tokens (8-bit codes) or two (4-bit); every run has its own address, from a page number that is requested three blocks ahead.  A run on a
@@ -20,19 +21,40 @@ namespace {
 
 constexpr int kGroupPieces = 16;         // pieces merged at a time
 constexpr int kMergeLoads = 8;           // of them in flight at once
+constexpr uint32_t kSegmentStart = 2;    // what beginning a segment costs, in quads
+constexpr uint32_t kAlignedQuads = 8;    // quads a CTA up to which work counts as little
 
-// Page numbers of a block's runs.
-template <int BITS>
+// Page numbers of the parts of a block.
+template <int PARTS>
 struct BlockPages {
-    int id[BITS == 8 ? 1 : 2];
+    int id[PARTS];
 };
 
-template <int BITS, bool PACK>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) void paged_columns_kernel(
+// What query column c of a tile of columns that begins at row r0 is: a token and a query head of the KV head's; not real: no row, or one whose position the table does not
+// reach, and the sequence's first row stands in as an address that exists.
+struct Column {
+    int tok, head;
+    bool real;
+    __device__ __forceinline__ Column(int c, bool pack, int r0, const PagedSeq& s, int G, int cap)
+    {
+        const int row = r0 + (pack ? c & 7 : c);
+        tok = row / G;
+        head = row - tok * G;
+        const long pos = (long)s.pos + tok;
+        real = row < s.count * G && pos >= 0 && pos < cap;
+        if (!real) tok = 0, head = 0;
+    }
+};
+
+// PARTS: pieces of a block that may lie on pages of their own: 2 for 4-bit codes on pages of a single run, else 1.
+template <int BITS, bool PACK, int PARTS>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(BITS == 4 && PACK ? 1 : 2, 2))) void paged_columns_kernel(
     PagedPool pool, PagedSeqs seqs, const uint16_t* __restrict__ Q, long q_stride, uint16_t* __restrict__ O, int q_heads, float scale_log2e, int most_rows,
-    int min_quads, float* __restrict__ partial, uint32_t* __restrict__ counters)
+    float* __restrict__ partial, uint32_t* __restrict__ counters)
 {
     constexpr int TOK = 256 / BITS, RUNS = TOK / kRun;       // tokens and runs of a block
+    constexpr uint32_t kLeastQuads = BITS == 8 ? 2 : 1;      // of a piece (1 x 2048 tokens, 8 heads, pieces of 1 / 2 / 3: 8-bit 9.8 / 9.0 / 9.2 us, 4-bit 9.5 / 10.6 / 11.6)
+    static_assert(PARTS == 1 || (BITS == 4 && PARTS == RUNS), "a part is a run, or the whole block");
     constexpr int COLS = PACK ? 8 : 16;
     constexpr int kPartial = COLS * (2 + kHeadDim);          // m, l, unnormalised outputs of every column
     __shared__ float sm_ml[4][2][16];
@@ -41,6 +63,8 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
     __shared__ __attribute__((aligned(16))) uint32_t sz_ring1[4][2 * TOK];
     __shared__ __attribute__((aligned(16))) uint32_t sz_ring2[4][2 * TOK];
     __shared__ uint32_t s_last;
+    __shared__ u32x2 s_sums[4][64];
+    __shared__ u32x4 s_seqs[4][64];
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int c = lane & 15, h = lane >> 4;
@@ -49,14 +73,43 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
     // ---- this CTA's piece of the work
     auto tiles_of = [&](const PagedSeq& s) { return s.count * G <= most_rows ? (s.count * G + COLS - 1) / COLS : 0; };
     auto quads_of = [&](const PagedSeq& s) { return (max(s.last(seqs.cap), 0) + 4 * TOK - 1) / (4 * TOK); };
-    const SeqFinder finder(
-        [&](int b) {
-            const PagedSeq s = paged_seq(seqs, b);
-            return (uint32_t)(tiles_of(s) * pool.heads) * (uint32_t)quads_of(s);
-        },
-        seqs.batch, lane);
-    const uint32_t total = finder.total;
-    const uint32_t piece = max((total + gridDim.x - 1) / gridDim.x, (uint32_t)min_quads);
+    const uint32_t ctas = gridDim.x;
+    // Up to 64 sequences a lane holds one, loaded once: a launch of few short contexts is a chain of memory round trips, and this one is its first.
+    const bool one_each = seqs.batch <= 64;
+    PagedSeq own{0, 0, 0};
+    uint32_t piece = 0;                                      // not 0: aligned, every piece of a segment but its last is as long, and every segment begins with a CTA
+    if (one_each) {
+        uint32_t n = 0, q = 0;
+        if (lane < seqs.batch) {
+            own = paged_seq(seqs, lane);
+            q = (uint32_t)quads_of(own);
+            n = q ? (uint32_t)(tiles_of(own) * pool.heads) : 0u;
+        }
+        const uint32_t segments = wave_total(n), all = wave_total(n * q);
+        if (2 * segments <= ctas && all <= kAlignedQuads * ctas) {
+            const uint32_t longest = wave_greatest(q), single = (longest + kGroupPieces - 1) / kGroupPieces;
+            piece = max((all + ctas - segments - 1) / (ctas - segments), kLeastQuads);
+            // up to sixteen pieces are merged in one level, and a second one costs more than a quad; three quads take no longer than a merge
+            if (single <= piece + 1) piece = max(piece, single);
+            if (longest <= 3) piece = max(piece, longest);
+        }
+    }
+    const bool aligned = piece != 0;
+    const uint32_t start = aligned ? 0u : kSegmentStart;
+    auto units_of = [&](const PagedSeq& s) {                 // of a segment
+        const uint32_t q = (uint32_t)quads_of(s);
+        return aligned ? (q + piece - 1) / piece * piece : q ? kSegmentStart + q : 0u;
+    };
+    auto work_of = [&](const PagedSeq& s) { return (uint32_t)(tiles_of(s) * pool.heads) * units_of(s); };
+    auto work_at = [&](int b) { return work_of(paged_seq(seqs, b)); };
+    uint32_t total;
+    {
+        const SeqFinder finder = one_each ? SeqFinder(work_at, seqs.batch, work_of(own)) : SeqFinder(work_at, seqs.batch, lane);
+        s_sums[wave][lane] = u32x2{finder.mine, finder.incl};            // (not in registers through the loops below)
+        s_seqs[wave][lane] = u32x4{(uint32_t)own.row, (uint32_t)own.count, (uint32_t)own.pos, 0u};
+        total = finder.total;
+    }
+    if (!aligned) piece = max((total + ctas - 1) / ctas, kLeastQuads);
     uint32_t at = blockIdx.x * piece;
     if (at >= total) return;
     const uint32_t end = min(at + piece, total);
@@ -67,73 +120,81 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
 
     while (at < end) {
         uint32_t base;
-        const int b = finder.find(at, base);
-        const PagedSeq s = paged_seq(seqs, b);
-        const uint32_t quads = (uint32_t)max(quads_of(s), 1), tiles = (uint32_t)max(tiles_of(s), 1);
-        const uint32_t segment = (at - base) / quads, qa = (at - base) - segment * quads;
-        const uint32_t seg_first = at - qa, qb = min(quads, qa + (end - at));
+        const u32x2 sums = s_sums[wave][lane];
+        const int b = SeqFinder(work_at, seqs.batch, sums[0], sums[1]).find(at, base);
+        auto sequence = [&](int i) {
+            if (!one_each) return paged_seq(seqs, i);
+            const u32x4 held = s_seqs[wave][lane];
+            return PagedSeq{__builtin_amdgcn_readlane((int)held[0], i), __builtin_amdgcn_readlane((int)held[1], i), __builtin_amdgcn_readlane((int)held[2], i)};
+        };
+        const PagedSeq s = sequence(b);
+        const uint32_t units = max(units_of(s), 1u), tiles = (uint32_t)max(tiles_of(s), 1);
+        const uint32_t segment = (at - base) / units, ua = (at - base) - segment * units;
+        const uint32_t seg_first = at - ua, ub = min(units, ua + (end - at));
         const int tile = (int)(segment % tiles), hk = min((int)(segment / tiles), pool.heads - 1);
-        at += qb - qa;
+        at += ub - ua;
+        if (ub <= start) continue;                           // (uniform) its quads are all the next CTA's
+        const uint32_t quads = (uint32_t)quads_of(s), qa = max(ua, start) - start, qb = min(ub - start, quads);
+        if (qa >= qb) continue;
 
         // ---- columns
         const int rows = s.count * G, r0 = tile * COLS;
-        const int row = r0 + (PACK ? c & 7 : c);
-        int tok = row / G;
-        int head = row - tok * G;
-        const long pos = (long)s.pos + tok;
-        const bool real = row < rows && pos >= 0 && pos < seqs.cap;
-        const int len = real ? (int)pos + 1 : 0;
+        const Column col(c, PACK, r0, s, G, seqs.cap);
+        const int len = col.real ? (int)(s.pos + col.tok) + 1 : 0;
         const int last_tok = (min(r0 + COLS, rows) - 1) / G;
         const int len_all = (int)min(max((long)s.pos + last_tok + 1, 0L), (long)seqs.cap);
-        if (!real) tok = 0, head = 0;                        // an address that exists
         f16x8 qraw[4];
         {
-            const uint16_t* qp = Q + (size_t)(s.row + tok) * q_stride + ((size_t)hk * G + head) * kHeadDim + 32 * h;
+            const uint16_t* qp = Q + (size_t)(s.row + col.tok) * q_stride + ((size_t)hk * G + col.head) * kHeadDim + 32 * h;
 #pragma unroll
             for (int tt = 0; tt < 4; ++tt) qraw[tt] = *(const f16x8*)(qp + 8 * tt);
         }
         const int blk1 = min((int)qb * 4, (len_all + TOK - 1) / TOK);
         int blk = (int)qa * 4 + wave;
 
+        constexpr uint32_t kPart = 4096 / PARTS, kPartTokens = TOK / PARTS;
+        // Unchecked, and of the context's last part where the block lies behind it: what is done with a page number waits for it, so that happens a step later.
+        const int last_part = max(len_all - 1, 0) / (int)kPartTokens;
         auto pages_of = [&](int k) {
-            BlockPages<BITS> p;
+            BlockPages<PARTS> p;
 #pragma unroll
-            for (int n = 0; n < RUNS; ++n) {
-                p.id[n] = -1;
-                if (k < blk1 && (k * RUNS + n) * kRun < len_all) p.id[n] = paged_page(pool, seqs, b, k * RUNS + n);
-            }
+            for (int n = 0; n < PARTS; ++n) p.id[n] = paged_entry(pool, seqs, b, min(k * PARTS + n, last_part) * (RUNS / PARTS));
             return p;
         };
-        // Requests a block; a run that is not there is a buffer of no bytes, whose loads return zeros without memory traffic.  Returns which runs are there.
-        auto load = [&](BlockRegs& r, uint32_t* slot, int k, const BlockPages<BITS>& p) {
+        // Requests a block; a part that is not there is a buffer of no bytes, whose loads return zeros without memory traffic.  Returns which parts are there.
+        auto load = [&](BlockRegs& r, uint32_t* slot, int k, const BlockPages<PARTS>& p) {
             uint32_t present = 0;
+            int off = lane * 16;                             // (opaque, so that the loads' distances go into the instructions and not into registers)
+            asm volatile("" : "+v"(off));
 #pragma unroll
-            for (int n = 0; n < RUNS; ++n) {
-                constexpr uint32_t bytes = 512 * BITS;
-                const bool ok = p.id[n] >= 0;
+            for (int n = 0; n < PARTS; ++n) {
+                const bool ok = k < blk1 && k * PARTS + n <= last_part && (uint32_t)p.id[n] < (uint32_t)pool.pages;
                 present |= (uint32_t)ok << n;
                 const size_t run = paged_run(pool, ok ? p.id[n] : 0, hk, k * RUNS + n);
-                const __amdgpu_buffer_rsrc_t rk = make_rsrc(pool.k + run * bytes, ok ? bytes : 0u), rv = make_rsrc(pool.v + run * bytes, ok ? bytes : 0u),
-                                             rz = make_rsrc(pool.pairs + run * kRun * 2, ok ? kRun * 8u : 0u);
+                const __amdgpu_buffer_rsrc_t rk = make_rsrc(pool.k + run * (512 * BITS), ok ? kPart : 0u), rv = make_rsrc(pool.v + run * (512 * BITS), ok ? kPart : 0u),
+                                             rz = make_rsrc(pool.pairs + run * kRun * 2, ok ? kPartTokens * 8u : 0u);
 #if defined(__HIP_DEVICE_COMPILE__)
-                __builtin_amdgcn_raw_ptr_buffer_load_lds(rz, (__attribute__((address_space(3))) void*)(slot + 64 * n), 4, lane * 4, 0, 0, 0);
+#pragma unroll
+                for (int i = 0; i < (int)kPartTokens / kRun; ++i)
+                    __builtin_amdgcn_raw_ptr_buffer_load_lds(rz, (__attribute__((address_space(3))) void*)(slot + 64 * (n + i)), 4, lane * 4 + i * 256, 0, 0, 0);
 #else
                 (void)rz, (void)slot;
 #endif
+                // key loads 0 .. 3 of a block: [16-token tile][half] of 8-bit codes, [run][16-token tile] of 4-bit ones
 #pragma unroll
-                for (int j = 0; j < 2; ++j)
+                for (int i = 0; i < 4 / PARTS; ++i) {
+                    const int at = 4 / PARTS * n + i;
+                    r.k[at >> 1][at & 1] = __builtin_amdgcn_raw_buffer_load_b128(rk, off + i * 1024, 0, kNonTemporal);
+                }
 #pragma unroll
-                    for (int i = 0; i < 2 / RUNS; ++i)
-                        r.k[RUNS == 1 ? j : n][RUNS == 1 ? i : j] = __builtin_amdgcn_raw_buffer_load_b128(rk, lane * 16 + (RUNS == 1 ? j * 2 + i : j) * 1024, 0, kNonTemporal);
-#pragma unroll
-                for (int i = 0; i < 4 / RUNS; ++i) r.v[4 / RUNS * n + i] = __builtin_amdgcn_raw_buffer_load_b128(rv, lane * 16 + i * 1024, 0, kNonTemporal);
+                for (int i = 0; i < 4 / PARTS; ++i) r.v[4 / PARTS * n + i] = __builtin_amdgcn_raw_buffer_load_b128(rv, off + i * 1024, 0, kNonTemporal);
             }
             return present;
         };
 
         BlockRegs g0, g1, g2;
-        BlockPages<BITS> next = pages_of(blk);
-        BlockPages<BITS> after = pages_of(blk + 4);
+        BlockPages<PARTS> next = pages_of(blk);
+        BlockPages<PARTS> after = pages_of(blk + 4);
         uint32_t there0 = load(g0, z0, blk, next);
         next = pages_of(blk + 8);
         uint32_t there1 = load(g1, z1, blk + 4, after), there2 = 0;
@@ -143,7 +204,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
 #pragma unroll
         for (int tt = 0; tt < 4; ++tt) {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) qf[tt][e] = real ? qraw[tt][e] : (_Float16)0.0f;
+            for (int e = 0; e < 8; ++e) qf[tt][e] = col.real ? qraw[tt][e] : (_Float16)0.0f;
             u32x4 bits = __builtin_bit_cast(u32x4, qf[tt]);
             asm volatile("" : "+v"(bits.x), "+v"(bits.y), "+v"(bits.z), "+v"(bits.w));            // (keeps this arithmetic behind the requests above)
             qf[tt] = __builtin_bit_cast(f16x8, bits);
@@ -165,7 +226,10 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
         auto step = [&](BlockRegs& use, uint32_t* zu, uint32_t there, BlockRegs& fill, uint32_t* zf, uint32_t& filled) {
             filled = load(fill, zf, blk + 8, next);
             next = pages_of(blk + 12);
-            process_block<BITS, PACK, true>(use, zu, qf, scale_log2e, qsum, neg_qbias, mg, blk, len, len_all, lane, st, acc, there);
+            if constexpr (PARTS == 1)
+                process_block<BITS, PACK>(use, zu, qf, scale_log2e, qsum, neg_qbias, mg, blk, there ? len : 0, len_all, lane, st, acc);
+            else
+                process_block<BITS, PACK, true>(use, zu, qf, scale_log2e, qsum, neg_qbias, mg, blk, len, len_all, lane, st, acc, there);
             blk += 4;
             return blk < blk1;
         };
@@ -208,13 +272,18 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
 #pragma unroll
                 for (int w = 0; w < 4; ++w) o[ii][rr] += sm_out[w][2 * wave + ii][rr][lane] * f[w];
             }
-        const bool writes = real && (!PACK || c < 8);
+        // What the loop above does not need is worked out again here rather than kept in registers through it.
+        int b_again = b, r0_again = r0;
+        asm volatile("" : "+s"(b_again), "+s"(r0_again));
+        const PagedSeq t = sequence(b_again);
+        const Column out(c, PACK, r0_again, t, G, seqs.cap);
+        const bool writes = out.real && (!PACK || c < 8);
         auto finish = [&](float m_l) {
             const float inv = m_l > 0.f ? 1.0f / m_l : 0.f;
 #pragma unroll
             for (int ii = 0; ii < 2; ++ii) {
                 const float v[4] = {o[ii][0] * inv, o[ii][1] * inv, o[ii][2] * inv, o[ii][3] * inv};
-                if (writes) store_out4(O, s.row + tok, q_heads, hk * G + head, 16 * (2 * wave + ii) + 4 * h, v);
+                if (writes) store_out4(O, t.row + out.tok, q_heads, hk * G + out.head, 16 * (2 * wave + ii) + 4 * h, v);
             }
         };
         if (qa == 0 && qb == quads) {                        // (uniform) the whole segment was this CTA's
@@ -224,7 +293,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
         }
 
         // ---- a piece of a segment.  Its slot: 2k + 1 for the segment that begins in CTA k, 2k for one that began before it.
-        const bool column = c < COLS && (PACK ? c & 7 : c) + r0 < rows;
+        const bool column = c < COLS && c + r0_again < t.count * G;
         auto where = [&](int ii, int rr) { return 2 * COLS + ((4 * (2 * wave + ii) + rr) * 4 + h) * COLS + c; };
         auto put = [&](uint32_t slot) {
             float* const p = partial + (size_t)slot * kPartial;
@@ -250,7 +319,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
             __syncthreads();
             return s_last != 0u;
         };
-        const uint32_t k0 = seg_first / piece, pieces = (seg_first + quads - 1) / piece - k0 + 1;
+        const uint32_t k0 = (seg_first + start) / piece, pieces = (seg_first + start + quads - 1) / piece - k0 + 1;
         auto slot_of = [&](uint32_t j) { return j == 0 ? 2 * k0 + 1 : 2 * (k0 + j); };
         // M, L, o := pieces j0, j0 + step, ... (n of them), in that order
         auto merge = [&](uint32_t j0, uint32_t stride, uint32_t n) {
@@ -314,7 +383,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
 }  // namespace
 
 hipError_t launch_paged_columns(const PagedPool& pool, const PagedSeqs& seqs, const uint16_t* Q, long q_stride, uint16_t* O, int q_heads, float scale, bool pack,
-                                int most_rows, int grid, int min_quads, void* workspace, hipStream_t stream)
+                                int most_rows, int grid, void* workspace, hipStream_t stream)
 {
     static_assert(3 * kPagedMostCtas * sizeof(uint32_t) <= kPagedCounterBytes, "three counters a CTA");
     static_assert(2 * kPagedMostCtas * 16 * (2 + kHeadDim) * sizeof(float) <= kPagedPartialBytes, "two slots a CTA");
@@ -322,9 +391,10 @@ hipError_t launch_paged_columns(const PagedPool& pool, const PagedSeqs& seqs, co
     uint32_t* const counters = (uint32_t*)workspace;
     float* const partial = (float*)((char*)workspace + kPagedCounterBytes);
     const float s = scale * 1.4426950408889634f;
-    const auto kernel = pool.bits == 8 ? (pack ? paged_columns_kernel<8, true> : paged_columns_kernel<8, false>)
-                                       : (pack ? paged_columns_kernel<4, true> : paged_columns_kernel<4, false>);
-    hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(256), 0, stream, pool, seqs, Q, q_stride, O, q_heads, s, most_rows, min_quads, partial, counters);
+    const auto kernel = pool.bits == 8        ? (pack ? paged_columns_kernel<8, true, 1> : paged_columns_kernel<8, false, 1>)
+                        : pool.run_log == 0 ? (pack ? paged_columns_kernel<4, true, 2> : paged_columns_kernel<4, false, 2>)
+                                            : (pack ? paged_columns_kernel<4, true, 1> : paged_columns_kernel<4, false, 1>);
+    hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(256), 0, stream, pool, seqs, Q, q_stride, O, q_heads, s, most_rows, partial, counters);
     return hipGetLastError();
 }
 

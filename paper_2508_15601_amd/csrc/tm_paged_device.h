@@ -25,6 +25,17 @@ struct PagedSeqs {
     int batch, max_pages, tokens, cap;   // cap = tokens a row of the table can hold
 };
 
+// An element of an array that no kernel of the launch writes.  With a wave-uniform index it is a scalar load, whatever the kernel stores elsewhere: as a vector load it would
+// stand in line with the blocks of codes, and waiting for a page number would be waiting for them.
+__device__ __forceinline__ int constant_load(const int32_t* p, size_t i)
+{
+#if defined(__HIP_DEVICE_COMPILE__)
+    return ((const __attribute__((address_space(4))) int32_t*)p)[i];
+#else
+    return p[i];
+#endif
+}
+
 struct PagedSeq {
     int row, count, pos;                 // first row, new tokens, position of the first
     __device__ __forceinline__ int first() const { return max(pos, 0); }             // cached positions of the new tokens: [first, last)
@@ -33,8 +44,8 @@ struct PagedSeq {
 
 __device__ __forceinline__ PagedSeq paged_seq(const PagedSeqs& s, int b)
 {
-    const int o0 = min(max(s.offsets[b], 0), s.tokens), o1 = min(max(s.offsets[b + 1], 0), s.tokens);
-    return PagedSeq{o0, max(o1 - o0, 0), s.positions[b]};
+    const int o0 = min(max(constant_load(s.offsets, b), 0), s.tokens), o1 = min(max(constant_load(s.offsets, b + 1), 0), s.tokens);
+    return PagedSeq{o0, max(o1 - o0, 0), constant_load(s.positions, b)};
 }
 
 // Inclusive sum over the lanes of a wave: rows of sixteen lanes, then the rows' totals to the rows behind them.
@@ -51,6 +62,14 @@ __device__ __forceinline__ uint32_t wave_sums(uint32_t v)
     add(std::integral_constant<int, 0x143>{}, std::integral_constant<int, 0xc>{});   // row_bcast 31: to the upper half
     return v;
 }
+
+__device__ __forceinline__ uint32_t wave_greatest(uint32_t v)
+{
+#pragma unroll
+    for (int m = 1; m < 64; m <<= 1) v = max(v, (uint32_t)__shfl_xor((int)v, m));
+    return (uint32_t)__builtin_amdgcn_readfirstlane((int)v);
+}
+__device__ __forceinline__ uint32_t wave_total(uint32_t v) { return (uint32_t)__builtin_amdgcn_readlane((int)wave_sums(v), 63); }
 
 // Work laid out sequence after sequence: units_of(b) units belong to sequence b.  Every wave sums them up by itself (a lane takes
 // ceil(batch / 64) neighbouring sequences; three loads each, all of them in the L2), so that no plan has to be made by another launch and
@@ -72,6 +91,17 @@ struct SeqFinder {
         incl = wave_sums(mine);
         total = (uint32_t)__builtin_amdgcn_readlane((int)incl, 63);
     }
+    // Up to 64 sequences, a lane's work known already.
+    __device__ __forceinline__ SeqFinder(F f, int sequences, uint32_t own) : units_of(f), per(1), batch(sequences), mine(own)
+    {
+        incl = wave_sums(mine);
+        total = (uint32_t)__builtin_amdgcn_readlane((int)incl, 63);
+    }
+    // The same again from the lane's two sums.
+    __device__ __forceinline__ SeqFinder(F f, int sequences, uint32_t own, uint32_t sum)
+        : units_of(f), per((sequences + 63) / 64), batch(sequences), mine(own), incl(sum), total(0)
+    {
+    }
     // The sequence that unit u < total belongs to, and its first unit (both wave-uniform).
     __device__ __forceinline__ int find(uint32_t u, uint32_t& base) const
     {
@@ -88,11 +118,15 @@ struct SeqFinder {
     }
 };
 
-// Page number of run `run` (counted over the sequence) of sequence b, -1 where the table names none of the pool's.  The run must lie within
-// the table's row.
+// The table's entry for run `run` (counted over the sequence) of sequence b; the run must lie within the table's row.
+__device__ __forceinline__ int paged_entry(const PagedPool& p, const PagedSeqs& s, int b, int run) 
+{
+    return constant_load(s.table, (size_t)b * s.max_pages + (run >> p.run_log));
+}
+// Its page number, -1 where that names none of the pool's.
 __device__ __forceinline__ int paged_page(const PagedPool& p, const PagedSeqs& s, int b, int run)
 {
-    const int id = s.table[(size_t)b * s.max_pages + (run >> p.run_log)];
+    const int id = paged_entry(p, s, b, run);
     return (uint32_t)id < (uint32_t)p.pages ? id : -1;
 }
 // Number of a run in the pool.

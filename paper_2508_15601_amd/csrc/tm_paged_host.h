@@ -24,13 +24,13 @@ hipError_t launch_paged_append(const PagedPool& pool, const PagedSeqs& seqs, Pag
                                long q_out_stride, int q_heads, hipStream_t stream);
 hipError_t launch_paged_read(const PagedPool& pool, const PagedSeqs& seqs, uint16_t* K, uint16_t* V, hipStream_t stream);
 // The new tokens of sequences with up to most_rows (token, query head of a KV head) rows; pack: columns by eight instead of sixteen.  Every CTA of `grid` takes an equal
-// piece, at least min_quads times four blocks.
+// piece of the work.
 hipError_t launch_paged_columns(const PagedPool& pool, const PagedSeqs& seqs, const uint16_t* Q, long q_stride, uint16_t* O, int q_heads, float scale, bool pack,
-                                int most_rows, int grid, int min_quads, void* workspace, hipStream_t stream);
+                                int most_rows, int grid, void* workspace, hipStream_t stream);
 
 // How a call is divided: sequences with at least least_rows rows in CTAs of 32 * row_waves rows (row_waves = 0: none), the others by columns (column_rows = 0: none).
 struct PagedForm {
-    int column_rows, column_ctas, min_quads;
+    int column_rows, column_ctas;
     bool pack;
     int least_rows, row_waves, pieces, piece_stages;
     uint32_t items;

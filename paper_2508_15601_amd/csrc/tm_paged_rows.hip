@@ -156,8 +156,7 @@ PagedForm paged_form(const PagedPool& pool, const PagedSeqs& seqs, int q_heads, 
     const long most = (long)(max_count > 0 && max_count < seqs.tokens ? max_count : seqs.tokens) * G;
     f.pack = G <= 8 && (most <= 8 || most > 64);
     f.column_rows = most <= 64 ? 64 : seqs.batch > 1 ? 16 : 0;
-    f.column_ctas = 2 * num_cu < kPagedMostCtas ? 2 * num_cu : kPagedMostCtas;
-    f.min_quads = 2;
+    f.column_ctas = num_cu < kPagedMostCtas ? num_cu : kPagedMostCtas;
     if (most <= 64) {
         f.column_rows = 1 << 30;                             // whatever the offsets say
         return f;
@@ -203,7 +202,7 @@ hipError_t launch_paged_attn(const PagedPool& pool, const PagedSeqs& seqs, const
                                  : launch<4, 4>(pool, seqs, Q, q_stride, O, q_heads, scale, plan, partial, stream);
     }
     if (e == hipSuccess && f.column_rows)
-        e = launch_paged_columns(pool, seqs, Q, q_stride, O, q_heads, scale, f.pack, f.column_rows, f.column_ctas, f.min_quads, workspace, stream);
+        e = launch_paged_columns(pool, seqs, Q, q_stride, O, q_heads, scale, f.pack, f.column_rows, f.column_ctas, workspace, stream);
     return e;
 }
 
