@@ -140,7 +140,7 @@ TM_API int tm_paged_attn(const uint16_t* Q, int64_t q_stride, const tm_paged_cac
 
 /*
  * Query hook: how tm_paged_attn divides such a call (host out-pointers, any may be NULL).  Sequences with up to *column_rows (token, query head of a KV head) rows, *columns of
- * them at a time (8 or 16; 0 = no such launch), the others in CTAs of *rows rows (128 or 256; 0 = no such launch), their contexts in up to *pieces.
+ * them at a time (8, 16 or 32; 0 = no such launch), the others in CTAs of *rows rows (128 or 256; 0 = no such launch), their contexts in up to *pieces.
  */
 TM_API int tm_get_paged_plan(const tm_paged_cache* cache, const tm_paged_batch* batch, int q_heads, int* columns, int* column_rows, int* rows, int* pieces);
 

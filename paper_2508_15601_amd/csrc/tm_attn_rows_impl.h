@@ -1,29 +1,13 @@
 // The kernel of prompt attention over a quantised cache; tm_attn_prefill.hip (contiguous cache, which describes it) and tm_paged_rows.hip (paged cache) build it.
 #pragma once
+#include "tm_attn_device.h"
 #include "tm_paged_device.h"
 
 namespace tmw4 {
 
 namespace {
 
-typedef float f32x16 __attribute__((ext_vector_type(16)));
-
-constexpr int kHeadDim = 128;
-constexpr float kNegBig = -1.0e30f;     // a masked score: "minus infinity" that stays finite under subtraction
-constexpr float kMaskFloor = -1.0e20f;  // lowest reference: exp2(kNegBig - kMaskFloor) is 0
-
-__device__ __forceinline__ f32x16 mfma32x32x16(f16x8 a, f16x8 b, f32x16 c)
-{
-    return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
-}
-
 __device__ __forceinline__ float other_half(float v) { return __shfl_xor(v, 32); }
-
-__device__ __forceinline__ f16x8 add_pairs(f16x8 v, f16x2 a, f16x2 b, f16x2 c, f16x2 d)
-{
-    const f16x2 r0 = f16x2{v[0], v[1]} + a, r1 = f16x2{v[2], v[3]} + b, r2 = f16x2{v[4], v[5]} + c, r3 = f16x2{v[6], v[7]} + d;
-    return f16x8{r0.x, r0.y, r1.x, r1.y, r2.x, r2.y, r3.x, r3.y};
-}
 
 constexpr int ST = 64;                           // tokens per stage
 constexpr int kStageBytes = ST * kHeadDim * 2;   // one stage of keys (or values) in fp16
@@ -56,7 +40,6 @@ __device__ __forceinline__ void attn_rows(const RowsJob& job, const uint8_t* kco
 {
     constexpr int KS = 8 / RW;                             // wave groups along the context
     constexpr int NB = 2 / KS;                             // 32-token runs per wave and stage
-    constexpr float kSlack = BITS == 8 ? 6.0f : 2.0f;      // 2^6 * (2 * 65504 / 255), 2^2 * (2 * 65504 / 15) < 65504
     unsigned char* const kbase = smem;
     unsigned char* const vbase = smem + 2 * kStageBytes;
     unsigned char* const pbase = vbase + 3 * kStageBytes;
@@ -332,7 +315,7 @@ __device__ __forceinline__ void attn_rows(const RowsJob& job, const uint8_t* kco
             const int st_n = sub + 1 < NB ? st : st + 1, sub_n = sub + 1 < NB ? sub + 1 : 0;
             if (sub + 1 == NB) barrier();                  // the next stage is in LDS
             if (t0 < wlen) {                               // wave-uniform
-                if (__any(mx > kSlack)) {
+                if (__any(mx > kSlack<BITS>)) {
                     const float up = fmaxf(fmaxf(mx, other_half(mx)), 0.f);
                     const float alpha = __builtin_amdgcn_exp2f(-up);
                     m_run += up;

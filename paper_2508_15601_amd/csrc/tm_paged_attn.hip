@@ -7,7 +7,7 @@
 //   - The work of the call - (sequence, KV head, column tile) segments of `quads` of four blocks, the length known on the device only - is laid out in one row and cut into
 //     equal pieces, one per CTA.  A CTA works through the end of one segment, whole ones, and the beginning of another, so a call takes as long as its work
 //     and not as long as its longest sequence; a server's contexts differ by factors of ten.  Beginning a segment costs as much as kSegmentStart quads, which counts as work.  Where
-//     there is little of it, pieces are cut so that every one begins a CTA and no short segment is cut at all.
+//     segments are few, pieces are cut so that every segment begins with a CTA, if that lengthens them by less than it saves.
 //   - A segment that several CTAs share is put together by the one that arrives last, in the order of the pieces, so results do not depend on who that is; above sixteen pieces in
 //     two levels, groups of sixteen first, which keeps the chain of loads short without another launch.
 //   - A block is one run of 32 tokens (8-bit codes) or two (4-bit); every run has its own address, from a page number that is requested three blocks ahead.  A run on a
@@ -22,7 +22,7 @@ namespace {
 constexpr int kGroupPieces = 16;         // pieces merged at a time
 constexpr int kMergeLoads = 8;           // of them in flight at once
 constexpr uint32_t kSegmentStart = 2;    // what beginning a segment costs, in quads
-constexpr uint32_t kAlignedQuads = 8;    // quads a CTA up to which work counts as little
+constexpr uint32_t kUnaligned = 4;       // what a CTA pays for not beginning with a segment: most of them have one more to begin, and two to hand on
 
 // Page numbers of the parts of a block.
 template <int PARTS>
@@ -35,9 +35,9 @@ struct BlockPages {
 struct Column {
     int tok, head;
     bool real;
-    __device__ __forceinline__ Column(int c, bool pack, int r0, const PagedSeq& s, int G, int cap)
+    __device__ __forceinline__ Column(int c, int r0, const PagedSeq& s, int G, int cap)
     {
-        const int row = r0 + (pack ? c & 7 : c);
+        const int row = r0 + c;
         tok = row / G;
         head = row - tok * G;
         const long pos = (long)s.pos + tok;
@@ -46,28 +46,124 @@ struct Column {
     }
 };
 
+// A wave's part: sixteen query columns, or eight (PACK), on the 16x16x32 instruction, with the arithmetic of decode attention over the contiguous cache (tm_attn_device.h).
+template <int BITS, bool PACK>
+struct Columns {
+    static constexpr int kCols = PACK ? 8 : 16;
+    f16x8 qf[4];
+    float qsum, scale_log2e;
+    f32x4 neg_qbias;
+    SoftmaxState st;
+    f32x4 acc[8];
+
+    static __device__ __forceinline__ int column(int lane) { return lane & (kCols - 1); }
+    static __device__ __forceinline__ bool owns(int lane) { return (lane & 15) < kCols; }          // the others are copies
+
+    // q: the row of the lane's column
+    f16x8 raw[4];
+    __device__ __forceinline__ void request_query(const uint16_t* q, int lane)
+    {
+#pragma unroll
+        for (int t = 0; t < 4; ++t) raw[t] = *(const f16x8*)(q + 32 * (lane >> 4) + 8 * t);
+    }
+    __device__ __forceinline__ void begin(bool real, float scale)
+    {
+        scale_log2e = scale;
+        float qbias = 0.f;
+        qsum = 0.f;
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) qf[t][e] = real ? raw[t][e] : (_Float16)0.0f;
+            u32x4 bits = __builtin_bit_cast(u32x4, qf[t]);
+            asm volatile("" : "+v"(bits.x), "+v"(bits.y), "+v"(bits.z), "+v"(bits.w));            // (keeps this arithmetic behind the requests before it)
+            qf[t] = __builtin_bit_cast(f16x8, bits);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                qsum += (float)qf[t][e];
+                qbias += ((e & 2) ? 64.0f : 1024.0f) * (float)qf[t][e];
+            }
+        }
+        qsum = xor_add(xor_add(qsum, 16), 32);
+        qbias = BITS == 8 ? 1024.0f * qsum : xor_add(xor_add(qbias, 16), 32);
+        neg_qbias = f32x4{-qbias, -qbias, -qbias, -qbias};
+        // the reference starts above the mask value: a wave may meet blocks in which a column has no live token
+        st = SoftmaxState{kMaskFloor, 0.f, 0.f, f32x4{0.f, 0.f, 0.f, 0.f}};
+#pragma unroll
+        for (int i = 0; i < 8; ++i) acc[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+    template <int PARTS>
+    __device__ __forceinline__ void block(const BlockRegs& r, const uint32_t* words, const Magic& mg, int blk, int len, int len_all, int lane, uint32_t present)
+    {
+        if constexpr (PARTS == 1)
+            process_block<BITS, PACK>(r, words, qf, scale_log2e, qsum, neg_qbias, mg, blk, present ? len : 0, len_all, lane, st, acc);
+        else
+            process_block<BITS, PACK, true>(r, words, qf, scale_log2e, qsum, neg_qbias, mg, blk, len, len_all, lane, st, acc, present);
+    }
+    // The four waves that share the columns meet in LDS: wave `wave` gets the unnormalised values o of dimensions 16 * (2 * wave + i / 4) + 4 * (lane / 16) + i % 4 of its lane's column, the
+    // reference M and the denominator L.  (One barrier; another has to follow before the next segment's.)
+    struct Join {
+        float ml[4][2][16];
+        float out[4][8][4][64];
+    };
+    __device__ __forceinline__ void join(Join& lds, int wave, int lane, float& M, float& L, float (&o)[8])
+    {
+        const int c = lane & 15;
+        float l = xor_add(xor_add(st.l_run, 16), 32), corr = xor_add(xor_add(st.corr, 16), 32);
+        if constexpr (PACK) l = xor_add(l, 8), corr = xor_add(corr, 8);
+        if (lane < 16) {
+            lds.ml[wave][0][c] = st.m_run;
+            lds.ml[wave][1][c] = l;
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+#pragma unroll
+            for (int rr = 0; rr < 4; ++rr) lds.out[wave][i][rr][lane] = (BITS == 8 ? acc[i][rr] + st.bias[rr] : acc[i][rr]) - corr;
+        __syncthreads();
+        M = kNegBig;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) M = fmaxf(M, lds.ml[w][0][c]);
+        float f[4];
+        L = 0.f;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            f[w] = exp2f(lds.ml[w][0][c] - M);
+            L += lds.ml[w][1][c] * f[w];
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            o[i] = 0.f;
+#pragma unroll
+            for (int w = 0; w < 4; ++w) o[i] += lds.out[w][2 * wave + (i >> 2)][i & 3][lane] * f[w];
+        }
+    }
+};
+
 // PARTS: pieces of a block that may lie on pages of their own: 2 for 4-bit codes on pages of a single run, else 1.
-template <int BITS, bool PACK, int PARTS>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(BITS == 4 && PACK ? 1 : 2, 2))) void paged_columns_kernel(
+// TILES: tiles of columns that a CTA takes at once, four waves each: with two, the waves that share a block ask for it at the same time, and it comes from memory once.  (Tiles one after
+// the other read it twice: 12 x 5 drafted tokens after 6000, 25 columns, 8-bit codes: 45 us, like this XX.)
+template <int BITS, bool PACK, int PARTS, int TILES>
+__global__ __launch_bounds__(256 * TILES) __attribute__((amdgpu_waves_per_eu(BITS == 4 && PACK ? 1 : 2, 2))) void paged_columns_kernel(
     PagedPool pool, PagedSeqs seqs, const uint16_t* __restrict__ Q, long q_stride, uint16_t* __restrict__ O, int q_heads, float scale_log2e, int most_rows,
     float* __restrict__ partial, uint32_t* __restrict__ counters)
 {
     constexpr int TOK = 256 / BITS, RUNS = TOK / kRun;       // tokens and runs of a block
     constexpr uint32_t kLeastQuads = BITS == 8 ? 2 : 1;      // of a piece (1 x 2048 tokens, 8 heads, pieces of 1 / 2 / 3: 8-bit 9.8 / 9.0 / 9.2 us, 4-bit 9.5 / 10.6 / 11.6)
     static_assert(PARTS == 1 || (BITS == 4 && PARTS == RUNS), "a part is a run, or the whole block");
-    constexpr int COLS = PACK ? 8 : 16;
+    typedef Columns<BITS, PACK> Form;
+    constexpr int COLS = Form::kCols * TILES;                // of a segment
     constexpr int kPartial = COLS * (2 + kHeadDim);          // m, l, unnormalised outputs of every column
-    __shared__ float sm_ml[4][2][16];
-    __shared__ float sm_out[4][8][4][64];
-    __shared__ __attribute__((aligned(16))) uint32_t sz_ring0[4][2 * TOK];
-    __shared__ __attribute__((aligned(16))) uint32_t sz_ring1[4][2 * TOK];
-    __shared__ __attribute__((aligned(16))) uint32_t sz_ring2[4][2 * TOK];
+    // scale/zero words of the blocks in flight; one array per ring slot so that the compiler can tell which direct-to-LDS load a read depends on
+    __shared__ __attribute__((aligned(16))) uint32_t sz_ring0[4 * TILES][2 * TOK];
+    __shared__ __attribute__((aligned(16))) uint32_t sz_ring1[4 * TILES][2 * TOK];
+    __shared__ __attribute__((aligned(16))) uint32_t sz_ring2[4 * TILES][2 * TOK];
+    __shared__ typename Form::Join s_join[TILES];
     __shared__ uint32_t s_last;
-    __shared__ u32x2 s_sums[4][64];
-    __shared__ u32x4 s_seqs[4][64];
+    __shared__ u32x2 s_sums[4 * TILES][64];
+    __shared__ u32x4 s_seqs[4 * TILES][64];
     const int tid = threadIdx.x, lane = tid & 63;
-    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int c = lane & 15, h = lane >> 4;
+    const int any_wave = __builtin_amdgcn_readfirstlane(tid >> 6), wave = any_wave / TILES, part = any_wave % TILES;      // part: the wave's tile
+    const int c = Form::kCols * part + Form::column(lane);   // column of the segment
     const int G = q_heads / pool.heads;
 
     // ---- this CTA's piece of the work
@@ -86,12 +182,15 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(BITS == 4 &
             n = q ? (uint32_t)(tiles_of(own) * pool.heads) : 0u;
         }
         const uint32_t segments = wave_total(n), all = wave_total(n * q);
-        if (2 * segments <= ctas && all <= kAlignedQuads * ctas) {
-            const uint32_t longest = wave_greatest(q), single = (longest + kGroupPieces - 1) / kGroupPieces;
-            piece = max((all + ctas - segments - 1) / (ctas - segments), kLeastQuads);
+        if (segments <= ctas) {
+            const uint32_t ideal = max((all + ctas - 1) / ctas, kLeastQuads), loose = (all + kSegmentStart * segments) / ctas + kUnaligned;
+            uint32_t p = ideal;
+            while (p <= loose && wave_total(n * ((q + p - 1) / p)) > ctas) p += 1 + (p >> 4);
             // up to sixteen pieces are merged in one level, and a second one costs more than a quad; three quads take no longer than a merge
-            if (single <= piece + 1) piece = max(piece, single);
-            if (longest <= 3) piece = max(piece, longest);
+            const uint32_t longest = wave_greatest(q), single = (longest + kGroupPieces - 1) / kGroupPieces;
+            if (single <= p + 1) p = max(p, single);
+            if (longest <= 3) p = max(p, longest);
+            if (p <= loose) piece = p;
         }
     }
     const bool aligned = piece != 0;
@@ -105,26 +204,24 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(BITS == 4 &
     uint32_t total;
     {
         const SeqFinder finder = one_each ? SeqFinder(work_at, seqs.batch, work_of(own)) : SeqFinder(work_at, seqs.batch, lane);
-        s_sums[wave][lane] = u32x2{finder.mine, finder.incl};            // (not in registers through the loops below)
-        s_seqs[wave][lane] = u32x4{(uint32_t)own.row, (uint32_t)own.count, (uint32_t)own.pos, 0u};
+        s_sums[any_wave][lane] = u32x2{finder.mine, finder.incl};            // (not in registers through the loops below)
+        s_seqs[any_wave][lane] = u32x4{(uint32_t)own.row, (uint32_t)own.count, (uint32_t)own.pos, 0u};
         total = finder.total;
     }
     if (!aligned) piece = max((total + ctas - 1) / ctas, kLeastQuads);
     uint32_t at = blockIdx.x * piece;
     if (at >= total) return;
     const uint32_t end = min(at + piece, total);
-    uint32_t* const z0 = sz_ring0[wave];
-    uint32_t* const z1 = sz_ring1[wave];
-    uint32_t* const z2 = sz_ring2[wave];
+    auto ring = [&](int i) { return i == 0 ? sz_ring0[any_wave] : i == 1 ? sz_ring1[any_wave] : sz_ring2[any_wave]; };
     const Magic mg = make_magic();
 
     while (at < end) {
         uint32_t base;
-        const u32x2 sums = s_sums[wave][lane];
+        const u32x2 sums = s_sums[any_wave][lane];
         const int b = SeqFinder(work_at, seqs.batch, sums[0], sums[1]).find(at, base);
         auto sequence = [&](int i) {
             if (!one_each) return paged_seq(seqs, i);
-            const u32x4 held = s_seqs[wave][lane];
+            const u32x4 held = s_seqs[any_wave][lane];
             return PagedSeq{__builtin_amdgcn_readlane((int)held[0], i), __builtin_amdgcn_readlane((int)held[1], i), __builtin_amdgcn_readlane((int)held[2], i)};
         };
         const PagedSeq s = sequence(b);
@@ -139,16 +236,12 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(BITS == 4 &
 
         // ---- columns
         const int rows = s.count * G, r0 = tile * COLS;
-        const Column col(c, PACK, r0, s, G, seqs.cap);
+        const Column col(c, r0, s, G, seqs.cap);
         const int len = col.real ? (int)(s.pos + col.tok) + 1 : 0;
         const int last_tok = (min(r0 + COLS, rows) - 1) / G;
         const int len_all = (int)min(max((long)s.pos + last_tok + 1, 0L), (long)seqs.cap);
-        f16x8 qraw[4];
-        {
-            const uint16_t* qp = Q + (size_t)(s.row + col.tok) * q_stride + ((size_t)hk * G + col.head) * kHeadDim + 32 * h;
-#pragma unroll
-            for (int tt = 0; tt < 4; ++tt) qraw[tt] = *(const f16x8*)(qp + 8 * tt);
-        }
+        Form form;
+        form.request_query(Q + (size_t)(s.row + col.tok) * q_stride + ((size_t)hk * G + col.head) * kHeadDim, lane);
         const int blk1 = min((int)qb * 4, (len_all + TOK - 1) / TOK);
         int blk = (int)qa * 4 + wave;
 
@@ -192,98 +285,38 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(BITS == 4 &
             return present;
         };
 
-        BlockRegs g0, g1, g2;
-        BlockPages<PARTS> next = pages_of(blk);
-        BlockPages<PARTS> after = pages_of(blk + 4);
-        uint32_t there0 = load(g0, z0, blk, next);
+        BlockRegs g[3];
+        uint32_t there[3];
+        BlockPages<PARTS> next = pages_of(blk), after = pages_of(blk + 4);
+        there[0] = load(g[0], ring(0), blk, next);
         next = pages_of(blk + 8);
-        uint32_t there1 = load(g1, z1, blk + 4, after), there2 = 0;
-
-        f16x8 qf[4];
-        float qsum = 0.f, qbias = 0.f;
-#pragma unroll
-        for (int tt = 0; tt < 4; ++tt) {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) qf[tt][e] = col.real ? qraw[tt][e] : (_Float16)0.0f;
-            u32x4 bits = __builtin_bit_cast(u32x4, qf[tt]);
-            asm volatile("" : "+v"(bits.x), "+v"(bits.y), "+v"(bits.z), "+v"(bits.w));            // (keeps this arithmetic behind the requests above)
-            qf[tt] = __builtin_bit_cast(f16x8, bits);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                qsum += (float)qf[tt][e];
-                qbias += ((e & 2) ? 64.0f : 1024.0f) * (float)qf[tt][e];
-            }
-        }
-        qsum = xor_add(xor_add(qsum, 16), 32);
-        qbias = BITS == 8 ? 1024.0f * qsum : xor_add(xor_add(qbias, 16), 32);
-        const f32x4 neg_qbias = {-qbias, -qbias, -qbias, -qbias};
-
-        // The reference starts above the mask value: a wave may meet blocks in which a column has no live token.
-        SoftmaxState st{kMaskFloor, 0.f, 0.f, f32x4{0.f, 0.f, 0.f, 0.f}};
-        f32x4 acc[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) acc[i] = f32x4{0.f, 0.f, 0.f, 0.f};
-        auto step = [&](BlockRegs& use, uint32_t* zu, uint32_t there, BlockRegs& fill, uint32_t* zf, uint32_t& filled) {
-            filled = load(fill, zf, blk + 8, next);
+        there[1] = load(g[1], ring(1), blk + 4, after);
+        form.begin(col.real, scale_log2e);
+        auto step = [&](int use) {
+            const int fill = (use + 2) % 3;
+            there[fill] = load(g[fill], ring(fill), blk + 8, next);
             next = pages_of(blk + 12);
-            if constexpr (PARTS == 1)
-                process_block<BITS, PACK>(use, zu, qf, scale_log2e, qsum, neg_qbias, mg, blk, there ? len : 0, len_all, lane, st, acc);
-            else
-                process_block<BITS, PACK, true>(use, zu, qf, scale_log2e, qsum, neg_qbias, mg, blk, len, len_all, lane, st, acc, there);
+            form.template block<PARTS>(g[use], ring(use), mg, blk, len, len_all, lane, there[use]);
             blk += 4;
             return blk < blk1;
         };
         if (blk < blk1)
-            while (step(g0, z0, there0, g2, z2, there2) && step(g1, z1, there1, g0, z0, there0) && step(g2, z2, there2, g1, z1, there1)) {
+            while (step(0) && step(1) && step(2)) {
             }
+        float M, L, o[8];                                    // of the thread's column
+        form.join(s_join[part], wave, lane, M, L, o);
 
-        // ---- the four lanes of a column add their partial sums; the waves meet in LDS
-        float l_w = xor_add(xor_add(st.l_run, 16), 32);
-        float corr_w = xor_add(xor_add(st.corr, 16), 32);
-        if constexpr (PACK) {
-            l_w = xor_add(l_w, 8);
-            corr_w = xor_add(corr_w, 8);
-        }
-        if (h == 0) {
-            sm_ml[wave][0][c] = st.m_run;
-            sm_ml[wave][1][c] = l_w;
-        }
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-#pragma unroll
-            for (int rr = 0; rr < 4; ++rr) sm_out[wave][i][rr][lane] = (BITS == 8 ? acc[i][rr] + st.bias[rr] : acc[i][rr]) - corr_w;
-        __syncthreads();
-        float M = kNegBig;
-#pragma unroll
-        for (int w = 0; w < 4; ++w) M = fmaxf(M, sm_ml[w][0][c]);
-        float L = 0.f, f[4];
-#pragma unroll
-        for (int w = 0; w < 4; ++w) {
-            f[w] = exp2f(sm_ml[w][0][c] - M);
-            L += sm_ml[w][1][c] * f[w];
-        }
-        // thread (wave w, lane) has dimensions 16 * (2w + ii) + 4h + rr of its column
-        float o[2][4];
-#pragma unroll
-        for (int ii = 0; ii < 2; ++ii)
-#pragma unroll
-            for (int rr = 0; rr < 4; ++rr) {
-                o[ii][rr] = 0.f;
-#pragma unroll
-                for (int w = 0; w < 4; ++w) o[ii][rr] += sm_out[w][2 * wave + ii][rr][lane] * f[w];
-            }
         // What the loop above does not need is worked out again here rather than kept in registers through it.
         int b_again = b, r0_again = r0;
         asm volatile("" : "+s"(b_again), "+s"(r0_again));
         const PagedSeq t = sequence(b_again);
-        const Column out(c, PACK, r0_again, t, G, seqs.cap);
-        const bool writes = out.real && (!PACK || c < 8);
+        const Column out(c, r0_again, t, G, seqs.cap);
         auto finish = [&](float m_l) {
             const float inv = m_l > 0.f ? 1.0f / m_l : 0.f;
 #pragma unroll
-            for (int ii = 0; ii < 2; ++ii) {
-                const float v[4] = {o[ii][0] * inv, o[ii][1] * inv, o[ii][2] * inv, o[ii][3] * inv};
-                if (writes) store_out4(O, t.row + out.tok, q_heads, hk * G + out.head, 16 * (2 * wave + ii) + 4 * h, v);
+            for (int i = 0; i < 2; ++i) {
+                const float v[4] = {o[4 * i] * inv, o[4 * i + 1] * inv, o[4 * i + 2] * inv, o[4 * i + 3] * inv};
+                if (out.real && Form::owns(lane)) store_out4(O, t.row + out.tok, q_heads, hk * G + out.head, 16 * (2 * wave + i) + 4 * (lane >> 4), v);
             }
         };
         if (qa == 0 && qb == quads) {                        // (uniform) the whole segment was this CTA's
@@ -293,19 +326,17 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(BITS == 4 &
         }
 
         // ---- a piece of a segment.  Its slot: 2k + 1 for the segment that begins in CTA k, 2k for one that began before it.
-        const bool column = c < COLS && c + r0_again < t.count * G;
-        auto where = [&](int ii, int rr) { return 2 * COLS + ((4 * (2 * wave + ii) + rr) * 4 + h) * COLS + c; };
+        const bool column = Form::owns(lane) && c + r0_again < t.count * G;
+        auto where = [&](int i) { return 2 * COLS + ((8 * wave + i) * 4 + (lane >> 4)) * COLS + c; };
         auto put = [&](uint32_t slot) {
             float* const p = partial + (size_t)slot * kPartial;
             if (!column) return;
-            if (wave == 0 && h == 0) {
+            if (wave == 0 && lane < Form::kCols) {
                 st_partial(p + c, M);
                 st_partial(p + COLS + c, L);
             }
 #pragma unroll
-            for (int ii = 0; ii < 2; ++ii)
-#pragma unroll
-                for (int rr = 0; rr < 4; ++rr) st_partial(p + where(ii, rr), o[ii][rr]);
+            for (int i = 0; i < 8; ++i) st_partial(p + where(i), o[i]);
         };
         // Bumps a counter once all of this CTA's stores have arrived; true in every thread of the CTA that is the last of n, which also resets it.
         auto arrive = [&](uint32_t* counter, uint32_t n) {
@@ -325,54 +356,46 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(BITS == 4 &
         auto merge = [&](uint32_t j0, uint32_t stride, uint32_t n) {
             M = kNegBig, L = 0.f;
 #pragma unroll
-            for (int ii = 0; ii < 2; ++ii)
-#pragma unroll
-                for (int rr = 0; rr < 4; ++rr) o[ii][rr] = 0.f;
+            for (int i = 0; i < 8; ++i) o[i] = 0.f;
             if (!column) return;
-            for (uint32_t i0 = 0; i0 < n; i0 += kMergeLoads) {
-                float ms[kMergeLoads], ls[kMergeLoads], v[kMergeLoads][2][4];
+            for (uint32_t j = 0; j < n; j += kMergeLoads) {
+                float ms[kMergeLoads], ls[kMergeLoads], v[kMergeLoads][8];
 #pragma unroll
-                for (int i = 0; i < kMergeLoads; ++i) {
-                    const float* const p = partial + (size_t)slot_of(j0 + stride * (i0 + i < n ? i0 + i : 0)) * kPartial;
-                    ms[i] = ld_partial(p + c);
-                    ls[i] = ld_partial(p + COLS + c);
+                for (int k = 0; k < kMergeLoads; ++k) {
+                    const float* const p = partial + (size_t)slot_of(j0 + stride * (j + k < n ? j + k : 0)) * kPartial;
+                    ms[k] = ld_partial(p + c);
+                    ls[k] = ld_partial(p + COLS + c);
 #pragma unroll
-                    for (int ii = 0; ii < 2; ++ii)
-#pragma unroll
-                        for (int rr = 0; rr < 4; ++rr) v[i][ii][rr] = ld_partial(p + where(ii, rr));
+                    for (int i = 0; i < 8; ++i) v[k][i] = ld_partial(p + where(i));
                 }
                 float up = M;
 #pragma unroll
-                for (int i = 0; i < kMergeLoads; ++i) up = fmaxf(up, i0 + i < n ? ms[i] : kNegBig);
+                for (int k = 0; k < kMergeLoads; ++k) up = fmaxf(up, j + k < n ? ms[k] : kNegBig);
                 const float old = exp2f(M - up);
                 M = up;
                 L *= old;
 #pragma unroll
-                for (int ii = 0; ii < 2; ++ii)
+                for (int i = 0; i < 8; ++i) o[i] *= old;
 #pragma unroll
-                    for (int rr = 0; rr < 4; ++rr) o[ii][rr] *= old;
+                for (int k = 0; k < kMergeLoads; ++k) {
+                    const float f = j + k < n ? exp2f(ms[k] - M) : 0.f;
+                    L += ls[k] * f;
 #pragma unroll
-                for (int i = 0; i < kMergeLoads; ++i) {
-                    const float fi = i0 + i < n ? exp2f(ms[i] - M) : 0.f;
-                    L += ls[i] * fi;
-#pragma unroll
-                    for (int ii = 0; ii < 2; ++ii)
-#pragma unroll
-                        for (int rr = 0; rr < 4; ++rr) o[ii][rr] += v[i][ii][rr] * fi;
+                    for (int i = 0; i < 8; ++i) o[i] += v[k][i] * f;
                 }
             }
         };
         const uint32_t mine = (at - 1) / piece - k0;         // this piece's number
-        const uint32_t groups = (pieces + kGroupPieces - 1) / kGroupPieces, g = mine / kGroupPieces;
-        const uint32_t in_group = min((uint32_t)kGroupPieces, pieces - g * kGroupPieces);
+        const uint32_t groups = (pieces + kGroupPieces - 1) / kGroupPieces, group = mine / kGroupPieces;
+        const uint32_t in_group = min((uint32_t)kGroupPieces, pieces - group * kGroupPieces);
         put(slot_of(mine));
         // Counters: of the first group, [CTA in which the segment begins]; of a later one, [CTA of its first piece] - only one segment enters a CTA from before; of the
         // groups of a segment, [CTA in which it begins].
-        if (!arrive(counters + (g == 0 ? k0 : gridDim.x + k0 + g * kGroupPieces), in_group)) continue;
-        merge(g * kGroupPieces, 1, in_group);
+        if (!arrive(counters + (group == 0 ? k0 : gridDim.x + k0 + group * kGroupPieces), in_group)) continue;
+        merge(group * kGroupPieces, 1, in_group);
         if (groups > 1) {
             __syncthreads();                                 // all of the group has been read before its first slot is written
-            put(slot_of(g * kGroupPieces));
+            put(slot_of(group * kGroupPieces));
             if (!arrive(counters + 2 * gridDim.x + k0, groups)) continue;
             merge(0, kGroupPieces, groups);
         }
@@ -382,19 +405,21 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(BITS == 4 &
 
 }  // namespace
 
-hipError_t launch_paged_columns(const PagedPool& pool, const PagedSeqs& seqs, const uint16_t* Q, long q_stride, uint16_t* O, int q_heads, float scale, bool pack,
+hipError_t launch_paged_columns(const PagedPool& pool, const PagedSeqs& seqs, const uint16_t* Q, long q_stride, uint16_t* O, int q_heads, float scale, int columns,
                                 int most_rows, int grid, void* workspace, hipStream_t stream)
 {
     static_assert(3 * kPagedMostCtas * sizeof(uint32_t) <= kPagedCounterBytes, "three counters a CTA");
-    static_assert(2 * kPagedMostCtas * 16 * (2 + kHeadDim) * sizeof(float) <= kPagedPartialBytes, "two slots a CTA");
+    static_assert(2 * kPagedMostCtas * 32 * (2 + kHeadDim) * sizeof(float) <= kPagedPartialBytes, "two slots a CTA");
     if (grid < 1 || grid > kPagedMostCtas) return hipErrorInvalidValue;
     uint32_t* const counters = (uint32_t*)workspace;
     float* const partial = (float*)((char*)workspace + kPagedCounterBytes);
     const float s = scale * 1.4426950408889634f;
-    const auto kernel = pool.bits == 8        ? (pack ? paged_columns_kernel<8, true, 1> : paged_columns_kernel<8, false, 1>)
-                        : pool.run_log == 0 ? (pack ? paged_columns_kernel<4, true, 2> : paged_columns_kernel<4, false, 2>)
-                                            : (pack ? paged_columns_kernel<4, true, 1> : paged_columns_kernel<4, false, 1>);
-    hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(256), 0, stream, pool, seqs, Q, q_stride, O, q_heads, s, most_rows, partial, counters);
+    const bool halves = pool.run_log == 0;
+    auto pick = [&](auto c8, auto c16, auto c32) { return columns == 8 ? c8 : columns == 16 ? c16 : c32; };
+    const auto kernel = pool.bits == 8 ? pick(paged_columns_kernel<8, true, 1, 1>, paged_columns_kernel<8, false, 1, 1>, paged_columns_kernel<8, false, 1, 2>)
+                        : halves       ? pick(paged_columns_kernel<4, true, 2, 1>, paged_columns_kernel<4, false, 2, 1>, paged_columns_kernel<4, false, 2, 2>)
+                                       : pick(paged_columns_kernel<4, true, 1, 1>, paged_columns_kernel<4, false, 1, 1>, paged_columns_kernel<4, false, 1, 2>);
+    hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(columns == 32 ? 512 : 256), 0, stream, pool, seqs, Q, q_stride, O, q_heads, s, most_rows, partial, counters);
     return hipGetLastError();
 }
 

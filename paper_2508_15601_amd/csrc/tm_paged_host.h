@@ -10,7 +10,7 @@ constexpr size_t kPagedCounterBytes = 16 * 1024;
 constexpr size_t kPagedPartialBytes = 48u << 20;
 constexpr size_t kPagedWorkspaceBytes = kPagedCounterBytes + kPagedPartialBytes;
 
-constexpr int kPagedMostCtas = 1024;     // of a launch whose CTAs share contexts
+constexpr int kPagedMostCtas = 512;      // of a launch whose CTAs share contexts
 
 struct PagedRows {                       // a packed array of new tokens: row r at p + r * stride
     const uint16_t* p;
@@ -23,15 +23,14 @@ hipError_t launch_rope(const uint16_t* X, long x_stride, const int32_t* position
 hipError_t launch_paged_append(const PagedPool& pool, const PagedSeqs& seqs, PagedRows k, PagedRows v, const RopePlan* rope, PagedRows q, uint16_t* q_out,
                                long q_out_stride, int q_heads, hipStream_t stream);
 hipError_t launch_paged_read(const PagedPool& pool, const PagedSeqs& seqs, uint16_t* K, uint16_t* V, hipStream_t stream);
-// The new tokens of sequences with up to most_rows (token, query head of a KV head) rows; pack: columns by eight instead of sixteen.  Every CTA of `grid` takes an equal
+// The new tokens of sequences with up to most_rows (token, query head of a KV head) rows; `columns` of them at a time, 8, 16 or 32.  Every CTA of `grid` takes an equal
 // piece of the work.
-hipError_t launch_paged_columns(const PagedPool& pool, const PagedSeqs& seqs, const uint16_t* Q, long q_stride, uint16_t* O, int q_heads, float scale, bool pack,
+hipError_t launch_paged_columns(const PagedPool& pool, const PagedSeqs& seqs, const uint16_t* Q, long q_stride, uint16_t* O, int q_heads, float scale, int columns,
                                 int most_rows, int grid, void* workspace, hipStream_t stream);
 
 // How a call is divided: sequences with at least least_rows rows in CTAs of 32 * row_waves rows (row_waves = 0: none), the others by columns (column_rows = 0: none).
 struct PagedForm {
-    int column_rows, column_ctas;
-    bool pack;
+    int columns, column_rows, column_ctas;
     int least_rows, row_waves, pieces, piece_stages;
     uint32_t items;
 };

@@ -154,7 +154,7 @@ PagedForm paged_form(const PagedPool& pool, const PagedSeqs& seqs, int q_heads, 
     const int G = q_heads / pool.heads;
     PagedForm f{};
     const long most = (long)(max_count > 0 && max_count < seqs.tokens ? max_count : seqs.tokens) * G;
-    f.pack = G <= 8 && (most <= 8 || most > 64);
+    f.columns = most > 64 ? G <= 8 ? 8 : 16 : most <= 8 ? 8 : most <= 16 ? 16 : 32;
     f.column_rows = most <= 64 ? 64 : seqs.batch > 1 ? 16 : 0;
     f.column_ctas = num_cu < kPagedMostCtas ? num_cu : kPagedMostCtas;
     if (most <= 64) {
@@ -202,7 +202,7 @@ hipError_t launch_paged_attn(const PagedPool& pool, const PagedSeqs& seqs, const
                                  : launch<4, 4>(pool, seqs, Q, q_stride, O, q_heads, scale, plan, partial, stream);
     }
     if (e == hipSuccess && f.column_rows)
-        e = launch_paged_columns(pool, seqs, Q, q_stride, O, q_heads, scale, f.pack, f.column_rows, f.column_ctas, workspace, stream);
+        e = launch_paged_columns(pool, seqs, Q, q_stride, O, q_heads, scale, f.columns, f.column_rows, f.column_ctas, workspace, stream);
     return e;
 }
 

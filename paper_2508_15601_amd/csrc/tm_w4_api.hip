@@ -2239,7 +2239,7 @@ int tm_get_paged_plan(const tm_paged_cache* cache, const tm_paged_batch* batch, 
     const int rc = check_paged_attn(cache, batch, q_heads, &seqs);
     if (rc != TM_OK) return rc;
     const PagedForm f = paged_form(cache->pool, seqs, q_heads, batch->max_count, batch->max_len, g_dev[cache->device].num_cu);
-    if (columns) *columns = !f.column_rows ? 0 : f.pack ? 8 : 16;
+    if (columns) *columns = f.column_rows ? f.columns : 0;
     if (column_rows) *column_rows = f.column_rows;
     if (rows) *rows = 32 * f.row_waves;
     if (pieces) *pieces = f.row_waves ? f.pieces : 0;

@@ -106,12 +106,12 @@ FEW = [
     (32, 2, 8, [1, 1, 1], [0, 31, 32], 8),                                 # last slot of a page, first of the next
     (64, 2, 10, [1, 1, 1, 1], [127, 128, 700, 63], 8),                     # blocks of 8- and 4-bit codes that end inside a page
     (32, 1, 16, [1, 1], [500, 99], 16),
-    (128, 1, 40, [1, 1], [300, 17], 16),                                   # more query heads than columns
-    (64, 1, 64, [1], [1000], 16),
-    (256, 2, 14, [2, 0, 4, 1], [1000, 5, 254, 0], 16),                     # drafted tokens; a sequence without any
+    (128, 1, 40, [1, 1], [300, 17], 32),                                   # more query heads than columns
+    (64, 1, 64, [1], [1000], 32),
+    (256, 2, 14, [2, 0, 4, 1], [1000, 5, 254, 0], 32),                     # drafted tokens; a sequence without any
     (32, 3, 3, [8, 3], [90, 0], 8),
-    (1024, 1, 5, [5, 5], [1500, 1], 16),
-    (64, 2, 8, [16, 13], [200, 64], 16),                                   # several column tiles of a sequence
+    (1024, 1, 5, [5, 5], [1500, 1], 32),
+    (64, 2, 8, [16, 13], [200, 64], 32),                                   # several column tiles of a sequence
 ]
 
 
