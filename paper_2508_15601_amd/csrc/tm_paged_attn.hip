@@ -21,6 +21,7 @@ namespace {
 
 constexpr int kGroupPieces = 16;         // pieces merged at a time
 constexpr int kMergeLoads = 8;           // of them in flight at once
+constexpr int kAgentScope = 16;          // cache-policy bit (sc1) of a store that goes through to memory, and of a load that sees such stores of other XCDs
 constexpr uint32_t kSegmentStart = 2;    // what beginning a segment costs, in quads
 constexpr uint32_t kUnaligned = 4;       // what a CTA pays for not beginning with a segment: most of them have one more to begin, and two to hand on
 
@@ -152,7 +153,7 @@ __global__ __launch_bounds__(256 * TILES) __attribute__((amdgpu_waves_per_eu(BIT
     static_assert(PARTS == 1 || (BITS == 4 && PARTS == RUNS), "a part is a run, or the whole block");
     typedef Columns<BITS, PACK> Form;
     constexpr int COLS = Form::kCols * TILES;                // of a segment
-    constexpr int kPartial = COLS * (2 + kHeadDim);          // m, l, unnormalised outputs of every column
+    constexpr int kPartial = 2 * COLS + 2048 * TILES;        // M and L of every column, eight unnormalised values a thread
     // scale/zero words of the blocks in flight; one array per ring slot so that the compiler can tell which direct-to-LDS load a read depends on
     __shared__ __attribute__((aligned(16))) uint32_t sz_ring0[4 * TILES][2 * TOK];
     __shared__ __attribute__((aligned(16))) uint32_t sz_ring1[4 * TILES][2 * TOK];
@@ -327,16 +328,21 @@ __global__ __launch_bounds__(256 * TILES) __attribute__((amdgpu_waves_per_eu(BIT
 
         // ---- a piece of a segment.  Its slot: 2k + 1 for the segment that begins in CTA k, 2k for one that began before it.
         const bool column = Form::owns(lane) && c + r0_again < t.count * G;
-        auto where = [&](int i) { return 2 * COLS + ((8 * wave + i) * 4 + (lane >> 4)) * COLS + c; };
+        // Slots are written through to memory and read past the caches of this XCD, sixteen bytes a lane: M and L of every column, then the threads' values in two rounds of 1 KiB a wave.
+        const __amdgpu_buffer_rsrc_t slots = make_rsrc(partial, (uint32_t)kPagedPartialBytes);
+        const int value_at = 2 * COLS * 4 + any_wave * 2048 + lane * 16;
         auto put = [&](uint32_t slot) {
-            float* const p = partial + (size_t)slot * kPartial;
+            const int base = (int)(slot * (uint32_t)(kPartial * 4));
             if (!column) return;
             if (wave == 0 && lane < Form::kCols) {
-                st_partial(p + c, M);
-                st_partial(p + COLS + c, L);
+                __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(uint32_t, M), slots, base + c * 4, 0, kAgentScope);
+                __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(uint32_t, L), slots, base + (COLS + c) * 4, 0, kAgentScope);
             }
 #pragma unroll
-            for (int i = 0; i < 8; ++i) st_partial(p + where(i), o[i]);
+            for (int i = 0; i < 2; ++i) {
+                const f32x4 v = {o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]};
+                __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, v), slots, base + value_at + i * 1024, 0, kAgentScope);
+            }
         };
         // Bumps a counter once all of this CTA's stores have arrived; true in every thread of the CTA that is the last of n, which also resets it.
         auto arrive = [&](uint32_t* counter, uint32_t n) {
@@ -359,14 +365,15 @@ __global__ __launch_bounds__(256 * TILES) __attribute__((amdgpu_waves_per_eu(BIT
             for (int i = 0; i < 8; ++i) o[i] = 0.f;
             if (!column) return;
             for (uint32_t j = 0; j < n; j += kMergeLoads) {
-                float ms[kMergeLoads], ls[kMergeLoads], v[kMergeLoads][8];
+                float ms[kMergeLoads], ls[kMergeLoads];
+                f32x4 v[kMergeLoads][2];
 #pragma unroll
                 for (int k = 0; k < kMergeLoads; ++k) {
-                    const float* const p = partial + (size_t)slot_of(j0 + stride * (j + k < n ? j + k : 0)) * kPartial;
-                    ms[k] = ld_partial(p + c);
-                    ls[k] = ld_partial(p + COLS + c);
+                    const int base = (int)(slot_of(j0 + stride * (j + k < n ? j + k : 0)) * (uint32_t)(kPartial * 4));
+                    ms[k] = __builtin_bit_cast(float, (uint32_t)__builtin_amdgcn_raw_buffer_load_b32(slots, base + c * 4, 0, kAgentScope));
+                    ls[k] = __builtin_bit_cast(float, (uint32_t)__builtin_amdgcn_raw_buffer_load_b32(slots, base + (COLS + c) * 4, 0, kAgentScope));
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) v[k][i] = ld_partial(p + where(i));
+                    for (int i = 0; i < 2; ++i) v[k][i] = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(slots, base + value_at + i * 1024, 0, kAgentScope));
                 }
                 float up = M;
 #pragma unroll
@@ -381,7 +388,7 @@ __global__ __launch_bounds__(256 * TILES) __attribute__((amdgpu_waves_per_eu(BIT
                     const float f = j + k < n ? exp2f(ms[k] - M) : 0.f;
                     L += ls[k] * f;
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) o[i] += v[k][i] * f;
+                    for (int i = 0; i < 8; ++i) o[i] += v[k][i >> 2][i & 3] * f;
                 }
             }
         };
@@ -409,7 +416,7 @@ hipError_t launch_paged_columns(const PagedPool& pool, const PagedSeqs& seqs, co
                                 int most_rows, int grid, void* workspace, hipStream_t stream)
 {
     static_assert(3 * kPagedMostCtas * sizeof(uint32_t) <= kPagedCounterBytes, "three counters a CTA");
-    static_assert(2 * kPagedMostCtas * 32 * (2 + kHeadDim) * sizeof(float) <= kPagedPartialBytes, "two slots a CTA");
+    static_assert(2 * kPagedMostCtas * (2 * 32 + 2 * 2048) * sizeof(float) <= kPagedPartialBytes, "two slots a CTA");
     if (grid < 1 || grid > kPagedMostCtas) return hipErrorInvalidValue;
     uint32_t* const counters = (uint32_t*)workspace;
     float* const partial = (float*)((char*)workspace + kPagedCounterBytes);
