@@ -82,12 +82,15 @@ __device__ __forceinline__ void attn_rows(const RowsJob& job, const uint8_t* kco
     const __amdgpu_buffer_rsrc_t zrs = make_rsrc(words, (uint32_t)len_all * 8u);    // zeros past the context
     u32x4 codes[BITS == 8 ? 2 : 1];                                                 // 16-byte chunks of a thread and stage
     u32x2 pairs = {0u, 0u};
-    // Paged: numbers in the pool of a stage's two runs, -1 where there is none; the run whose codes this wave stages is `mine`.
+    // Paged: numbers in the pool of a stage's two runs, -1 where there is none; the run whose codes this wave stages is `mine`.  (A pool of 2^31 runs would take 4 TB.)
     struct StageRuns {
-        long at[2];
+        int at[2];
     };
     constexpr int kChunks = BITS == 8 ? 256 : 128;                                  // of 16 bytes a run
     const int mine = (BITS == 8 ? wave >> 2 : wave >> 1) & 1;
+    // Entries of the table for 64 pages at a time, a lane each: one wait for the table in 64 pages.  Loading the entry of a run when its turn comes made all
+    // waves stand still twice a stage.
+    int ids = -1, ids_at = -64;                            // of pages ids_at .. ids_at + 63 of the sequence
     auto runs_of = [&](int st) {
         StageRuns r{{-1, -1}};
         if constexpr (PAGED) {
@@ -95,8 +98,13 @@ __device__ __forceinline__ void attn_rows(const RowsJob& job, const uint8_t* kco
             for (int n = 0; n < 2; ++n) {
                 const int run = (tok0 >> 5) + 2 * st + n;
                 if (run * kRun >= len_all) continue;
-                const int page = paged_page(where.pool, where.seqs, where.b, run);
-                if (page >= 0) r.at[n] = (long)paged_run(where.pool, page, where.hk, run);
+                const int page = run >> where.pool.run_log;
+                if (page >= ids_at + 64) {
+                    ids_at = page;
+                    ids = page + lane < where.seqs.max_pages ? where.seqs.table[(size_t)where.b * where.seqs.max_pages + page + lane] : -1;
+                }
+                const int id = __builtin_amdgcn_readlane(ids, page - ids_at);
+                if ((uint32_t)id < (uint32_t)where.pool.pages) r.at[n] = (int)paged_run(where.pool, id, where.hk, run);
             }
         }
         return r;
@@ -111,7 +119,7 @@ __device__ __forceinline__ void attn_rows(const RowsJob& job, const uint8_t* kco
     };
     auto load_codes = [&](int st, const StageRuns& r) {
         if constexpr (PAGED) {
-            const long run = mine ? r.at[1] : r.at[0];
+            const int run = mine ? r.at[1] : r.at[0];
             const uint32_t bytes = run >= 0 ? kRunBytes : 0u;
             const size_t at = (size_t)(run >= 0 ? run : 0) * kRunBytes;
             const int off = (tid & (kChunks - 1)) * 16;
@@ -132,13 +140,8 @@ __device__ __forceinline__ void attn_rows(const RowsJob& job, const uint8_t* kco
     };
     auto load_pairs = [&](int st, const StageRuns& r) {
         if constexpr (PAGED) {
-            if (tid < ST) {                                // wave 0: lanes 0 .. 31 the first run
-                const __amdgpu_buffer_rsrc_t za = make_rsrc(words + (size_t)(r.at[0] >= 0 ? r.at[0] : 0) * (kRun * 2), r.at[0] >= 0 ? kRun * 8u : 0u);
-                const __amdgpu_buffer_rsrc_t zb = make_rsrc(words + (size_t)(r.at[1] >= 0 ? r.at[1] : 0) * (kRun * 2), r.at[1] >= 0 ? kRun * 8u : 0u);
-                const u32x2 a = __builtin_amdgcn_raw_buffer_load_b64(za, tid * 8, 0, 0);              // zeros outside the run
-                const u32x2 b = __builtin_amdgcn_raw_buffer_load_b64(zb, tid * 8 - kRun * 8, 0, 0);
-                pairs = u32x2{a.x | b.x, a.y | b.y};
-            }
+            if (tid < ST)                                  // wave 0: lanes 0 .. 31 the first run.  What stands in for a run that is not there (the pool's first) is masked.
+                pairs = *(const u32x2*)(words + ((size_t)(uint32_t)max(tid < kRun ? r.at[0] : r.at[1], 0) * kRun + (tid & (kRun - 1))) * 2);
             (void)st;
         } else {
             if (tid < ST) pairs = __builtin_amdgcn_raw_buffer_load_b64(zrs, (st * ST + tid) * 8, 0, 0);
@@ -276,12 +279,13 @@ __device__ __forceinline__ void attn_rows(const RowsJob& job, const uint8_t* kco
         }
     };
     // x = s * scale - ref; masked: tokens from the row's length on get kNegBig.  t0: first of the 32 tokens
-    auto scale_scores = [&](const f32x16& s, float ref, auto MASKED, int t0, bool there) {
+    auto scale_scores = [&](const f32x16& s, float ref, bool masked, int t0, bool there) {
         const int rem = !PAGED || there ? len - t0 - 4 * hl : -1;
 #pragma unroll
-        for (int e = 0; e < 16; ++e) {
-            const float v = __builtin_fmaf(s[e], ks[e >> 2][e & 3], -ref);
-            x[e] = !decltype(MASKED)::value || ((e >> 2) & 1) * 16 + (e >> 3) * 8 + (e & 3) < rem ? v : kNegBig;
+        for (int e = 0; e < 16; ++e) x[e] = __builtin_fmaf(s[e], ks[e >> 2][e & 3], -ref);
+        if (masked) {
+#pragma unroll
+            for (int e = 0; e < 16; ++e) x[e] = ((e >> 2) & 1) * 16 + (e >> 3) * 8 + (e & 3) < rem ? x[e] : kNegBig;
         }
         mx = x[0];
 #pragma unroll
@@ -294,9 +298,9 @@ __device__ __forceinline__ void attn_rows(const RowsJob& job, const uint8_t* kco
         const int t0 = first_token(0, 0);
         const f32x16 s = multiply_k(kbase + (KS > 1 ? ksg : 0) * 8192);
         read_scales(pbase, KS > 1 ? ksg : 0);
-        scale_scores(s, 0.f, std::true_type{}, t0, is_there(0, 0));
+        scale_scores(s, 0.f, true, t0, is_there(0, 0));
         m_run = fmaxf(fmaxf(mx, other_half(mx)), kMaskFloor);
-        scale_scores(s, m_run, std::true_type{}, t0, is_there(0, 0));
+        scale_scores(s, m_run, true, t0, is_there(0, 0));
     }
 
     for (int st = 0; st < nst; ++st) {
@@ -350,13 +354,12 @@ __device__ __forceinline__ void attn_rows(const RowsJob& job, const uint8_t* kco
                     // up from the lowest reference would leave nothing of them.  (Its sums are still zero.)
                     const bool fresh = m_run == kMaskFloor && len > t_n;
                     if (__any(fresh)) {
-                        scale_scores(s, 0.f, std::true_type{}, t_n, there);
+                        scale_scores(s, 0.f, true, t_n, there);
                         const float ref = fmaxf(fmaxf(mx, other_half(mx)), kMaskFloor);
                         if (fresh) m_run = ref;
                     }
                 }
-                if (t_n + 32 > wmin || !there) scale_scores(s, m_run, std::true_type{}, t_n, there);
-                else scale_scores(s, m_run, std::false_type{}, t_n, there);
+                scale_scores(s, m_run, t_n + 32 > wmin || !there, t_n, there);
             }
         }
     }

@@ -91,8 +91,8 @@ struct SeqFinder {
         incl = wave_sums(mine);
         total = (uint32_t)__builtin_amdgcn_readlane((int)incl, 63);
     }
-    // Up to 64 sequences, a lane's work known already.
-    __device__ __forceinline__ SeqFinder(F f, int sequences, uint32_t own) : units_of(f), per(1), batch(sequences), mine(own)
+    // A lane's work known already.
+    __device__ __forceinline__ SeqFinder(F f, int sequences, uint32_t own) : units_of(f), per((sequences + 63) / 64), batch(sequences), mine(own)
     {
         incl = wave_sums(mine);
         total = (uint32_t)__builtin_amdgcn_readlane((int)incl, 63);

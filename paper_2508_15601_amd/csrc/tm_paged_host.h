@@ -7,7 +7,7 @@ namespace tmw4 {
 
 // Workspace of tm_paged_attn: arrival counters, then partial results of contexts that are cut into pieces.
 constexpr size_t kPagedCounterBytes = 16 * 1024;
-constexpr size_t kPagedPartialBytes = 48u << 20;
+constexpr size_t kPagedPartialBytes = 66u << 20;          // 520 pieces of 256 rows
 constexpr size_t kPagedWorkspaceBytes = kPagedCounterBytes + kPagedPartialBytes;
 
 constexpr int kPagedMostCtas = 512;      // of a launch whose CTAs share contexts
@@ -31,7 +31,7 @@ hipError_t launch_paged_columns(const PagedPool& pool, const PagedSeqs& seqs, co
 // How a call is divided: sequences with at least least_rows rows in CTAs of 32 * row_waves rows (row_waves = 0: none), the others by columns (column_rows = 0: none).
 struct PagedForm {
     int columns, column_rows, column_ctas;
-    int least_rows, row_waves, pieces, piece_stages;
+    int least_rows, row_waves, pieces, target;
     uint32_t items;
 };
 PagedForm paged_form(const PagedPool& pool, const PagedSeqs& seqs, int q_heads, int max_count, int max_len, int num_cu);

@@ -168,6 +168,18 @@ def test_pieces_of_a_chunk(tm, bits):
 
 
 @pytest.mark.parametrize("bits", [8, 4])
+@pytest.mark.parametrize("counts, positions, heads, q_heads", [
+    ([300, 90, 200], [4000, 2500, 100], 1, 4),                             # cut into different numbers of pieces, one into none
+    ([1] * 40 + [70] + [1] * 40 + [33, 150], [50 * i for i in range(40)] + [3000] + [9 * i for i in range(40)] + [1200, 0], 1, 8),   # more sequences than lanes
+    ([64, 0, 64, 2], [6000, 100, 5900, 3000], 2, 4),
+])
+def test_pieces_of_several_chunks(tm, bits, counts, positions, heads, q_heads):
+    s = Setup(tm, bits, 64, heads, counts, positions, q_heads=q_heads, before=2, behind=1, seed=len(counts), max_count=max(counts))
+    assert s.plan()[3] > 4
+    s.check()
+
+
+@pytest.mark.parametrize("bits", [8, 4])
 def test_mixed(tm, bits):
     """Decoding sequences, drafts, chunks and prompts in one call."""
     counts = [1, 1, 90, 1, 0, 5, 1, 33, 1, 170, 1, 2]
