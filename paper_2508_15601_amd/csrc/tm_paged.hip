@@ -199,6 +199,82 @@ __global__ __launch_bounds__(256) void paged_append_kernel(PagedPool pool, Paged
     rotate_row(seqs, q, q_out, q_out_stride, q_heads, rope, row, h0, min(h0 + per_wave, q_heads), cs + wave * (kHeadDim / 2), lane);
 }
 
+// Few new tokens a sequence (a decoding step, drafts): a wave takes four of a token's vectors - keys of the KV heads, their values, then query heads - and puts codes where they
+// belong by itself; the CTAs above would each go through LDS for a token or a few.  Waves are numbered over the sequences, `step` tokens each; a sequence with more has the further
+// ones follow in the same waves.
+constexpr int kFewTokens = 8;
+template <int BITS>
+__global__ __launch_bounds__(256) void paged_append_tokens_kernel(PagedPool pool, PagedSeqs seqs, PagedRows k, PagedRows v, RopePlan rope, PagedRows q, uint16_t* q_out,
+                                                                  long q_out_stride, int q_heads, int per_token, int step)
+{
+    __shared__ CosSin cs[4][kHeadDim / 2];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), sub = lane & 15;
+    const uint32_t job = blockIdx.x * 4 + wave;
+    const uint32_t token = job / (uint32_t)per_token;
+    const int b = (int)(token / (uint32_t)step), vec = (int)(job - token * per_token) * 4 + (lane >> 4);
+    if (b >= seqs.batch) return;
+    const PagedSeq s = paged_seq(seqs, b);
+    const int which = vec < pool.heads ? 0 : vec < 2 * pool.heads ? 1 : 2, h = vec - which * pool.heads;   // keys, values, queries
+    for (int i = (int)(token - (uint32_t)b * step); i < s.count; i += step) {
+        const int pos = (int)((uint32_t)s.pos + (uint32_t)i);
+        const long row = (long)s.row + i;
+        const int page = pos >= 0 && pos < seqs.cap ? paged_page(pool, seqs, b, pos / kRun) : -1;
+        const PagedRows& from = which == 0 ? k : which == 1 ? v : q;
+        u32x4 raw = {0u, 0u, 0u, 0u};
+        if (which < 2 || h < q_heads) raw = *(const u32x4*)(from.p + row * from.stride + h * kHeadDim + 8 * sub);
+        if (rope.rot) {
+            rope_angles(cs[wave], rope, pos, lane);
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            __builtin_amdgcn_wave_barrier();
+            const u32x4 turned = rope_sixteenth(raw, rope, cs[wave], lane);
+            if (which != 1) raw = turned;
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            __builtin_amdgcn_wave_barrier();
+        }
+        if (which == 2) {
+            if (h < q_heads) *(u32x4*)(q_out + row * q_out_stride + h * kHeadDim + 8 * sub) = raw;
+        }
+        uint32_t code[8];
+        const uint32_t pair = quantise_row8<BITS>(raw, code);
+        if (page < 0 || which == 2) continue;
+        const int u = pos & (kRun - 1), hh = (u & 15) >> 2, e = (u & 3) + 4 * (u >> 4);
+        const size_t run = paged_run(pool, page, h, pos / kRun);
+        if (sub == 0) pool.pairs[(run * kRun + u) * 2 + which] = pair;
+        if constexpr (BITS == 8) {
+            if (which == 0) {
+                const int d = 8 * sub, chunk = ((u >> 4) * 2 + ((d & 31) >> 4)) * 64 + 16 * (d >> 5) + (u & 15);
+                *reinterpret_cast<u32x2*>(pool.k + run * 4096 + chunk * 16 + (d & 15)) =
+                    u32x2{code[0] | (code[1] << 8) | (code[2] << 16) | (code[3] << 24), code[4] | (code[5] << 8) | (code[6] << 16) | (code[7] << 24)};
+            } else {
+                uint8_t* const at = pool.v + run * 4096 + ((sub >> 2) * 64 + 16 * hh + 8 * (sub & 1)) * 16 + (sub >> 1 & 1) * 8 + e;
+#pragma unroll
+                for (int n = 0; n < 8; ++n) at[16 * n] = (uint8_t)code[n];
+            }
+        } else if (which == 0) {
+            uint32_t w = 0;
+#pragma unroll
+            for (int n = 0; n < 8; ++n) w |= code[n] << (4 * ((n >> 1) + 4 * (n & 1)));
+            reinterpret_cast<uint32_t*>(pool.k + run * 2048)[((u >> 4) * 64 + 16 * (sub >> 2) + (u & 15)) * 4 + (sub & 3)] = w;
+        } else {                                                       // a word holds a dimension of eight tokens
+            uint32_t* const at = reinterpret_cast<uint32_t*>(pool.v + run * 2048) + ((sub >> 3) * 64 + 16 * hh + 8 * (sub & 1)) * 4 + (sub >> 1 & 3);
+            const int sh = 4 * ((e >> 1) + 4 * (e & 1));
+            if (s.count == 1) {
+                uint32_t old[8];
+#pragma unroll
+                for (int n = 0; n < 8; ++n) old[n] = at[4 * n];
+#pragma unroll
+                for (int n = 0; n < 8; ++n) at[4 * n] = (old[n] & ~(0xfu << sh)) | (code[n] << sh);
+            } else {                                                   // others of them may be written at the same time, in any order: each leaves the others' bits alone
+#pragma unroll
+                for (int n = 0; n < 8; ++n) {
+                    __hip_atomic_fetch_and(at + 4 * n, ~(0xfu << sh), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                    __hip_atomic_fetch_or(at + 4 * n, code[n] << sh, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                }
+            }
+        }
+    }
+}
+
 // Reading back: 256 threads turn a run's 4 KiB (2 KiB) of key codes and as many of value codes into fp16 rows in LDS, [32 tokens][128] with rows 16 bytes apart
 // in the banks, and write whole 256-byte rows.  x = (q - z) * s: the product is exact in fp32 (8 + 11 bits), so there is one rounding.
 constexpr int kReadRow = kHeadDim + 8;   // fp16 values of an LDS row
@@ -280,9 +356,19 @@ long most_runs(const PagedSeqs& s)
 }  // namespace
 
 hipError_t launch_paged_append(const PagedPool& pool, const PagedSeqs& seqs, PagedRows k, PagedRows v, const RopePlan* rope, PagedRows q, uint16_t* q_out,
-                               long q_out_stride, int q_heads, hipStream_t stream)
+                               long q_out_stride, int q_heads, int max_count, hipStream_t stream)
 {
     const RopePlan plan = rope ? *rope : RopePlan{nullptr, 1.0, 0, 0};
+    // Measured (32 / 8 heads, 8-bit, queries too), in brackets by runs: one token each of 1, 16, 64 and 256 sequences 3.7, 4.0, 4.0 and 5.3 us (5.2, 5.4, 7.2, 19.5); five each of
+    // 12, 64 and 256 sequences 4.1, 6.4 and 14.4 us (5.5, 7.9, 27.6), eight 4.4, 7.9 and 20.1 (5.8, 8.5, 31.2).  Beyond that runs, whose tokens share their way to the page.
+    if (max_count >= 1 && max_count <= kFewTokens) {
+        const int heads = q.p ? q_heads : 0, per_token = (2 * pool.heads + heads + 3) / 4;
+        const long blocks = ((long)seqs.batch * max_count * per_token + 3) / 4;
+        if (blocks > 0x3fffffffL) return hipErrorInvalidValue;
+        const auto kernel = pool.bits == 8 ? paged_append_tokens_kernel<8> : paged_append_tokens_kernel<4>;
+        hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(256), 0, stream, pool, seqs, k, v, plan, q, q_out, q_out_stride, heads, per_token, max_count);
+        return hipGetLastError();
+    }
     const long kv = most_runs(seqs) * pool.heads;
     const int per_wave = (long)seqs.tokens * q_heads >= 16384L * 8 ? q_heads : 8;
     const long jobs = q.p ? (long)seqs.tokens * ((q_heads + per_wave - 1) / per_wave) : 0, blocks = kv + (jobs + 3) / 4;

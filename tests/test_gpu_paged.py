@@ -254,6 +254,26 @@ def test_many_sequences(tm, bits, batch):
     _check_read(tm, pool)
 
 
+ONE_EACH = SHAPES + [
+    (64, 8, [1] * 70, list(range(60, 130)), 3),                            # more sequences than lanes, four waves of vectors a token
+    (32, 5, [1, 0, 1], [0, 10, 63], 2),                                    # vectors that do not fill the last wave
+    (64, 2, [8, 5, 8, 7, 0, 8], [0, 3, 28, 57, 5, 120], 2),                # drafts: tokens that share bytes of 4-bit values
+]
+
+
+@pytest.mark.parametrize("bits", [8, 4])
+@pytest.mark.parametrize("page, heads, counts, positions, cols", ONE_EACH)
+@pytest.mark.parametrize("most, turn, q_heads", [(1, None, 1), (1, ("half", 128), 3), (1, ("half", 48), 40), (1, ("interleaved", 64), 6), (3, ("half", 128), 5), (8, None, 1),
+                                                 (9, ("half", 32), 2)])
+def test_append_with_a_hint(tm, bits, page, heads, counts, positions, cols, most, turn, q_heads):
+    """The hint of one token a sequence or a few, where it is true and where it is not."""
+    _say(f"append bits={bits} page={page} heads={heads} counts={counts[:8]} positions={positions[:8]} rope={turn} hint={most}")
+    pool = Pool(tm, bits, page, heads, counts, positions, cols, seed=sum(counts), before=2, behind=3, max_count=most)
+    rope = _rope(tm, turn[1], turn[0], base=500.0) if turn else None
+    _check_append(tm, pool, rope, q_heads=q_heads)
+    _check_read(tm, pool)
+
+
 @pytest.mark.parametrize("bits", [8, 4])
 def test_pages_that_do_not_exist(tm, bits):
     _say(f"append bad pages bits={bits}")
@@ -264,6 +284,8 @@ def test_pages_that_do_not_exist(tm, bits):
     pool.batch.table.copy_(_dev(table))
     _check_append(tm, pool, _rope(tm, 128))
     _check_read(tm, pool)
+    pool.batch = tm.PagedBatch(pool.batch.table, pool.batch.offsets, pool.batch.positions, max_count=1)
+    _check_append(tm, pool, _rope(tm, 128))
 
 
 def test_extreme_values_are_stored_as_by_the_contiguous_cache(tm):
