@@ -201,8 +201,9 @@ __global__ __launch_bounds__(256) void paged_append_kernel(PagedPool pool, Paged
 
 // Few new tokens a sequence (a decoding step, drafts): a wave takes four of a token's vectors - keys of the KV heads, their values, then query heads - and puts codes where they
 // belong by itself; the CTAs above would each go through LDS for a token or a few.  Waves are numbered over the sequences, `step` tokens each; a sequence with more has the further
-// ones follow in the same waves.
-constexpr int kFewTokens = 8;
+// ones follow in the same waves.  4-bit values of a sequence's tokens share bytes, so there a sequence's tokens all go through the same waves (step = 1).
+template <int BITS>
+constexpr int kFewTokens = BITS == 8 ? 8 : 1;
 template <int BITS>
 __global__ __launch_bounds__(256) void paged_append_tokens_kernel(PagedPool pool, PagedSeqs seqs, PagedRows k, PagedRows v, RopePlan rope, PagedRows q, uint16_t* q_out,
                                                                   long q_out_stride, int q_heads, int per_token, int step)
@@ -255,22 +256,14 @@ __global__ __launch_bounds__(256) void paged_append_tokens_kernel(PagedPool pool
 #pragma unroll
             for (int n = 0; n < 8; ++n) w |= code[n] << (4 * ((n >> 1) + 4 * (n & 1)));
             reinterpret_cast<uint32_t*>(pool.k + run * 2048)[((u >> 4) * 64 + 16 * (sub >> 2) + (u & 15)) * 4 + (sub & 3)] = w;
-        } else {                                                       // a word holds a dimension of eight tokens
+        } else {                                                       // a word holds a dimension of eight tokens, which this thread writes one after another
             uint32_t* const at = reinterpret_cast<uint32_t*>(pool.v + run * 2048) + ((sub >> 3) * 64 + 16 * hh + 8 * (sub & 1)) * 4 + (sub >> 1 & 3);
             const int sh = 4 * ((e >> 1) + 4 * (e & 1));
-            if (s.count == 1) {
-                uint32_t old[8];
+            uint32_t old[8];
 #pragma unroll
-                for (int n = 0; n < 8; ++n) old[n] = at[4 * n];
+            for (int n = 0; n < 8; ++n) old[n] = at[4 * n];
 #pragma unroll
-                for (int n = 0; n < 8; ++n) at[4 * n] = (old[n] & ~(0xfu << sh)) | (code[n] << sh);
-            } else {                                                   // others of them may be written at the same time, in any order: each leaves the others' bits alone
-#pragma unroll
-                for (int n = 0; n < 8; ++n) {
-                    __hip_atomic_fetch_and(at + 4 * n, ~(0xfu << sh), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-                    __hip_atomic_fetch_or(at + 4 * n, code[n] << sh, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-                }
-            }
+            for (int n = 0; n < 8; ++n) at[4 * n] = (old[n] & ~(0xfu << sh)) | (code[n] << sh);
         }
     }
 }
@@ -360,8 +353,9 @@ hipError_t launch_paged_append(const PagedPool& pool, const PagedSeqs& seqs, Pag
 {
     const RopePlan plan = rope ? *rope : RopePlan{nullptr, 1.0, 0, 0};
     // Measured (32 / 8 heads, 8-bit, queries too), in brackets by runs: one token each of 1, 16, 64 and 256 sequences 3.7, 4.0, 4.0 and 5.3 us (5.2, 5.4, 7.2, 19.5); five each of
-    // 12, 64 and 256 sequences 4.1, 6.4 and 14.4 us (5.5, 7.9, 27.6), eight 4.4, 7.9 and 20.1 (5.8, 8.5, 31.2).  Beyond that runs, whose tokens share their way to the page.
-    if (max_count >= 1 && max_count <= kFewTokens) {
+    // 12, 64 and 256 sequences 4.1, 6.4 and 14.4 us (5.5, 7.9, 27.6), eight 4.4, 7.9 and 20.1 (5.8, 8.5, 31.2).  Beyond that runs, whose tokens share their way to the page;
+    // with 4-bit codes from two tokens on (with atomic operations on the shared bytes 64 sequences of five took 11.9 us, by runs 7.8).
+    if (max_count >= 1 && max_count <= (pool.bits == 8 ? kFewTokens<8> : kFewTokens<4>)) {
         const int heads = q.p ? q_heads : 0, per_token = (2 * pool.heads + heads + 3) / 4;
         const long blocks = ((long)seqs.batch * max_count * per_token + 3) / 4;
         if (blocks > 0x3fffffffL) return hipErrorInvalidValue;
