@@ -8,6 +8,7 @@
 //     equal pieces, one per CTA.  A CTA works through the end of one segment, whole ones, and the beginning of another, so a call takes as long as its work
 //     and not as long as its longest sequence; a server's contexts differ by factors of ten.  Beginning a segment costs as much as kSegmentStart quads, which counts as work.  Where
 //     segments are few, pieces are cut so that every segment begins with a CTA, if that lengthens them by less than it saves.
+//   - ALONE: the same with a wave in place of a CTA, for many segments: a wave takes every block of its segment, and nothing waits for another wave.
 //   - A segment that several CTAs share is put together by the one that arrives last, in the order of the pieces, so results do not depend on who that is; above sixteen pieces in
 //     two levels, groups of sixteen first, which keeps the chain of loads short without another launch.
 //   - A block is one run of 32 tokens (8-bit codes) or two (4-bit); every run has its own address, from a page number that is requested three blocks ahead.  A run on a
@@ -20,7 +21,6 @@ namespace tmw4 {
 namespace {
 
 constexpr int kGroupPieces = 16;         // pieces merged at a time
-constexpr int kMergeLoads = 8;           // of them in flight at once
 constexpr int kAgentScope = 16;          // cache-policy bit (sc1) of a store that goes through to memory, and of a load that sees such stores of other XCDs
 constexpr uint32_t kSegmentStart = 2;    // what beginning a segment costs, in quads
 constexpr uint32_t kUnaligned = 4;       // what a CTA pays for not beginning with a segment: most of them have one more to begin, and two to hand on
@@ -101,25 +101,48 @@ struct Columns {
         else
             process_block<BITS, PACK, true>(r, words, qf, scale_log2e, qsum, neg_qbias, mg, blk, len, len_all, lane, st, acc, present);
     }
-    // The four waves that share the columns meet in LDS: wave `wave` gets the unnormalised values o of dimensions 16 * (2 * wave + i / 4) + 4 * (lane / 16) + i % 4 of its lane's column, the
+    // The four waves that share the columns meet in LDS: wave `wave` gets the unnormalised values o[i] of dimensions 16 * (2 * wave + i) + 4 * (lane / 16) ... of its lane's column, the
     // reference M and the denominator L.  (One barrier; another has to follow before the next segment's.)
     struct Join {
         float ml[4][2][16];
         float out[4][8][4][64];
     };
-    __device__ __forceinline__ void join(Join& lds, int wave, int lane, float& M, float& L, float (&o)[8])
+    __device__ __forceinline__ f32x4 values(int i, float corr) const
+    {
+        f32x4 v;
+#pragma unroll
+        for (int rr = 0; rr < 4; ++rr) v[rr] = (BITS == 8 ? acc[i][rr] + st.bias[rr] : acc[i][rr]) - corr;
+        return v;
+    }
+    __device__ __forceinline__ void sums(float& l, float& corr) const
+    {
+        l = xor_add(xor_add(st.l_run, 16), 32), corr = xor_add(xor_add(st.corr, 16), 32);
+        if constexpr (PACK) l = xor_add(l, 8), corr = xor_add(corr, 8);
+    }
+    // A wave that has its columns to itself: o[i] are dimensions 16 * i + 4 * (lane / 16) ...
+    __device__ __forceinline__ void alone(float& M, float& L, f32x4 (&o)[8])
+    {
+        float corr;
+        sums(L, corr);
+        M = st.m_run;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) o[i] = values(i, corr);
+    }
+    __device__ __forceinline__ void join(Join& lds, int wave, int lane, float& M, float& L, f32x4 (&o)[2])
     {
         const int c = lane & 15;
-        float l = xor_add(xor_add(st.l_run, 16), 32), corr = xor_add(xor_add(st.corr, 16), 32);
-        if constexpr (PACK) l = xor_add(l, 8), corr = xor_add(corr, 8);
+        float l, corr;
+        sums(l, corr);
         if (lane < 16) {
             lds.ml[wave][0][c] = st.m_run;
             lds.ml[wave][1][c] = l;
         }
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
+        for (int i = 0; i < 8; ++i) {
+            const f32x4 v = values(i, corr);
 #pragma unroll
-            for (int rr = 0; rr < 4; ++rr) lds.out[wave][i][rr][lane] = (BITS == 8 ? acc[i][rr] + st.bias[rr] : acc[i][rr]) - corr;
+            for (int rr = 0; rr < 4; ++rr) lds.out[wave][i][rr][lane] = v[rr];
+        }
         __syncthreads();
         M = kNegBig;
 #pragma unroll
@@ -133,44 +156,48 @@ struct Columns {
         }
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            o[i] = 0.f;
+            float v = 0.f;
 #pragma unroll
-            for (int w = 0; w < 4; ++w) o[i] += lds.out[w][2 * wave + (i >> 2)][i & 3][lane] * f[w];
+            for (int w = 0; w < 4; ++w) v += lds.out[w][2 * wave + (i >> 2)][i & 3][lane] * f[w];
+            o[i >> 2][i & 3] = v;
         }
     }
 };
 
 // PARTS: pieces of a block that may lie on pages of their own: 2 for 4-bit codes on pages of a single run, else 1.
 // TILES: tiles of columns that a CTA takes at once, four waves each: with two, the waves that share a block ask for it at the same time, and it comes from memory once.  (Tiles one after
-// the other read it twice: 12 x 5 drafted tokens after 6000, 25 columns, 8-bit codes: 45 us, like this XX.)
-template <int BITS, bool PACK, int PARTS, int TILES>
+// the other read it twice: 12 x 5 drafted tokens after 6000, 25 columns, 8-bit codes: 45 us, like this 37.)
+template <int BITS, bool PACK, int PARTS, int TILES, bool ALONE>
 __global__ __launch_bounds__(256 * TILES) __attribute__((amdgpu_waves_per_eu(BITS == 4 && PACK ? 1 : 2, 2))) void paged_columns_kernel(
     PagedPool pool, PagedSeqs seqs, const uint16_t* __restrict__ Q, long q_stride, uint16_t* __restrict__ O, int q_heads, float scale_log2e, int most_rows,
     float* __restrict__ partial, uint32_t* __restrict__ counters)
 {
     constexpr int TOK = 256 / BITS, RUNS = TOK / kRun;       // tokens and runs of a block
-    constexpr uint32_t kLeastQuads = BITS == 8 ? 2 : 1;      // of a piece (1 x 2048 tokens, 8 heads, pieces of 1 / 2 / 3: 8-bit 9.8 / 9.0 / 9.2 us, 4-bit 9.5 / 10.6 / 11.6)
+    constexpr int kStep = ALONE ? 1 : 4;                     // blocks of a quad
+    constexpr int kValues = ALONE ? 8 : 2;                   // vectors of four values that a thread has of the result
+    constexpr uint32_t kLeastQuads = ALONE || BITS == 8 ? 2 : 1;      // of a piece (1 x 2048 tokens, 8 heads, pieces of 1 / 2 / 3: 8-bit 9.8 / 9.0 / 9.2 us, 4-bit 9.5 / 10.6 / 11.6)
     static_assert(PARTS == 1 || (BITS == 4 && PARTS == RUNS), "a part is a run, or the whole block");
     typedef Columns<BITS, PACK> Form;
     constexpr int COLS = Form::kCols * TILES;                // of a segment
+    constexpr int kMergeLoads = ALONE ? 2 : 8;               // pieces in flight at once when they are merged
     constexpr int kPartial = 2 * COLS + 2048 * TILES;        // M and L of every column, eight unnormalised values a thread
     // scale/zero words of the blocks in flight; one array per ring slot so that the compiler can tell which direct-to-LDS load a read depends on
     __shared__ __attribute__((aligned(16))) uint32_t sz_ring0[4 * TILES][2 * TOK];
     __shared__ __attribute__((aligned(16))) uint32_t sz_ring1[4 * TILES][2 * TOK];
     __shared__ __attribute__((aligned(16))) uint32_t sz_ring2[4 * TILES][2 * TOK];
-    __shared__ typename Form::Join s_join[TILES];
+    __shared__ typename std::conditional<ALONE, int, typename Form::Join>::type s_join[TILES];
     __shared__ uint32_t s_last;
     __shared__ u32x2 s_sums[4 * TILES][64];
     __shared__ u32x4 s_seqs[4 * TILES][64];
     const int tid = threadIdx.x, lane = tid & 63;
-    const int any_wave = __builtin_amdgcn_readfirstlane(tid >> 6), wave = any_wave / TILES, part = any_wave % TILES;      // part: the wave's tile
+    const int any_wave = __builtin_amdgcn_readfirstlane(tid >> 6), wave = ALONE ? 0 : any_wave / TILES, part = ALONE ? 0 : any_wave % TILES;      // part: the wave's tile
     const int c = Form::kCols * part + Form::column(lane);   // column of the segment
     const int G = q_heads / pool.heads;
 
     // ---- this CTA's piece of the work
     auto tiles_of = [&](const PagedSeq& s) { return s.count * G <= most_rows ? (s.count * G + COLS - 1) / COLS : 0; };
-    auto quads_of = [&](const PagedSeq& s) { return (max(s.last(seqs.cap), 0) + 4 * TOK - 1) / (4 * TOK); };
-    const uint32_t ctas = gridDim.x;
+    auto quads_of = [&](const PagedSeq& s) { return (max(s.last(seqs.cap), 0) + kStep * TOK - 1) / (kStep * TOK); };
+    const uint32_t ctas = ALONE ? 4 * gridDim.x : gridDim.x, me = ALONE ? 4 * blockIdx.x + any_wave : blockIdx.x;      // CTAs, or waves, that share the work
     // Up to 64 sequences a lane holds one, loaded once: a launch of few short contexts is a chain of memory round trips, and this one is its first.
     const bool one_each = seqs.batch <= 64;
     PagedSeq own{0, 0, 0};
@@ -183,7 +210,7 @@ __global__ __launch_bounds__(256 * TILES) __attribute__((amdgpu_waves_per_eu(BIT
             n = q ? (uint32_t)(tiles_of(own) * pool.heads) : 0u;
         }
         const uint32_t segments = wave_total(n), all = wave_total(n * q);
-        if (segments <= ctas) {
+        if (!ALONE && segments <= ctas) {
             const uint32_t ideal = max((all + ctas - 1) / ctas, kLeastQuads), loose = (all + kSegmentStart * segments) / ctas + kUnaligned;
             uint32_t p = ideal;
             while (p <= loose && wave_total(n * ((q + p - 1) / p)) > ctas) p += 1 + (p >> 4);
@@ -210,7 +237,7 @@ __global__ __launch_bounds__(256 * TILES) __attribute__((amdgpu_waves_per_eu(BIT
         total = finder.total;
     }
     if (!aligned) piece = max((total + ctas - 1) / ctas, kLeastQuads);
-    uint32_t at = blockIdx.x * piece;
+    uint32_t at = me * piece;
     if (at >= total) return;
     const uint32_t end = min(at + piece, total);
     auto ring = [&](int i) { return i == 0 ? sz_ring0[any_wave] : i == 1 ? sz_ring1[any_wave] : sz_ring2[any_wave]; };
@@ -243,8 +270,8 @@ __global__ __launch_bounds__(256 * TILES) __attribute__((amdgpu_waves_per_eu(BIT
         const int len_all = (int)min(max((long)s.pos + last_tok + 1, 0L), (long)seqs.cap);
         Form form;
         form.request_query(Q + (size_t)(s.row + col.tok) * q_stride + ((size_t)hk * G + col.head) * kHeadDim, lane);
-        const int blk1 = min((int)qb * 4, (len_all + TOK - 1) / TOK);
-        int blk = (int)qa * 4 + wave;
+        const int blk1 = min((int)qb * kStep, (len_all + TOK - 1) / TOK);
+        int blk = (int)qa * kStep + wave;
 
         constexpr uint32_t kPart = 4096 / PARTS, kPartTokens = TOK / PARTS;
         // Unchecked, and of the context's last part where the block lies behind it: what is done with a page number waits for it, so that happens a step later.
@@ -288,24 +315,29 @@ __global__ __launch_bounds__(256 * TILES) __attribute__((amdgpu_waves_per_eu(BIT
 
         BlockRegs g[3];
         uint32_t there[3];
-        BlockPages<PARTS> next = pages_of(blk), after = pages_of(blk + 4);
+        BlockPages<PARTS> next = pages_of(blk), after = pages_of(blk + kStep);
         there[0] = load(g[0], ring(0), blk, next);
-        next = pages_of(blk + 8);
-        there[1] = load(g[1], ring(1), blk + 4, after);
+        next = pages_of(blk + 2 * kStep);
+        there[1] = load(g[1], ring(1), blk + kStep, after);
         form.begin(col.real, scale_log2e);
         auto step = [&](int use) {
             const int fill = (use + 2) % 3;
-            there[fill] = load(g[fill], ring(fill), blk + 8, next);
-            next = pages_of(blk + 12);
+            there[fill] = load(g[fill], ring(fill), blk + 2 * kStep, next);
+            next = pages_of(blk + 3 * kStep);
             form.template block<PARTS>(g[use], ring(use), mg, blk, len, len_all, lane, there[use]);
-            blk += 4;
+            blk += kStep;
             return blk < blk1;
         };
         if (blk < blk1)
             while (step(0) && step(1) && step(2)) {
             }
-        float M, L, o[8];                                    // of the thread's column
-        form.join(s_join[part], wave, lane, M, L, o);
+        float M, L;                                          // of the thread's column
+        f32x4 o[kValues];
+        if constexpr (ALONE) form.alone(M, L, o);
+        else form.join(s_join[part], wave, lane, M, L, o);
+        auto sync = [&]() {
+            if constexpr (!ALONE) __syncthreads();
+        };
 
         // What the loop above does not need is worked out again here rather than kept in registers through it.
         int b_again = b, r0_again = r0;
@@ -315,14 +347,14 @@ __global__ __launch_bounds__(256 * TILES) __attribute__((amdgpu_waves_per_eu(BIT
         auto finish = [&](float m_l) {
             const float inv = m_l > 0.f ? 1.0f / m_l : 0.f;
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const float v[4] = {o[4 * i] * inv, o[4 * i + 1] * inv, o[4 * i + 2] * inv, o[4 * i + 3] * inv};
-                if (out.real && Form::owns(lane)) store_out4(O, t.row + out.tok, q_heads, hk * G + out.head, 16 * (2 * wave + i) + 4 * (lane >> 4), v);
+            for (int i = 0; i < kValues; ++i) {
+                const float v[4] = {o[i][0] * inv, o[i][1] * inv, o[i][2] * inv, o[i][3] * inv};
+                if (out.real && Form::owns(lane)) store_out4(O, t.row + out.tok, q_heads, hk * G + out.head, 16 * (kValues * wave + i) + 4 * (lane >> 4), v);
             }
         };
         if (qa == 0 && qb == quads) {                        // (uniform) the whole segment was this CTA's
             finish(L);
-            __syncthreads();
+            sync();
             continue;
         }
 
@@ -330,7 +362,7 @@ __global__ __launch_bounds__(256 * TILES) __attribute__((amdgpu_waves_per_eu(BIT
         const bool column = Form::owns(lane) && c + r0_again < t.count * G;
         // Slots are written through to memory and read past the caches of this XCD, sixteen bytes a lane: M and L of every column, then the threads' values in two rounds of 1 KiB a wave.
         const __amdgpu_buffer_rsrc_t slots = make_rsrc(partial, (uint32_t)kPagedPartialBytes);
-        const int value_at = 2 * COLS * 4 + any_wave * 2048 + lane * 16;
+        const int value_at = 2 * COLS * 4 + (ALONE ? 0 : any_wave * 2048) + lane * 16;
         auto put = [&](uint32_t slot) {
             const int base = (int)(slot * (uint32_t)(kPartial * 4));
             if (!column) return;
@@ -339,14 +371,19 @@ __global__ __launch_bounds__(256 * TILES) __attribute__((amdgpu_waves_per_eu(BIT
                 __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(uint32_t, L), slots, base + (COLS + c) * 4, 0, kAgentScope);
             }
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const f32x4 v = {o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]};
-                __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, v), slots, base + value_at + i * 1024, 0, kAgentScope);
-            }
+            for (int i = 0; i < kValues; ++i) __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, o[i]), slots, base + value_at + i * 1024, 0, kAgentScope);
         };
         // Bumps a counter once all of this CTA's stores have arrived; true in every thread of the CTA that is the last of n, which also resets it.
         auto arrive = [&](uint32_t* counter, uint32_t n) {
             wait_stores_done();
+            if constexpr (ALONE) {
+                uint32_t prev = 0;
+                if (lane == 0) prev = atomicAdd(counter, 1u);
+                prev = (uint32_t)__builtin_amdgcn_readfirstlane((int)prev);
+                if (prev == n - 1u && lane == 0) __hip_atomic_store(counter, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                asm volatile("" ::: "memory");
+                return prev == n - 1u;
+            }
             __syncthreads();
             if (tid == 0) {
                 const uint32_t prev = atomicAdd(counter, 1u);
@@ -362,18 +399,18 @@ __global__ __launch_bounds__(256 * TILES) __attribute__((amdgpu_waves_per_eu(BIT
         auto merge = [&](uint32_t j0, uint32_t stride, uint32_t n) {
             M = kNegBig, L = 0.f;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) o[i] = 0.f;
+            for (int i = 0; i < kValues; ++i) o[i] = f32x4{0.f, 0.f, 0.f, 0.f};
             if (!column) return;
             for (uint32_t j = 0; j < n; j += kMergeLoads) {
                 float ms[kMergeLoads], ls[kMergeLoads];
-                f32x4 v[kMergeLoads][2];
+                f32x4 v[kMergeLoads][kValues];
 #pragma unroll
                 for (int k = 0; k < kMergeLoads; ++k) {
                     const int base = (int)(slot_of(j0 + stride * (j + k < n ? j + k : 0)) * (uint32_t)(kPartial * 4));
                     ms[k] = __builtin_bit_cast(float, (uint32_t)__builtin_amdgcn_raw_buffer_load_b32(slots, base + c * 4, 0, kAgentScope));
                     ls[k] = __builtin_bit_cast(float, (uint32_t)__builtin_amdgcn_raw_buffer_load_b32(slots, base + (COLS + c) * 4, 0, kAgentScope));
 #pragma unroll
-                    for (int i = 0; i < 2; ++i) v[k][i] = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(slots, base + value_at + i * 1024, 0, kAgentScope));
+                    for (int i = 0; i < kValues; ++i) v[k][i] = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(slots, base + value_at + i * 1024, 0, kAgentScope));
                 }
                 float up = M;
 #pragma unroll
@@ -382,13 +419,13 @@ __global__ __launch_bounds__(256 * TILES) __attribute__((amdgpu_waves_per_eu(BIT
                 M = up;
                 L *= old;
 #pragma unroll
-                for (int i = 0; i < 8; ++i) o[i] *= old;
+                for (int i = 0; i < kValues; ++i) o[i] *= old;
 #pragma unroll
                 for (int k = 0; k < kMergeLoads; ++k) {
                     const float f = j + k < n ? exp2f(ms[k] - M) : 0.f;
                     L += ls[k] * f;
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) o[i] += v[k][i >> 2][i & 3] * f;
+                    for (int i = 0; i < kValues; ++i) o[i] += v[k][i] * f;
                 }
             }
         };
@@ -398,12 +435,12 @@ __global__ __launch_bounds__(256 * TILES) __attribute__((amdgpu_waves_per_eu(BIT
         put(slot_of(mine));
         // Counters: of the first group, [CTA in which the segment begins]; of a later one, [CTA of its first piece] - only one segment enters a CTA from before; of the
         // groups of a segment, [CTA in which it begins].
-        if (!arrive(counters + (group == 0 ? k0 : gridDim.x + k0 + group * kGroupPieces), in_group)) continue;
+        if (!arrive(counters + (group == 0 ? k0 : ctas + k0 + group * kGroupPieces), in_group)) continue;
         merge(group * kGroupPieces, 1, in_group);
         if (groups > 1) {
-            __syncthreads();                                 // all of the group has been read before its first slot is written
+            sync();                                          // all of the group has been read before its first slot is written
             put(slot_of(group * kGroupPieces));
-            if (!arrive(counters + 2 * gridDim.x + k0, groups)) continue;
+            if (!arrive(counters + 2 * ctas + k0, groups)) continue;
             merge(0, kGroupPieces, groups);
         }
         finish(L);
@@ -413,19 +450,26 @@ __global__ __launch_bounds__(256 * TILES) __attribute__((amdgpu_waves_per_eu(BIT
 }  // namespace
 
 hipError_t launch_paged_columns(const PagedPool& pool, const PagedSeqs& seqs, const uint16_t* Q, long q_stride, uint16_t* O, int q_heads, float scale, int columns,
-                                int most_rows, int grid, void* workspace, hipStream_t stream)
+                                int most_rows, int grid, bool alone, void* workspace, hipStream_t stream)
 {
-    static_assert(3 * kPagedMostCtas * sizeof(uint32_t) <= kPagedCounterBytes, "three counters a CTA");
+    static_assert(3 * 4 * kPagedMostCtas * sizeof(uint32_t) <= kPagedCounterBytes, "three counters a wave");
     static_assert(2 * kPagedMostCtas * (2 * 32 + 2 * 2048) * sizeof(float) <= kPagedPartialBytes, "two slots a CTA");
-    if (grid < 1 || grid > kPagedMostCtas) return hipErrorInvalidValue;
+    static_assert(2 * 4 * kPagedMostCtas * (2 * 16 + 2048) * sizeof(float) <= kPagedPartialBytes, "two slots a wave");
+    if (grid < 1 || grid > kPagedMostCtas || (alone && columns == 32)) return hipErrorInvalidValue;
     uint32_t* const counters = (uint32_t*)workspace;
     float* const partial = (float*)((char*)workspace + kPagedCounterBytes);
     const float s = scale * 1.4426950408889634f;
-    const bool halves = pool.run_log == 0;
-    auto pick = [&](auto c8, auto c16, auto c32) { return columns == 8 ? c8 : columns == 16 ? c16 : c32; };
-    const auto kernel = pool.bits == 8 ? pick(paged_columns_kernel<8, true, 1, 1>, paged_columns_kernel<8, false, 1, 1>, paged_columns_kernel<8, false, 1, 2>)
-                        : halves       ? pick(paged_columns_kernel<4, true, 2, 1>, paged_columns_kernel<4, false, 2, 1>, paged_columns_kernel<4, false, 2, 2>)
-                                       : pick(paged_columns_kernel<4, true, 1, 1>, paged_columns_kernel<4, false, 1, 1>, paged_columns_kernel<4, false, 1, 2>);
+    auto pick = [&](auto bits, auto parts) {
+        constexpr int BITS = decltype(bits)::value, PARTS = decltype(parts)::value;
+        if (alone) return columns == 8 ? paged_columns_kernel<BITS, true, PARTS, 1, true> : paged_columns_kernel<BITS, false, PARTS, 1, true>;
+        return columns == 8    ? paged_columns_kernel<BITS, true, PARTS, 1, false>
+               : columns == 16 ? paged_columns_kernel<BITS, false, PARTS, 1, false>
+                               : paged_columns_kernel<BITS, false, PARTS, 2, false>;
+    };
+    typedef std::integral_constant<int, 1> One;
+    typedef std::integral_constant<int, 2> Two;
+    const auto kernel = pool.bits == 8 ? pick(std::integral_constant<int, 8>{}, One{})
+                        : pool.run_log == 0 ? pick(std::integral_constant<int, 4>{}, Two{}) : pick(std::integral_constant<int, 4>{}, One{});
     hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(columns == 32 ? 512 : 256), 0, stream, pool, seqs, Q, q_stride, O, q_heads, s, most_rows, partial, counters);
     return hipGetLastError();
 }

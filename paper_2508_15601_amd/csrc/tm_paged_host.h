@@ -6,7 +6,7 @@
 namespace tmw4 {
 
 // Workspace of tm_paged_attn: arrival counters, then partial results of contexts that are cut into pieces.
-constexpr size_t kPagedCounterBytes = 16 * 1024;
+constexpr size_t kPagedCounterBytes = 32 * 1024;
 constexpr size_t kPagedPartialBytes = 66u << 20;          // 520 pieces of 256 rows
 constexpr size_t kPagedWorkspaceBytes = kPagedCounterBytes + kPagedPartialBytes;
 
@@ -23,14 +23,15 @@ hipError_t launch_rope(const uint16_t* X, long x_stride, const int32_t* position
 hipError_t launch_paged_append(const PagedPool& pool, const PagedSeqs& seqs, PagedRows k, PagedRows v, const RopePlan* rope, PagedRows q, uint16_t* q_out,
                                long q_out_stride, int q_heads, int max_count, hipStream_t stream);
 hipError_t launch_paged_read(const PagedPool& pool, const PagedSeqs& seqs, uint16_t* K, uint16_t* V, hipStream_t stream);
-// The new tokens of sequences with up to most_rows (token, query head of a KV head) rows; `columns` of them at a time, 8, 16 or 32.  Every CTA of `grid` takes an equal
-// piece of the work.
+// The new tokens of sequences with up to most_rows (token, query head of a KV head) rows; `columns` of them at a time, 8, 16 or 32.  Every CTA of `grid`, or every wave (alone; not
+// with 32 columns), takes an equal piece of the work.
 hipError_t launch_paged_columns(const PagedPool& pool, const PagedSeqs& seqs, const uint16_t* Q, long q_stride, uint16_t* O, int q_heads, float scale, int columns,
-                                int most_rows, int grid, void* workspace, hipStream_t stream);
+                                int most_rows, int grid, bool alone, void* workspace, hipStream_t stream);
 
 // How a call is divided: sequences with at least least_rows rows in CTAs of 32 * row_waves rows (row_waves = 0: none), the others by columns (column_rows = 0: none).
 struct PagedForm {
     int columns, column_rows, column_ctas;
+    bool alone;
     int least_rows, row_waves, pieces, target;
     uint32_t items;
 };

@@ -261,6 +261,12 @@ hipError_t paged_rows_setup()
 
 // Up to 64 rows (tokens times query heads of a KV head) a sequence, everything goes by columns: 12 sequences of 5 tokens and 32 / 8 heads 37 us, by rows 40; with 128 rows and one
 // sequence of 8000 tokens it is 38 us against 31.  With more, a sequence of up to 16 rows still does: those of a mixed call are decoding.
+// By columns, a CTA to a segment (a sequence's column tile and KV head) at a time, or each of its waves to one of its own, which saves their meeting and lets one wave's start hide
+// behind the others' work, but leaves more pieces to merge.  Waves win where segments are many: 8 KV heads, 4-bit, 256 sequences of 300 / 1000 tokens 23.5 / 51 us (a CTA each 52 /
+// 77), 64 skewed ones up to 16384 52 (64), 64 of 5 drafted tokens after 500 16 (21), 33 of 300 10.5 (14.4); with a segment per compute unit or less they lose: 32 of 8192 54 (47).
+// 8-bit codes take the memory's time sooner: 256 of 300 / 1000 31 / 86 (48 / 98), 128 of 1000 43 (50), but 64 of 1000 26.9 (25.0), 256 skewed ones up to 9000 212 (200), 64 skewed 97 (87),
+// 256 x 5 after 1000, whose segments need two column tiles, 183 (152): from four segments a compute unit on.  Below that two CTAs a compute unit hide each other's starts if contexts are
+// short: 48 of 300 10.2 us (13.0 with one), 64 of 500 14.2 (15.3), 64 of 2000 42.8 (45), but 40 of 2000 to 4000 50 (45).
 // 128 or 256 rows a CTA: a stage of 128 costs 0.66 of one of 256 (the four prompts above: 1154 against 867 us).  So 256, unless the chip does not fill with either and pieces cannot
 // make up for it, a context being short (two prompts of 307 and 161 tokens, 2 / 1 heads: 19 against 20 us; 400 and 150, 16 / 1: 34 against 39).  Over 57 random calls (one chunk after
 // up to 40000 tokens, up to six prompts, up to 30 decoding sequences with chunks; 1 to 8 KV heads, 1 to 16 query heads each) the rule's choice takes 1.02 of the better one's time,
@@ -273,7 +279,11 @@ PagedForm paged_form(const PagedPool& pool, const PagedSeqs& seqs, int q_heads, 
     const long most = (long)(max_count > 0 && max_count < seqs.tokens ? max_count : seqs.tokens) * G;
     f.columns = most > 64 ? G <= 8 ? 8 : 16 : most <= 8 ? 8 : most <= 16 ? 16 : 32;
     f.column_rows = most <= 64 ? 64 : seqs.batch > 1 ? 16 : 0;
-    f.column_ctas = num_cu < kPagedMostCtas ? num_cu : kPagedMostCtas;
+    const long segments = (long)seqs.batch * pool.heads * (most <= 64 ? (most + f.columns - 1) / f.columns : 1);
+    f.alone = pool.bits == 4 ? segments > num_cu : f.columns < 32 && segments >= 4L * num_cu;
+    if (f.alone && f.columns == 32) f.columns = 16;
+    const bool twice = pool.bits == 8 && !f.alone && f.columns < 32 && segments > num_cu && max_len > 0 && max_len <= 1024;
+    f.column_ctas = std::min(twice ? 2 * num_cu : num_cu, kPagedMostCtas);
     if (most <= 64) {
         f.column_rows = 1 << 30;                             // whatever the offsets say
         return f;
@@ -315,7 +325,7 @@ hipError_t launch_paged_attn(const PagedPool& pool, const PagedSeqs& seqs, const
                                  : launch<4, 4>(pool, seqs, Q, q_stride, O, q_heads, scale, plan, f.items, partial, stream);
     }
     if (e == hipSuccess && f.column_rows)
-        e = launch_paged_columns(pool, seqs, Q, q_stride, O, q_heads, scale, f.columns, f.column_rows, f.column_ctas, workspace, stream);
+        e = launch_paged_columns(pool, seqs, Q, q_stride, O, q_heads, scale, f.columns, f.column_rows, f.column_ctas, f.alone, workspace, stream);
     return e;
 }
 

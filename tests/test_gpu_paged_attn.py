@@ -140,6 +140,51 @@ def test_contexts_of_very_different_lengths(tm, bits, batch):
     Setup(tm, bits, 32, 1 if batch > 64 else 2, counts.tolist(), positions.tolist(), q_heads=4, max_count=1, max_len=5001, seed=batch).check((8, True, 0, 0))
 
 
+def _lengths(batch, longest, seed):
+    rng = np.random.default_rng(seed)
+    lengths = (40 + 200 * rng.random(batch)).astype(int)
+    lengths[batch // 3] = longest
+    return lengths.tolist()
+
+
+@pytest.mark.parametrize("page, heads, q_heads, batch, longest, count, columns", [
+    (32, 8, 32, 40, 700, 1, 8),                                            # a few segments more than compute units: pieces of a segment
+    (64, 8, 8, 40, 3600, 1, 8),                                            # one sequence in more than sixteen pieces
+    (64, 4, 48, 70, 300, 1, 16),                                           # more sequences than lanes
+    (128, 8, 40, 34, 500, 5, 16),                                          # more columns than a tile
+    (32, 2, 6, 131, 400, 2, 8),
+])
+def test_many_segments_4bit(tm, page, heads, q_heads, batch, longest, count, columns):
+    """More segments than compute units: every wave works by itself."""
+    counts = [count] * batch
+    counts[1] = 0
+    Setup(tm, 4, page, heads, counts, _lengths(batch, longest, page), q_heads=q_heads, before=1, behind=1, max_count=count, seed=batch).check((columns, True, 0, 0))
+
+
+@pytest.mark.parametrize("page, heads, q_heads, batch, longest, count, max_len, columns", [
+    (64, 16, 32, 64, 1500, 1, 1501, 8),
+    (32, 16, 160, 66, 300, 1, 0, 16),
+    (64, 16, 32, 64, 200, 3, 0, 8),
+    (64, 8, 32, 33, 500, 1, 501, 8),                                       # short contexts: two CTAs a compute unit
+    (32, 4, 40, 90, 700, 1, 701, 16),
+])
+def test_many_segments_8bit(tm, page, heads, q_heads, batch, longest, count, max_len, columns):
+    counts = [count] * batch
+    counts[1] = 0
+    Setup(tm, 8, page, heads, counts, _lengths(batch, longest, page), q_heads=q_heads, before=1, behind=1, max_count=count, max_len=max_len, seed=batch).check((columns, True, 0, 0))
+
+
+@pytest.mark.parametrize("bits", [8, 4])
+def test_many_segments_and_bad_pages(tm, bits):
+    """Sequences of missing pages only, first, in the middle and last, and with lengths of none: every wave by itself."""
+    batch = 130 if bits == 8 else 40
+    lengths = _lengths(batch, 333, 5)
+    bad = [(3, c, -1) for c in range(11)] + [(5, 0, 1 << 30), (7, 1, -2), (9, lengths[9] // 32, -5)]
+    positions = list(lengths)
+    positions[11], positions[12] = -1, -4
+    Setup(tm, bits, 32, 8, [1] * batch, positions, q_heads=16, max_count=1, seed=3, bad=bad).check((8, True, 0, 0))
+
+
 MANY = [
     # page, KV heads, query heads, counts, positions
     (64, 1, 4, [65], [0]),                                                 # a whole prompt
