@@ -13,6 +13,11 @@
 //     two levels, groups of sixteen first, which keeps the chain of loads short without another launch.
 //   - A block is one run of 32 tokens (8-bit codes) or two (4-bit); every run has its own address, from a page number that is requested three blocks ahead.  A run on a
 //     page that the pool does not have is not read and its tokens are masked.
+//
+// Measured (32 / 8 heads unless said): 32 sequences of 8192 tokens, 8-bit 84 us (6.5 TB/s), 4-bit 52 us (5.4 TB/s); 4 of 60000 down to 30000, 64 / 8 heads, 8-bit 63 us (6.0 TB/s); 64
+// skewed ones up to 16384, 4-bit 57 us (5.2 TB/s); one of 2048, 8-bit 8.9 us; 12 x 5 drafted tokens after 3000 to 6000, 40 / 8 heads, 8-bit 36 us (3.3 TB/s).  Long contexts are bound by
+// memory (a large copy reaches 5.2 TB/s, both ways together); short ones by a launch, a plan, a chain of three round trips to memory (lengths, page numbers, blocks) and the
+// meeting of the pieces, 8 us together; tiles of 32 columns by instruction issue, the codes being converted for each half.
 #include "tm_attn_device.h"
 #include "tm_paged_host.h"
 
@@ -166,7 +171,8 @@ struct Columns {
 
 // PARTS: pieces of a block that may lie on pages of their own: 2 for 4-bit codes on pages of a single run, else 1.
 // TILES: tiles of columns that a CTA takes at once, four waves each: with two, the waves that share a block ask for it at the same time, and it comes from memory once.  (Tiles one after
-// the other read it twice: 12 x 5 drafted tokens after 6000, 25 columns, 8-bit codes: 45 us, like this 37.)
+// the other read it twice: 12 x 5 drafted tokens after 6000, 25 columns, 8-bit codes: 45 us, like this 36.  The codes are then not loaded as data that nobody else wants, which
+// cost the second wave a quarter of its hits: 32 x 5 after 8000 120 us, so 104.)
 template <int BITS, bool PACK, int PARTS, int TILES, bool ALONE>
 __global__ __launch_bounds__(256 * TILES) __attribute__((amdgpu_waves_per_eu(BITS == 4 && PACK ? 1 : 2, 2))) void paged_columns_kernel(
     PagedPool pool, PagedSeqs seqs, const uint16_t* __restrict__ Q, long q_stride, uint16_t* __restrict__ O, int q_heads, float scale_log2e, int most_rows,
@@ -305,10 +311,10 @@ __global__ __launch_bounds__(256 * TILES) __attribute__((amdgpu_waves_per_eu(BIT
 #pragma unroll
                 for (int i = 0; i < 4 / PARTS; ++i) {
                     const int at = 4 / PARTS * n + i;
-                    r.k[at >> 1][at & 1] = __builtin_amdgcn_raw_buffer_load_b128(rk, off + i * 1024, 0, kNonTemporal);
+                    r.k[at >> 1][at & 1] = __builtin_amdgcn_raw_buffer_load_b128(rk, off + i * 1024, 0, TILES > 1 ? 0 : kNonTemporal);
                 }
 #pragma unroll
-                for (int i = 0; i < 4 / PARTS; ++i) r.v[4 / PARTS * n + i] = __builtin_amdgcn_raw_buffer_load_b128(rv, off + i * 1024, 0, kNonTemporal);
+                for (int i = 0; i < 4 / PARTS; ++i) r.v[4 / PARTS * n + i] = __builtin_amdgcn_raw_buffer_load_b128(rv, off + i * 1024, 0, TILES > 1 ? 0 : kNonTemporal);
             }
             return present;
         };
