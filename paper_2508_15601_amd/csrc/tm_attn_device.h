@@ -31,115 +31,6 @@ __device__ __forceinline__ f16x8 add_pairs(f16x8 v, f16x2 a, f16x2 b, f16x2 c, f
 __device__ __forceinline__ float xor_max(float v, int mask) { return fmaxf(v, __shfl_xor(v, mask)); }
 __device__ __forceinline__ float xor_add(float v, int mask) { return v + __shfl_xor(v, mask); }
 
-// ------------------------------------------------------------------------------------------------ quantise + store
-// Minimum and maximum over every row of sixteen lanes, in each of its lanes.
-__device__ __forceinline__ void row_min_max(float& mn, float& mx)
-{
-    auto fold = [&](auto CTRL) {
-        constexpr int ctrl = decltype(CTRL)::value;        // row_ror by 8, 4, 2, 1
-        const float a = __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, mn), ctrl, 0xf, 0xf, true));
-        const float b = __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, mx), ctrl, 0xf, 0xf, true));
-        mn = fminf(mn, a);
-        mx = fmaxf(mx, b);
-    };
-    fold(std::integral_constant<int, 0x128>{});
-    fold(std::integral_constant<int, 0x124>{});
-    fold(std::integral_constant<int, 0x122>{});
-    fold(std::integral_constant<int, 0x121>{});
-}
-
-// The same over the wave: rows first, then swaps between rows.
-__device__ __forceinline__ void wave_min_max(float& mn, float& mx)
-{
-    row_min_max(mn, mx);
-#if defined(__HIP_DEVICE_COMPILE__)
-    auto pair = [](auto r, auto f) { return f(__builtin_bit_cast(float, (uint32_t)r[0]), __builtin_bit_cast(float, (uint32_t)r[1])); };
-    auto lo = [](float x, float y) { return fminf(x, y); };
-    auto hi = [](float x, float y) { return fmaxf(x, y); };
-    uint32_t a = __builtin_bit_cast(uint32_t, mn), b = __builtin_bit_cast(uint32_t, mx);
-    mn = pair(__builtin_amdgcn_permlane16_swap(a, a, false, false), lo);
-    mx = pair(__builtin_amdgcn_permlane16_swap(b, b, false, false), hi);
-    a = __builtin_bit_cast(uint32_t, mn), b = __builtin_bit_cast(uint32_t, mx);
-    mn = pair(__builtin_amdgcn_permlane32_swap(a, a, false, false), lo);
-    mx = pair(__builtin_amdgcn_permlane32_swap(b, b, false, false), hi);
-#endif
-}
-
-// a / b rounded to nearest, exactly as the division gives it, from the correctly rounded reciprocal of b: a product and one
-// correction (Markstein), three instructions where a division is ten.  The tests check it against the division for every mantissa of an
-// fp16 value over every one of an fp16 scale, and for every fp32 mantissa over 15 and 255.
-__device__ __forceinline__ float quotient(float a, float b, float inv)
-{
-    const float q = a * inv;
-    return __builtin_fmaf(__builtin_fmaf(-q, b, a), inv, q);
-}
-
-// Scale and zero-point of a vector from its extremes, and the codes of its values: scale = range / levels rounded to fp16 (1 where
-// that is zero or not finite), code = round(x / scale) + zero-point, within the levels.
-template <int BITS>
-struct Quantiser {
-    static constexpr float top = BITS == 8 ? 255.0f : 15.0f;
-    _Float16 s16;
-    float s, inv, zero;
-    bool odd;                              // the scale was replaced by 1 (only then can a value be infinite)
-
-    __device__ __forceinline__ Quantiser(float mn, float mx)
-    {
-        s16 = (_Float16)quotient(mx - mn, top, 1.0f / top);
-        s = (float)s16;
-        odd = !(s > 0.0f) || __builtin_isinf(s);
-        if (odd) {
-            s = 1.0f;
-            s16 = (_Float16)1.0f;
-        }
-        const float r = __builtin_amdgcn_rcpf(s);            // within an ulp; one step makes it the nearest number
-        inv = __builtin_fmaf(__builtin_fmaf(-s, r, 1.0f), r, r);
-        zero = fminf(fmaxf(rintf(over_scale(-mn)), 0.0f), top);
-    }
-    __device__ __forceinline__ float over_scale(float x) const { return odd ? x : quotient(x, s, inv); }
-    __device__ __forceinline__ uint32_t code(float x) const { return (uint32_t)fminf(fmaxf(rintf(over_scale(x)) + zero, 0.0f), top); }
-    __device__ __forceinline__ uint32_t pair() const
-    {
-        return (uint32_t)__builtin_bit_cast(unsigned short, s16) | ((uint32_t)__builtin_bit_cast(unsigned short, (_Float16)zero) << 16);
-    }
-};
-
-// The codes of the lane's two values and the vector's scale / zero word.
-template <int BITS>
-__device__ __forceinline__ uint32_t quantise_pair(float x0, float x1, uint32_t& q0, uint32_t& q1)
-{
-    float mn = fminf(x0, x1), mx = fmaxf(x0, x1);
-    wave_min_max(mn, mx);
-    const Quantiser<BITS> z(mn, mx);
-    q0 = z.code(x0);
-    q1 = z.code(x1);
-    return z.pair();
-}
-
-// The codes of the lane's eight values and the vector's scale / zero word.
-template <int BITS>
-__device__ __forceinline__ uint32_t quantise_row8(const u32x4& raw, uint32_t (&q)[8])
-{
-    float x[8];
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-        const f16x2 two = as_f16x2(raw[k]);
-        x[2 * k] = (float)two.x;
-        x[2 * k + 1] = (float)two.y;
-    }
-    float mn = x[0], mx = x[0];
-#pragma unroll
-    for (int k = 1; k < 8; ++k) {
-        mn = fminf(mn, x[k]);
-        mx = fmaxf(mx, x[k]);
-    }
-    row_min_max(mn, mx);
-    const Quantiser<BITS> z(mn, mx);
-#pragma unroll
-    for (int k = 0; k < 8; ++k) q[k] = z.code(x[k]);
-    return z.pair();
-}
-
 // ------------------------------------------------------------------------------------------------ decode attention
 // The codes of a block travel in registers (they are the in-flight memory of the pipeline: two blocks ahead).  The 64
 // scale/zero words of a block would cost as many registers per lane as its 8 KiB of codes, so they go through LDS

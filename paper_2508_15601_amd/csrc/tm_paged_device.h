@@ -135,4 +135,37 @@ __device__ __forceinline__ size_t paged_run(const PagedPool& p, int page, int he
     return (((size_t)page * p.heads + head) << p.run_log) + (run & ((1 << p.run_log) - 1));
 }
 
+// Runs of the cache in which a sequence has new tokens.
+__device__ __forceinline__ uint32_t touched_runs(const PagedSeqs& s, const PagedSeq& q)
+{
+    const int f = q.first(), l = q.last(s.cap);
+    return l > f ? (uint32_t)((l - 1) / kRun - f / kRun + 1) : 0u;
+}
+
+// A CTA's run: tokens u0 .. u1 - 1 of run `run` of sequence b are new.
+struct RunJob {
+    int b, run, u0, u1, page;
+    long row;                            // packed row of the run's slot 0 (may lie before the first)
+    bool live;
+};
+__device__ __forceinline__ RunJob run_job(const PagedPool& pool, const PagedSeqs& s, uint32_t item, int lane)
+{
+    RunJob j{};
+    const SeqFinder finder([&](int b) { return touched_runs(s, paged_seq(s, b)); }, s.batch, lane);
+    if (item >= finder.total) return j;
+    uint32_t base;
+    j.b = finder.find(item, base);
+    const PagedSeq q = paged_seq(s, j.b);
+    const int f = q.first(), l = q.last(s.cap);
+    if (item - base >= touched_runs(s, q)) return j;
+    j.run = f / kRun + (int)(item - base);
+    const int t = j.run * kRun;
+    j.u0 = max(f - t, 0);
+    j.u1 = min(l - t, kRun);
+    j.row = (long)q.row + ((long)t - q.pos);
+    j.page = paged_page(pool, s, j.b, j.run);
+    j.live = true;
+    return j;
+}
+
 }  // namespace tmw4

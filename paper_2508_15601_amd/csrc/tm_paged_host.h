@@ -17,6 +17,13 @@ struct PagedRows {                       // a packed array of new tokens: row r 
     long stride;
 };
 
+// Most runs that the sequences' new tokens can touch.
+inline long most_runs(const PagedSeqs& s)
+{
+    const long spread = s.tokens / kRun + 2L * s.batch;
+    return spread < s.tokens ? spread : s.tokens;
+}
+
 hipError_t launch_rope(const uint16_t* X, long x_stride, const int32_t* positions, const RopePlan& r, uint16_t* Y, long y_stride, int tokens, int heads,
                        int dim, hipStream_t stream);
 // q.p == nullptr: keys and values only; rope == nullptr: stored as they are

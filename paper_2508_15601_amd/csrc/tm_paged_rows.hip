@@ -82,10 +82,9 @@ __device__ __forceinline__ int piece_stages(const RowsWork<RW>& w, int heads, co
     float work = w.template sum<float>(w.seqs.batch, [](const RowsShape& r) { return r.work; });
 #pragma unroll
     for (int m = 1; m < 64; m <<= 1) work += __shfl_xor(work, m);
-    const float tiles = (float)wave_total(w.template sum<uint32_t>(w.seqs.batch, [](const RowsShape& r) { return r.tiles; })) * (float)heads;
     const float target = (float)plan.target, mean = fminf(work * (float)heads / target, (float)kWhole);
     int best = max((int)mean + 1, kLeastStages);
-    if (w.per == 1 && tiles < 2.f * target) {
+    if (w.per == 1 && (float)wave_total(w.own.tiles) * (float)heads < 2.f * target) {
         const float tried = lane == 63 ? (float)kWhole : fmaxf(floorf(mean * 0.5f * __builtin_amdgcn_exp2f((float)lane * 0.0625f)), (float)kLeastStages), inv = 1.0f / tried;
         float n = 0.f, cut = 0.f, longest = 0.f;
         for (uint64_t left = __builtin_amdgcn_ballot_w64(w.own.tiles != 0u); left; left &= left - 1) {
@@ -280,7 +279,8 @@ PagedForm paged_form(const PagedPool& pool, const PagedSeqs& seqs, int q_heads, 
     f.columns = most > 64 ? G <= 8 ? 8 : 16 : most <= 8 ? 8 : most <= 16 ? 16 : 32;
     f.column_rows = most <= 64 ? 64 : seqs.batch > 1 ? 16 : 0;
     const long segments = (long)seqs.batch * pool.heads * (most <= 64 ? (most + f.columns - 1) / f.columns : 1);
-    f.alone = pool.bits == 4 ? segments > num_cu : f.columns < 32 && segments >= 4L * num_cu;
+    const double most_units = ((double)seqs.tokens * G / 8 + seqs.batch) * pool.heads * (seqs.cap / 32 + 3);      // blocks and starts, were every context as long as the table
+    f.alone = (pool.bits == 4 ? segments > num_cu : f.columns < 32 && segments >= 4L * num_cu) && most_units < 2147483648.0;      // (counted in 32 bits)
     if (f.alone && f.columns == 32) f.columns = 16;
     const bool twice = pool.bits == 8 && !f.alone && f.columns < 32 && segments > num_cu && max_len > 0 && max_len <= 1024;
     f.column_ctas = std::min(twice ? 2 * num_cu : num_cu, kPagedMostCtas);

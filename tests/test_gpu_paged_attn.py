@@ -185,6 +185,17 @@ def test_many_segments_and_bad_pages(tm, bits):
     Setup(tm, bits, 32, 8, [1] * batch, positions, q_heads=16, max_count=1, seed=3, bad=bad).check((8, True, 0, 0))
 
 
+def test_work_of_a_wide_table_is_counted_in_32_bits(tm):
+    """Every wave by itself counts its work in blocks, four to a CTA's unit: not where a table is so wide that the count might not fit."""
+    import torch
+    k, v, pairs = tm.tm_paged_pool(2, 8, 64, 4)
+    cache = tm.tm_paged_create(k, v, pairs)
+    offsets, positions = torch.arange(0, 175, 5, dtype=torch.int32, device="cuda"), torch.zeros(34, dtype=torch.int32, device="cuda")
+    for cols, columns in ((1 << 20, 16), (1 << 21, 32)):
+        table = torch.zeros(34, cols, dtype=torch.int32, device="cuda")
+        assert tm.tm_get_paged_plan(cache, tm.PagedBatch(table, offsets, positions, max_count=5), 170, 32)[0] == columns
+
+
 MANY = [
     # page, KV heads, query heads, counts, positions
     (64, 1, 4, [65], [0]),                                                 # a whole prompt
