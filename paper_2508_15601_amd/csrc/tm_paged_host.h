@@ -7,8 +7,9 @@ namespace tmw4 {
 
 // Workspace of tm_paged_attn: arrival counters, then partial results of contexts that are cut into pieces.
 constexpr size_t kPagedCounterBytes = 32 * 1024;
-constexpr size_t kPagedPartialBytes = 66u << 20;          // 520 pieces of 256 rows
-constexpr size_t kPagedWorkspaceBytes = kPagedCounterBytes + kPagedPartialBytes;
+constexpr size_t kPagedColumnBytes = 34u << 20;           // two pieces each of 2048 waves
+constexpr size_t kPagedRowBytes = 66u << 20;              // 520 pieces of 256 rows
+constexpr size_t kPagedWorkspaceBytes = kPagedCounterBytes + kPagedColumnBytes + kPagedRowBytes;
 
 constexpr int kPagedMostCtas = 512;      // of a launch whose CTAs share contexts
 
@@ -38,7 +39,7 @@ hipError_t launch_paged_columns(const PagedPool& pool, const PagedSeqs& seqs, co
 // How a call is divided: sequences with at least least_rows rows in CTAs of 32 * row_waves rows (row_waves = 0: none), the others by columns (column_rows = 0: none).
 struct PagedForm {
     int columns, column_rows, column_ctas;
-    bool alone;
+    bool alone, together;                // columns: every wave by itself; in one launch with the rows
     int least_rows, row_waves, pieces, target;
     uint32_t items;
 };

@@ -11,6 +11,7 @@
 // Measured (32 / 8 heads): prompts of 6000, 5000, 4000 and 3000 tokens, 8-bit: 862 us (0.82 PFLOP/s); 512 tokens after 30000, 4-bit: 313 us (0.81 PFLOP/s), 1024 without pieces; 100
 // after 8000, 8-bit: 45 us, 259 without pieces.  What bounds it is the issue of vector and matrix instructions (tm_attn_prefill.hip); a piece of 256 rows leaves 133 KB in memory.
 #include "tm_attn_rows_impl.h"
+#include "tm_paged_columns_impl.h"
 #include "tm_paged_host.h"
 
 #include <algorithm>
@@ -157,15 +158,13 @@ __device__ __forceinline__ bool rows_tile(RowsTile& t, const PagedSeqs& seqs, in
 }
 
 template <int BITS, int RW>
-__global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) void paged_rows_kernel(PagedPool pool, PagedSeqs seqs, const uint16_t* __restrict__ Q, long q_stride,
-                                                                                                    uint16_t* __restrict__ O, int q_heads, float scale_log2e, RowsPlan plan,
-                                                                                                    float* __restrict__ partial)
+__device__ __forceinline__ void paged_rows(const PagedPool& pool, const PagedSeqs& seqs, const uint16_t* __restrict__ Q, long q_stride, uint16_t* __restrict__ O, int q_heads,
+                                           float scale_log2e, const RowsPlan& plan, float* __restrict__ partial, uint32_t block, unsigned char* smem)
 {
-    extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
-    const uint32_t heads = (uint32_t)pool.heads, hk = blockIdx.x % heads;
+    const uint32_t heads = (uint32_t)pool.heads, hk = block % heads;
     const int G = q_heads / pool.heads;
     RowsTile t;
-    if (!rows_tile<RW, false>(t, seqs, G, pool.heads, plan, blockIdx.x / heads, threadIdx.x & 63)) return;            // (uniform)
+    if (!rows_tile<RW, false>(t, seqs, G, pool.heads, plan, block / heads, threadIdx.x & 63)) return;            // (uniform)
     const int first = t.piece * t.piece_stages;
     const int stages = t.piece == t.pieces - 1 ? t.stages - first : t.piece_stages;
     float* const part = t.pieces > 1 ? partial + ((size_t)(t.slot + t.piece) * heads + hk) * kPieceFloats<RW> : nullptr;
@@ -173,6 +172,35 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
     const long o_stride = (long)q_heads * kHeadDim;
     const RowsJob job{Q + t.s.row * q_stride + at, q_stride, O + t.s.row * o_stride + at, o_stride, t.s.count, G, t.row0, seqs.cap, t.s.pos, first, stages, part};
     attn_rows<BITS, RW, true>(job, pool.k, pool.v, pool.pairs, PagedWhere{pool, seqs, t.b, (int)hk}, t.len, scale_log2e, smem);
+}
+
+template <int BITS, int RW>
+__global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) void paged_rows_kernel(PagedPool pool, PagedSeqs seqs, const uint16_t* __restrict__ Q, long q_stride,
+                                                                                                    uint16_t* __restrict__ O, int q_heads, float scale_log2e, RowsPlan plan,
+                                                                                                    float* __restrict__ partial)
+{
+    extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
+    paged_rows<BITS, RW>(pool, seqs, Q, q_stride, O, q_heads, scale_log2e, plan, partial, blockIdx.x, smem);
+}
+
+// Sequences of few rows in the same launch, every wave by itself (tm_paged_columns_impl.h): its first `ctas` CTAs.  They wait for memory where the rows multiply; in a launch of their
+// own they would begin when the last row is done.
+struct ColumnsPart {
+    int most_rows;
+    uint32_t ctas;
+    float* partial;
+    uint32_t* counters;
+};
+template <int BITS, int RW, bool PACK, int PARTS>
+__global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) void paged_mixed_kernel(PagedPool pool, PagedSeqs seqs, const uint16_t* __restrict__ Q, long q_stride,
+                                                                                                     uint16_t* __restrict__ O, int q_heads, float scale_log2e, RowsPlan plan,
+                                                                                                     float* __restrict__ partial, ColumnsPart few)
+{
+    extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
+    if (blockIdx.x < few.ctas)
+        paged_columns<BITS, PACK, PARTS, 1, true, 8>(pool, seqs, Q, q_stride, O, q_heads, scale_log2e, few.most_rows, few.partial, few.counters, blockIdx.x, few.ctas);
+    else
+        paged_rows<BITS, RW>(pool, seqs, Q, q_stride, O, q_heads, scale_log2e, plan, partial, blockIdx.x - few.ctas, smem);
 }
 
 // Puts the pieces of rows together: a CTA of 256 threads takes kMergeRows rows, eight at a time, a thread four dimensions of one; kLoads pieces in flight at once.
@@ -227,24 +255,52 @@ __global__ __launch_bounds__(256) void paged_rows_merge_kernel(int heads, PagedS
     }
 }
 
-template <int BITS, int RW>
-hipError_t launch(const PagedPool& pool, const PagedSeqs& seqs, const uint16_t* Q, long q_stride, uint16_t* O, int q_heads, float scale, const RowsPlan& plan, uint32_t items,
-                  float* partial, hipStream_t stream)
+template <int BITS, int RW, bool PACK, int PARTS>
+hipError_t allow_lds_mixed()
 {
-    const unsigned long tiles = (unsigned long)items * pool.heads, ctas = tiles + (plan.target ? plan.slots : 0), cut = std::min(tiles, (unsigned long)plan.slots / 2);
-    if (ctas < 1 || ctas > 0x7fffffffUL) return hipErrorInvalidValue;
-    hipLaunchKernelGGL((paged_rows_kernel<BITS, RW>), dim3((unsigned)ctas), dim3(512), kLdsBytes, stream, pool, seqs, Q, q_stride, O, q_heads, scale * 1.4426950408889634f, plan,
-                       partial);
-    hipError_t e = hipGetLastError();
-    if (e != hipSuccess || plan.target == 0) return e;
-    hipLaunchKernelGGL((paged_rows_merge_kernel<RW>), dim3((unsigned)(cut * (32 * RW / kMergeRows))), dim3(256), 0, stream, pool.heads, seqs, O, q_heads, plan, partial);
-    return hipGetLastError();
+    return hipFuncSetAttribute(reinterpret_cast<const void*>(&paged_mixed_kernel<BITS, RW, PACK, PARTS>), hipFuncAttributeMaxDynamicSharedMemorySize, kLdsBytes);
 }
-
 template <int BITS, int RW>
 hipError_t allow_lds()
 {
-    return hipFuncSetAttribute(reinterpret_cast<const void*>(&paged_rows_kernel<BITS, RW>), hipFuncAttributeMaxDynamicSharedMemorySize, kLdsBytes);
+    hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(&paged_rows_kernel<BITS, RW>), hipFuncAttributeMaxDynamicSharedMemorySize, kLdsBytes);
+    if (e == hipSuccess) e = allow_lds_mixed<BITS, RW, true, 1>();
+    if (e == hipSuccess) e = allow_lds_mixed<BITS, RW, false, 1>();
+    if constexpr (BITS == 4) {
+        if (e == hipSuccess) e = allow_lds_mixed<BITS, RW, true, 2>();
+        if (e == hipSuccess) e = allow_lds_mixed<BITS, RW, false, 2>();
+    }
+    return e;
+}
+
+template <int BITS, int RW>
+hipError_t launch(const PagedPool& pool, const PagedSeqs& seqs, const uint16_t* Q, long q_stride, uint16_t* O, int q_heads, float scale, const PagedForm& f, void* workspace,
+                  hipStream_t stream)
+{
+    constexpr int ROWS = 32 * RW;
+    char* const space = (char*)workspace + kPagedCounterBytes;
+    float* const partial = (float*)(space + kPagedColumnBytes);
+    const RowsPlan plan{f.least_rows, f.target, (uint32_t)std::min(kPagedRowBytes / (kPieceFloats<RW> * sizeof(float)), (size_t)f.target * 2)};
+    const unsigned long tiles = (unsigned long)f.items * pool.heads, ctas = tiles + plan.slots, cut = std::min(tiles, (unsigned long)plan.slots / 2);
+    const float s = scale * 1.4426950408889634f;
+    if (ctas < 1 || ctas > 0x7ffff000UL) return hipErrorInvalidValue;
+    if (f.together) {
+        const ColumnsPart few{f.column_rows, (uint32_t)f.column_ctas, (float*)space, (uint32_t*)workspace};
+        auto pick = [&](auto parts) {
+            constexpr int PARTS = decltype(parts)::value;
+            return f.columns == 8 ? paged_mixed_kernel<BITS, RW, true, PARTS> : paged_mixed_kernel<BITS, RW, false, PARTS>;
+        };
+        auto kernel = pick(std::integral_constant<int, 1>{});
+        if constexpr (BITS == 4)
+            if (pool.run_log == 0) kernel = pick(std::integral_constant<int, 2>{});
+        hipLaunchKernelGGL(kernel, dim3((unsigned)(ctas + few.ctas)), dim3(512), kLdsBytes, stream, pool, seqs, Q, q_stride, O, q_heads, s, plan, partial, few);
+    } else {
+        hipLaunchKernelGGL((paged_rows_kernel<BITS, RW>), dim3((unsigned)ctas), dim3(512), kLdsBytes, stream, pool, seqs, Q, q_stride, O, q_heads, s, plan, partial);
+    }
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess || plan.target == 0) return e;
+    hipLaunchKernelGGL((paged_rows_merge_kernel<RW>), dim3((unsigned)(cut * (ROWS / kMergeRows))), dim3(256), 0, stream, pool.heads, seqs, O, q_heads, plan, partial);
+    return hipGetLastError();
 }
 
 }  // namespace
@@ -266,6 +322,9 @@ hipError_t paged_rows_setup()
 // 8-bit codes take the memory's time sooner: 256 of 300 / 1000 31 / 86 (48 / 98), 128 of 1000 43 (50), but 64 of 1000 26.9 (25.0), 256 skewed ones up to 9000 212 (200), 64 skewed 97 (87),
 // 256 x 5 after 1000, whose segments need two column tiles, 183 (152): from four segments a compute unit on.  Below that two CTAs a compute unit hide each other's starts if contexts are
 // short: 48 of 300 10.2 us (13.0 with one), 64 of 500 14.2 (15.3), 64 of 2000 42.8 (45), but 40 of 2000 to 4000 50 (45).
+// Both in one call go in one launch, the columns' CTAs (eight waves) first, on half the compute units, or 11 / 16 where row tiles are few (64 decoding at up to 4000 and a chunk of 512 at
+// 4000, 8-bit: 146 us, 154 with 11 / 16, 160 in two launches; 40 decoding and chunks of 1500 and 750: 141, 147, 161; 128 at 1000 and 512 at 2000: 99, 105, 117; 200 at 2000 and a prompt
+// of 256: 157, 143, 147; 300 at 300 and one of 64: 45, 40, 47).  Behind the row tiles the columns' long pieces stick out: 144, 151, 107, 149, 42; on all compute units first 157, 160, 113, 149, 42.
 // 128 or 256 rows a CTA: a stage of 128 costs 0.66 of one of 256 (the four prompts above: 1154 against 867 us).  So 256, unless the chip does not fill with either and pieces cannot
 // make up for it, a context being short (two prompts of 307 and 161 tokens, 2 / 1 heads: 19 against 20 us; 400 and 150, 16 / 1: 34 against 39).  Over 57 random calls (one chunk after
 // up to 40000 tokens, up to six prompts, up to 30 decoding sequences with chunks; 1 to 8 KV heads, 1 to 16 query heads each) the rule's choice takes 1.02 of the better one's time,
@@ -289,6 +348,7 @@ PagedForm paged_form(const PagedPool& pool, const PagedSeqs& seqs, int q_heads, 
         return f;
     }
     f.least_rows = f.column_rows + 1;
+    f.together = f.column_rows && most_units < 2147483648.0;
     const int len = max_len > 0 && max_len < seqs.cap ? max_len : seqs.cap, stages = (len + ST - 1) / ST;
     const long rows = (long)seqs.tokens * G, big = rows / f.least_rows < seqs.batch ? rows / f.least_rows : seqs.batch, equal = (rows + most - 1) / most;
     const int past_none = (int)((most / G + ST - 1) / ST);   // stages of the longest new tokens alone
@@ -305,6 +365,7 @@ PagedForm paged_form(const PagedPool& pool, const PagedSeqs& seqs, int q_heads, 
             f.pieces = cut ? (stages + kLeastStages - 1) / kLeastStages : 1;
         }
     }
+    if (f.together) f.column_ctas = std::min(rows / (32 * f.row_waves) * pool.heads >= num_cu / 4 ? num_cu / 2 : num_cu * 11 / 16, kPagedMostCtas / 2);
     return f;
 }
 
@@ -314,17 +375,12 @@ hipError_t launch_paged_attn(const PagedPool& pool, const PagedSeqs& seqs, const
     const PagedForm f = paged_form(pool, seqs, q_heads, max_count, max_len, num_cu);
     hipError_t e = hipSuccess;
     if (f.row_waves) {
-        const size_t room = kPagedPartialBytes / ((size_t)(32 * f.row_waves) * (2 + kHeadDim) * sizeof(float));
-        const RowsPlan plan{f.least_rows, f.target, (uint32_t)std::min(room, (size_t)f.target * 2)};
-        float* const partial = (float*)((char*)workspace + kPagedCounterBytes);
         if (pool.bits == 8)
-            e = f.row_waves == 8 ? launch<8, 8>(pool, seqs, Q, q_stride, O, q_heads, scale, plan, f.items, partial, stream)
-                                 : launch<8, 4>(pool, seqs, Q, q_stride, O, q_heads, scale, plan, f.items, partial, stream);
+            e = f.row_waves == 8 ? launch<8, 8>(pool, seqs, Q, q_stride, O, q_heads, scale, f, workspace, stream) : launch<8, 4>(pool, seqs, Q, q_stride, O, q_heads, scale, f, workspace, stream);
         else
-            e = f.row_waves == 8 ? launch<4, 8>(pool, seqs, Q, q_stride, O, q_heads, scale, plan, f.items, partial, stream)
-                                 : launch<4, 4>(pool, seqs, Q, q_stride, O, q_heads, scale, plan, f.items, partial, stream);
+            e = f.row_waves == 8 ? launch<4, 8>(pool, seqs, Q, q_stride, O, q_heads, scale, f, workspace, stream) : launch<4, 4>(pool, seqs, Q, q_stride, O, q_heads, scale, f, workspace, stream);
     }
-    if (e == hipSuccess && f.column_rows)
+    if (e == hipSuccess && f.column_rows && !f.together)
         e = launch_paged_columns(pool, seqs, Q, q_stride, O, q_heads, scale, f.columns, f.column_rows, f.column_ctas, f.alone, workspace, stream);
     return e;
 }

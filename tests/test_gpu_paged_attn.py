@@ -245,6 +245,26 @@ def test_mixed(tm, bits):
 
 
 @pytest.mark.parametrize("bits", [8, 4])
+@pytest.mark.parametrize("page, heads, q_heads, counts, positions", [
+    (32, 2, 24, [1, 40, 1, 1, 9, 1], [300, 500, 0, 95, 64, 2100]),         # sixteen columns; parts of a block on pages of their own
+    (32, 1, 3, [2, 200, 5, 1], [33, 3000, 700, 4000]),
+    (128, 8, 8, [1] * 70 + [300], [11 * i for i in range(70)] + [50]),     # more sequences than lanes, and more segments than waves
+])
+def test_mixed_forms(tm, bits, page, heads, q_heads, counts, positions):
+    Setup(tm, bits, page, heads, counts, positions, q_heads=q_heads, before=1, behind=2, seed=page, max_count=max(counts), max_len=max(n + p for n, p in zip(counts, positions))).check(
+        (True, True, True, True))
+
+
+def test_mixed_over_a_wide_table(tm):
+    """Wider than a wave's count of blocks allows: two launches."""
+    s = Setup(tm, 8, 64, 8, [1, 100, 3], [200, 900, 70], q_heads=32, seed=5, max_count=100, max_len=1000)
+    s.check((True, True, True, True))
+    s.table = np.pad(s.table, ((0, 0), (0, 2600000 - s.table.shape[1])), constant_values=-1)
+    s.batch = tm.PagedBatch(_dev(s.table), s.batch.offsets, s.batch.positions, max_count=100, max_len=1000)
+    s.check((True, True, True, True))
+
+
+@pytest.mark.parametrize("bits", [8, 4])
 @pytest.mark.parametrize("hints", [dict(), dict(max_count=1), dict(max_count=1, max_len=1), dict(max_count=5, max_len=10), dict(max_len=40), dict(max_count=1 << 20, max_len=1 << 20)])
 def test_results_do_not_depend_on_the_hints(tm, bits, hints):
     """Hints that are missing, far too small or too large."""
