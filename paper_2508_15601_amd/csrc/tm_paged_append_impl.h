@@ -4,8 +4,8 @@
 // touches are numbered over the sequences on the device, so the grid is an upper bound (every run has a token, and a sequence of n tokens touches at most n / 32 + 2) and
 // surplus CTAs end at once.
 //
-// Measured: 10 prompts of 901 tokens, 28 / 4 heads, 4-bit, keys and queries turned: 31 us (152 MB, 4.9 TB/s, most of it the queries, a wave a token); 4 x 2000, 32 / 8 heads, 8-bit 44 us
-// (4.1 TB/s): memory.
+// Measured: 10 prompts of 451 to 901 tokens, 28 / 4 heads, 4-bit, keys and queries turned, nothing in the caches: 29 us (114 MB, 3.9 TB/s, most of it the queries, a wave a token);
+// 4 x 2000, 32 / 8 heads, 8-bit 42 us (4.3 TB/s): memory and, for the keys, 64-bit arithmetic.
 #pragma once
 
 namespace tmw4 {
@@ -14,122 +14,129 @@ namespace {
 
 constexpr int kAppendLds = 2 * 4096;
 
-// 256 threads.  Sixteen lanes hold a token's vector, eight dimensions each; a thread takes two tokens, keys then values (the layout of the block-wise append
+// 256 threads, heads h0 .. h1 - 1.  Sixteen lanes hold a token's vector, eight dimensions each; a thread takes two tokens, keys then values (the layout of the block-wise append
 // of the contiguous cache).  All four vectors are requested before the angles are worked out, which hides behind them: sines and cosines of the run's new tokens,
-// a thread a pair at a time, go through LDS.
+// a thread a pair at a time, go through LDS.  The next head's vectors are requested while this one's codes are stored.
 template <int BITS>
-__device__ __forceinline__ void append_run(const PagedPool& pool, const PagedSeqs& seqs, PagedRows k, PagedRows v, const RopePlan& rope, uint32_t item, int h,
-                                           unsigned char* lds, CosSin* cs)
+__device__ __forceinline__ void append_run(const PagedPool& pool, const PagedSeqs& seqs, PagedRows k, PagedRows v, const RopePlan& rope, uint32_t item, int h0,
+                                           int h1, unsigned char* lds, CosSin* cs)
 {
     const int tid = threadIdx.x, lane = tid & 63, sub = tid & 15;
     const RunJob job = run_job(pool, seqs, item, lane);
     if (!job.live || job.page < 0) return;                             // CTA-uniform
     const int u0 = job.u0, u1 = job.u1;
-    u32x4 raw[4];
     int slot[2];
+    u32x4 raw[4];
+    auto request = [&](int h) {
 #pragma unroll
-    for (int it = 0; it < 4; ++it) {
-        const int u = (tid >> 6) * 8 + (it & 1) * 4 + (lane >> 4);
-        slot[it & 1] = u;
-        raw[it] = u32x4{0u, 0u, 0u, 0u};
-        if (u >= u0 && u < u1) {
-            const PagedRows& r = it >> 1 ? v : k;
-            raw[it] = *(const u32x4*)(r.p + (job.row + u) * r.stride + h * kHeadDim + 8 * sub);
+        for (int it = 0; it < 4; ++it) {
+            const int u = (tid >> 6) * 8 + (it & 1) * 4 + (lane >> 4);
+            slot[it & 1] = u;
+            raw[it] = u32x4{0u, 0u, 0u, 0u};
+            if (u >= u0 && u < u1) {
+                const PagedRows& r = it >> 1 ? v : k;
+                raw[it] = *(const u32x4*)(r.p + (job.row + u) * r.stride + h * kHeadDim + 8 * sub);
+            }
         }
-    }
-    const int pairs = rope.rot / 2;
+    };
+    request(h0);
     if (rope.rot) {
-        for (int i = tid; i < (u1 - u0) * pairs; i += 256) {
-            const int u = u0 + i / pairs, p = i % pairs;
-            cs[u * (kHeadDim / 2) + p] = rope_angle(rope, job.run * kRun + u, rope.turns[p]);
+        const int pairs = rope.rot / 2, at_once = 64 / pairs, tok = lane / pairs, p = lane - tok * pairs;      // tokens of a wave at a time
+        if (tok < at_once) {
+            const uint64_t turns = rope.turns[p];
+            for (int u = u0 + (tid >> 6) * at_once + tok; u < u1; u += 4 * at_once) cs[u * (kHeadDim / 2) + p] = rope_angle(rope, job.run * kRun + u, turns);
         }
         __syncthreads();
     }
-    const size_t run = paged_run(pool, job.page, h, job.run);
     uint32_t* const words = reinterpret_cast<uint32_t*>(lds);          // 4-bit: keys in cache order, then value codes [token][136]
     uint8_t* const vcodes = lds + 2048;
+    const bool whole = u0 == 0 && u1 == kRun;
+    for (int h = h0; h < h1; ++h) {
+        const size_t run = paged_run(pool, job.page, h, job.run);
 #pragma unroll
-    for (int it = 0; it < 4; ++it) {
-        const int which = it >> 1, u = slot[it & 1];
-        const bool live = u >= u0 && u < u1;
-        if (which == 0 && rope.rot) raw[it] = rope_sixteenth(raw[it], rope, cs + (live ? u : u0) * (kHeadDim / 2), lane);
-        uint32_t q[8];
-        const uint32_t pair = quantise_row8<BITS>(raw[it], q);
-        u32x2 bytes;
-        bytes[0] = q[0] | (q[1] << 8) | (q[2] << 16) | (q[3] << 24);
-        bytes[1] = q[4] | (q[5] << 8) | (q[6] << 16) | (q[7] << 24);
-        if constexpr (BITS == 8) {
-            if (which == 0) {
-                const int d = 8 * sub, chunk = ((u >> 4) * 2 + ((d & 31) >> 4)) * 64 + 16 * (d >> 5) + (u & 15);
-                *reinterpret_cast<u32x2*>(lds + chunk * 16 + (d & 15)) = bytes;
+        for (int it = 0; it < 4; ++it) {
+            const int which = it >> 1, u = slot[it & 1];
+            const bool live = u >= u0 && u < u1;
+            if (which == 0 && rope.rot) raw[it] = rope_sixteenth(raw[it], rope, cs + (live ? u : u0) * (kHeadDim / 2), lane);
+            uint32_t q[8];
+            const uint32_t pair = quantise_row8<BITS>(raw[it], q);
+            u32x2 bytes;
+            bytes[0] = q[0] | (q[1] << 8) | (q[2] << 16) | (q[3] << 24);
+            bytes[1] = q[4] | (q[5] << 8) | (q[6] << 16) | (q[7] << 24);
+            if constexpr (BITS == 8) {
+                if (which == 0) {
+                    const int d = 8 * sub, chunk = ((u >> 4) * 2 + ((d & 31) >> 4)) * 64 + 16 * (d >> 5) + (u & 15);
+                    *reinterpret_cast<u32x2*>(lds + chunk * 16 + (d & 15)) = bytes;
+                } else {
+                    const int hh = (u & 15) >> 2, e = (u & 3) + 4 * (u >> 4);
+#pragma unroll
+                    for (int n = 0; n < 8; ++n) {
+                        const int d = 8 * sub + n, i = d >> 4;
+                        lds[4096 + ((i >> 1) * 64 + 16 * hh + (d & 15)) * 16 + (i & 1) * 8 + e] = (uint8_t)q[n];
+                    }
+                }
             } else {
-                const int hh = (u & 15) >> 2, e = (u & 3) + 4 * (u >> 4);
+                if (which == 0) {
+                    const int chunk = (u >> 4) * 64 + 16 * (sub >> 2) + (u & 15);
+                    uint32_t w = 0;
 #pragma unroll
-                for (int n = 0; n < 8; ++n) {
-                    const int d = 8 * sub + n, i = d >> 4;
-                    lds[4096 + ((i >> 1) * 64 + 16 * hh + (d & 15)) * 16 + (i & 1) * 8 + e] = (uint8_t)q[n];
+                    for (int e = 0; e < 8; ++e) w |= q[e] << (4 * ((e >> 1) + 4 * (e & 1)));
+                    words[chunk * 4 + (sub & 3)] = w;
+                } else {
+                    *reinterpret_cast<u32x2*>(vcodes + u * 136 + 8 * sub) = bytes;
                 }
             }
+            if (live && sub == 0) pool.pairs[(run * kRun + u) * 2 + which] = pair;
+        }
+        __syncthreads();
+        if (h + 1 < h1) request(h + 1);
+        if constexpr (BITS == 8) {
+            const u32x4 kc = *reinterpret_cast<const u32x4*>(lds + tid * 16);
+            u32x4 vc = *reinterpret_cast<const u32x4*>(lds + 4096 + tid * 16);
+            u32x4* const kd = reinterpret_cast<u32x4*>(pool.k + run * 4096) + tid;
+            u32x4* const vd = reinterpret_cast<u32x4*>(pool.v + run * 4096) + tid;
+            const int ku = (tid >> 7) * 16 + (tid & 15);                   // a key chunk is one token's
+            if (whole || (ku >= u0 && ku < u1)) *kd = kc;
+            if (!whole) {                                                  // a value chunk holds eight: e % 4 + 4 * hh + 16 * (e / 4)
+                const int hh = (tid & 63) >> 4;
+                uint32_t lo = 0, hi = 0;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int a = e + 4 * hh;
+                    if (a >= u0 && a < u1) lo |= 0xffu << (8 * e);
+                    if (a + 16 >= u0 && a + 16 < u1) hi |= 0xffu << (8 * e);
+                }
+                const u32x4 old = *vd;
+                const u32x4 keep = {lo, hi, lo, hi};
+                vc = (vc & keep) | (old & ~keep);
+            }
+            *vd = vc;
         } else {
-            if (which == 0) {
-                const int chunk = (u >> 4) * 64 + 16 * (sub >> 2) + (u & 15);
-                uint32_t w = 0;
-#pragma unroll
-                for (int e = 0; e < 8; ++e) w |= q[e] << (4 * ((e >> 1) + 4 * (e & 1)));
-                words[chunk * 4 + (sub & 3)] = w;
+            const int chunk = tid & 127;
+            if (tid < 128) {
+                const int ku = (chunk >> 6) * 16 + (chunk & 15);
+                if (whole || (ku >= u0 && ku < u1))
+                    reinterpret_cast<u32x4*>(pool.k + run * 2048)[chunk] = *reinterpret_cast<const u32x4*>(words + chunk * 4);
             } else {
-                *reinterpret_cast<u32x2*>(vcodes + u * 136 + 8 * sub) = bytes;
+                const int ii = chunk >> 6, hh = (chunk & 63) >> 4, c = chunk & 15;
+                u32x4 vc = {0u, 0u, 0u, 0u};
+                uint32_t keep = 0;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const int u = (e & 3) + 4 * hh + 16 * (e >> 2), sh = 4 * ((e >> 1) + 4 * (e & 1));
+                    if (u >= u0 && u < u1) keep |= 0xfu << sh;
+#pragma unroll
+                    for (int w = 0; w < 4; ++w) vc[w] |= (uint32_t)vcodes[u * 136 + 16 * (4 * ii + w) + c] << sh;
+                }
+                u32x4* const vd = reinterpret_cast<u32x4*>(pool.v + run * 2048) + chunk;
+                if (!whole) {
+                    const u32x4 old = *vd, mask = {keep, keep, keep, keep};
+                    vc = (vc & mask) | (old & ~mask);
+                }
+                *vd = vc;
             }
         }
-        if (live && sub == 0) pool.pairs[(run * kRun + u) * 2 + which] = pair;
-    }
-    __syncthreads();
-    const bool whole = u0 == 0 && u1 == kRun;
-    if constexpr (BITS == 8) {
-        const u32x4 kc = *reinterpret_cast<const u32x4*>(lds + tid * 16);
-        u32x4 vc = *reinterpret_cast<const u32x4*>(lds + 4096 + tid * 16);
-        u32x4* const kd = reinterpret_cast<u32x4*>(pool.k + run * 4096) + tid;
-        u32x4* const vd = reinterpret_cast<u32x4*>(pool.v + run * 4096) + tid;
-        const int ku = (tid >> 7) * 16 + (tid & 15);                   // a key chunk is one token's
-        if (whole || (ku >= u0 && ku < u1)) *kd = kc;
-        if (!whole) {                                                  // a value chunk holds eight: e % 4 + 4 * hh + 16 * (e / 4)
-            const int hh = (tid & 63) >> 4;
-            uint32_t lo = 0, hi = 0;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const int a = e + 4 * hh;
-                if (a >= u0 && a < u1) lo |= 0xffu << (8 * e);
-                if (a + 16 >= u0 && a + 16 < u1) hi |= 0xffu << (8 * e);
-            }
-            const u32x4 old = *vd;
-            const u32x4 keep = {lo, hi, lo, hi};
-            vc = (vc & keep) | (old & ~keep);
-        }
-        *vd = vc;
-    } else {
-        const int chunk = tid & 127;
-        if (tid < 128) {
-            const int ku = (chunk >> 6) * 16 + (chunk & 15);
-            if (whole || (ku >= u0 && ku < u1))
-                reinterpret_cast<u32x4*>(pool.k + run * 2048)[chunk] = *reinterpret_cast<const u32x4*>(words + chunk * 4);
-            return;
-        }
-        const int ii = chunk >> 6, hh = (chunk & 63) >> 4, c = chunk & 15;
-        u32x4 vc = {0u, 0u, 0u, 0u};
-        uint32_t keep = 0;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const int u = (e & 3) + 4 * hh + 16 * (e >> 2), sh = 4 * ((e >> 1) + 4 * (e & 1));
-            if (u >= u0 && u < u1) keep |= 0xfu << sh;
-#pragma unroll
-            for (int w = 0; w < 4; ++w) vc[w] |= (uint32_t)vcodes[u * 136 + 16 * (4 * ii + w) + c] << sh;
-        }
-        u32x4* const vd = reinterpret_cast<u32x4*>(pool.v + run * 2048) + chunk;
-        if (!whole) {
-            const u32x4 old = *vd, mask = {keep, keep, keep, keep};
-            vc = (vc & mask) | (old & ~mask);
-        }
-        *vd = vc;
+        if (h + 1 < h1) __syncthreads();
     }
 }
 
@@ -152,13 +159,15 @@ __device__ __forceinline__ void rotate_row(const PagedSeqs& seqs, PagedRows q, u
 
 // Blocks 0 .. kv_blocks - 1: runs of keys and values, heads of a run next to each other; the blocks behind them: queries, a wave `per_wave` heads of a row.
 template <int BITS>
-__global__ __launch_bounds__(256) void paged_append_kernel(PagedPool pool, PagedSeqs seqs, PagedRows k, PagedRows v, RopePlan rope, unsigned kv_blocks, PagedRows q,
-                                                           uint16_t* q_out, long q_out_stride, int q_heads, int per_wave)
+__global__ __launch_bounds__(256) void paged_append_kernel(PagedPool pool, PagedSeqs seqs, PagedRows k, PagedRows v, RopePlan rope, unsigned kv_blocks, int kv_heads,
+                                                           PagedRows q, uint16_t* q_out, long q_out_stride, int q_heads, int per_wave)
 {
     __shared__ __align__(16) unsigned char lds[kAppendLds];
     __shared__ CosSin cs[kRun * kHeadDim / 2];
     if (blockIdx.x < kv_blocks) {
-        append_run<BITS>(pool, seqs, k, v, rope, blockIdx.x / (unsigned)pool.heads, (int)(blockIdx.x % (unsigned)pool.heads), lds, cs);
+        const unsigned groups = (unsigned)((pool.heads + kv_heads - 1) / kv_heads), run = blockIdx.x / groups;
+        const int h0 = (int)(blockIdx.x - run * groups) * kv_heads;
+        append_run<BITS>(pool, seqs, k, v, rope, run, h0, min(h0 + kv_heads, pool.heads), lds, cs);
         return;
     }
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -254,12 +263,16 @@ hipError_t launch_paged_append(const PagedPool& pool, const PagedSeqs& seqs, Pag
         hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(256), 0, stream, pool, seqs, k, v, plan, q, q_out, q_out_stride, heads, per_token, max_count);
         return hipGetLastError();
     }
-    const long kv = most_runs(seqs) * pool.heads;
+    // KV heads a CTA: they share a run's sines and cosines, but take their turns.  One, two and four of them, 8 heads, 8-bit: 4 x 2000 tokens with queries 47.6 / 45.2 / 42.0 us, without
+    // 24.5 / 22.3 / 24.1, not turned 14.8 / 14.3 / 16.5; 512 tokens with queries 7.4 / 10.0 / 15.4.  Queries fill the chip beside fewer CTAs.
+    const long each = most_runs(seqs) * pool.heads;
+    const int kv_heads = std::min(!plan.rot ? 1 : q.p ? each >= 880 ? 4 : each >= 440 ? 2 : 1 : each >= 1000 ? 2 : 1, pool.heads);
+    const long kv = most_runs(seqs) * ((pool.heads + kv_heads - 1) / kv_heads);
     const int per_wave = (long)seqs.tokens * q_heads >= 16384L * 8 ? q_heads : 8;
     const long jobs = q.p ? (long)seqs.tokens * ((q_heads + per_wave - 1) / per_wave) : 0, blocks = kv + (jobs + 3) / 4;
     if (blocks <= 0 || blocks > 0x7fffffffL) return hipErrorInvalidValue;
     const auto kernel = pool.bits == 8 ? paged_append_kernel<8> : paged_append_kernel<4>;
-    hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(256), 0, stream, pool, seqs, k, v, plan, (unsigned)kv, q, q_out, q_out_stride, q_heads, per_wave);
+    hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(256), 0, stream, pool, seqs, k, v, plan, (unsigned)kv, kv_heads, q, q_out, q_out_stride, q_heads, per_wave);
     return hipGetLastError();
 }
 

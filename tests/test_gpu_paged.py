@@ -243,6 +243,29 @@ def test_append_and_read(tm, bits, page, heads, counts, positions, cols, turn):
 
 
 @pytest.mark.parametrize("bits", [8, 4])
+@pytest.mark.parametrize("heads, counts, positions, cols", [(9, [1700, 1400, 77], [0, 45, 1000], 14), (8, [900, 803], [5, 64], 8), (3, [1000], [31], 9)])
+def test_append_of_prompts(tm, bits, heads, counts, positions, cols):
+    """Several KV heads a CTA, with and without queries beside them; heads that do not divide evenly."""
+    _say(f"append bits={bits} heads={heads} counts={counts}")
+    pool = Pool(tm, bits, 128, heads, counts, positions, cols, seed=heads, before=1, behind=1)
+    for rope in (_rope(tm, 96), None):
+        _check_append(tm, pool, rope, q_heads=heads)
+    _check_read(tm, pool)
+
+
+@pytest.mark.parametrize("bits", [8, 4])
+def test_append_of_a_prompt_without_queries(tm, bits):
+    pool = Pool(tm, bits, 64, 5, [7000], [3], 110, seed=bits)
+    K, V = (_dev(np.random.default_rng(i).standard_normal((7000, 5, 128)).astype(np.float16)) for i in range(2))
+    rope = _rope(tm, 128)
+    tm.tm_paged_append(pool.cache, pool.batch, K, V, rope=rope)
+    got = pool.arrays()
+    tm.tm_paged_append(pool.cache, pool.batch, K, V, rope=rope, Q=K, Q_out=K.clone())
+    for a, b in zip(got, pool.arrays()):
+        assert np.array_equal(_bits(a), _bits(b))
+
+
+@pytest.mark.parametrize("bits", [8, 4])
 @pytest.mark.parametrize("batch", [63, 64, 65, 130, 700])
 def test_many_sequences(tm, bits, batch):
     """More sequences than a wave has lanes; counts of none, one and a few."""
