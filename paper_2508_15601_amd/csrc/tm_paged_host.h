@@ -7,11 +7,12 @@ namespace tmw4 {
 
 // Workspace of tm_paged_attn: arrival counters, then partial results of contexts that are cut into pieces.
 constexpr size_t kPagedCounterBytes = 32 * 1024;
-constexpr size_t kPagedColumnBytes = 34u << 20;           // two pieces each of 2048 waves
-constexpr size_t kPagedRowBytes = 66u << 20;              // 520 pieces of 256 rows
+constexpr size_t kPagedColumnBytes = 23u << 20;           // two pieces each of 1408 waves
+constexpr size_t kPagedRowBytes = 33u << 20;              // 259 pieces of 256 rows
 constexpr size_t kPagedWorkspaceBytes = kPagedCounterBytes + kPagedColumnBytes + kPagedRowBytes;
 
 constexpr int kPagedMostCtas = 512;      // of a launch whose CTAs share contexts
+constexpr int kPagedMostWaves = 1408;    // of one whose waves do
 
 struct PagedRows {                       // a packed array of new tokens: row r at p + r * stride
     const uint16_t* p;

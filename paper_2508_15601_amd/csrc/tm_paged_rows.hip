@@ -62,13 +62,21 @@ struct RowsWork {
         if (per == 1 && lane < s.batch) own = rows_shape<RW>(paged_seq(s, lane), s, g, p);
     }
     __device__ __forceinline__ RowsShape shape(int b) const { return rows_shape<RW>(paged_seq(seqs, b), seqs, G, plan); }
-    // Sum over the lane's sequences before `end` of f(shape).
+    // f(shape) of the lane's sequences before `end`, and its sum.
+    template <class F>
+    __device__ __forceinline__ void each(int end, F f) const
+    {
+        if (per == 1) {
+            if (first < end) f(own);
+        } else {
+            for (int b = first; b < min(first + per, end); ++b) f(shape(b));
+        }
+    }
     template <class T, class F>
     __device__ __forceinline__ T sum(int end, F f) const
     {
-        if (per == 1) return first < end ? f(own) : T(0);
         T v = T(0);
-        for (int b = first; b < min(first + per, end); ++b) v += f(shape(b));
+        each(end, [&](const RowsShape& r) { v += f(r); });
         return v;
     }
 };
@@ -111,9 +119,18 @@ __device__ __forceinline__ int piece_stages(const RowsWork<RW>& w, int heads, co
         for (int m = 1; m < 64; m <<= 1) least = fminf(least, __shfl_xor(least, m));
         best = __builtin_amdgcn_readlane((int)tried, __builtin_ctzll(__builtin_amdgcn_ballot_w64(cost == least) | 1ull << 63));
     }
+    // The workspace has room for `slots` pieces of cut contexts: a little longer if need be, and never more than twice the mean work.
     best = __builtin_amdgcn_readfirstlane(best);
-    const uint32_t cut = w.template sum<uint32_t>(w.seqs.batch, [&](const RowsShape& r) { return r.stages > (uint32_t)best ? r.tiles * pieces_of(r.stages, best) : 0u; });
-    return wave_total(cut) * (uint32_t)heads <= plan.slots ? best : kWhole;
+    const int tries[4] = {best, best + best / 8 + 1, best + best / 2 + 1, max(best, (int)fminf(2.f * work * (float)heads / (float)plan.slots, (float)kWhole) + 1)};
+    uint32_t cut[4] = {0u, 0u, 0u, 0u};
+    w.each(w.seqs.batch, [&](const RowsShape& r) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) cut[i] += r.stages > (uint32_t)tries[i] ? r.tiles * pieces_of(r.stages, tries[i]) : 0u;
+    });
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        if ((uint64_t)wave_total(cut[i]) * (uint32_t)heads <= plan.slots) return __builtin_amdgcn_readfirstlane(tries[i]);
+    return kWhole;
 }
 
 // Piece `unit` of the launch, or with MERGE row tile `unit` of those that are cut: its sequence, first row, context, pieces, and where its pieces' results go.  False: there
@@ -342,7 +359,7 @@ PagedForm paged_form(const PagedPool& pool, const PagedSeqs& seqs, int q_heads, 
     f.alone = (pool.bits == 4 ? segments > num_cu : f.columns < 32 && segments >= 4L * num_cu) && most_units < 2147483648.0;      // (counted in 32 bits)
     if (f.alone && f.columns == 32) f.columns = 16;
     const bool twice = pool.bits == 8 && !f.alone && f.columns < 32 && segments > num_cu && max_len > 0 && max_len <= 1024;
-    f.column_ctas = std::min(twice ? 2 * num_cu : num_cu, kPagedMostCtas);
+    f.column_ctas = std::min(twice ? 2 * num_cu : num_cu, f.alone ? kPagedMostWaves / 4 : kPagedMostCtas);
     if (most <= 64) {
         f.column_rows = 1 << 30;                             // whatever the offsets say
         return f;
@@ -365,7 +382,7 @@ PagedForm paged_form(const PagedPool& pool, const PagedSeqs& seqs, int q_heads, 
             f.pieces = cut ? (stages + kLeastStages - 1) / kLeastStages : 1;
         }
     }
-    if (f.together) f.column_ctas = std::min(rows / (32 * f.row_waves) * pool.heads >= num_cu / 4 ? num_cu / 2 : num_cu * 11 / 16, kPagedMostCtas / 2);
+    if (f.together) f.column_ctas = std::min(rows / (32 * f.row_waves) * pool.heads >= num_cu / 4 ? num_cu / 2 : num_cu * 11 / 16, kPagedMostWaves / 8);
     return f;
 }
 
