@@ -34,6 +34,23 @@ struct Column {
     }
 };
 
+// The value plus those of lanes 16 and 32 apart, and plus that of the lane 8 apart, without a trip through LDS.
+__device__ __forceinline__ float fold_halves(float v)
+{
+#if defined(__HIP_DEVICE_COMPILE__)
+    auto add = [](auto r) { return __builtin_bit_cast(float, (uint32_t)r[0]) + __builtin_bit_cast(float, (uint32_t)r[1]); };
+    uint32_t a = __builtin_bit_cast(uint32_t, v);
+    v = add(__builtin_amdgcn_permlane16_swap(a, a, false, false));
+    a = __builtin_bit_cast(uint32_t, v);
+    v = add(__builtin_amdgcn_permlane32_swap(a, a, false, false));
+#endif
+    return v;
+}
+__device__ __forceinline__ float fold_row(float v)
+{
+    return v + __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, v), 0x128, 0xf, 0xf, true));       // row_ror 8
+}
+
 // A wave's part: sixteen query columns, or eight (PACK), on the 16x16x32 instruction, with the arithmetic of decode attention over the contiguous cache (tm_attn_device.h).
 template <int BITS, bool PACK>
 struct Columns {
@@ -103,8 +120,8 @@ struct Columns {
     }
     __device__ __forceinline__ void sums(float& l, float& corr) const
     {
-        l = xor_add(xor_add(st.l_run, 16), 32), corr = xor_add(xor_add(st.corr, 16), 32);
-        if constexpr (PACK) l = xor_add(l, 8), corr = xor_add(corr, 8);
+        l = fold_halves(st.l_run), corr = fold_halves(st.corr);
+        if constexpr (PACK) l = fold_row(l), corr = fold_row(corr);
     }
     // A wave that has its columns to itself: o[i] are dimensions 16 * i + 4 * (lane / 16) ...
     __device__ __forceinline__ void alone(float& M, float& L, f32x4 (&o)[8])

@@ -49,10 +49,11 @@ __device__ __forceinline__ PagedSeq paged_seq(const PagedSeqs& s, int b)
 }
 
 // Inclusive sum over the lanes of a wave: rows of sixteen lanes, then the rows' totals to the rows behind them.
-__device__ __forceinline__ uint32_t wave_sums(uint32_t v)
+template <class F>
+__device__ __forceinline__ uint32_t wave_scan(uint32_t v, F f)              // f(0, v) = v
 {
     auto add = [&](auto CTRL, auto ROWS) {
-        v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, decltype(CTRL)::value, decltype(ROWS)::value, 0xf, false);
+        v = f(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, decltype(CTRL)::value, decltype(ROWS)::value, 0xf, false));
     };
     add(std::integral_constant<int, 0x111>{}, std::integral_constant<int, 0xf>{});   // row_shr by 1, 2, 4, 8
     add(std::integral_constant<int, 0x112>{}, std::integral_constant<int, 0xf>{});
@@ -63,11 +64,13 @@ __device__ __forceinline__ uint32_t wave_sums(uint32_t v)
     return v;
 }
 
+__device__ __forceinline__ uint32_t wave_sums(uint32_t v)
+{
+    return wave_scan(v, [](uint32_t a, uint32_t b) { return a + b; });
+}
 __device__ __forceinline__ uint32_t wave_greatest(uint32_t v)
 {
-#pragma unroll
-    for (int m = 1; m < 64; m <<= 1) v = max(v, (uint32_t)__shfl_xor((int)v, m));
-    return (uint32_t)__builtin_amdgcn_readfirstlane((int)v);
+    return (uint32_t)__builtin_amdgcn_readlane((int)wave_scan(v, [](uint32_t a, uint32_t b) { return max(a, b); }), 63);
 }
 __device__ __forceinline__ uint32_t wave_total(uint32_t v) { return (uint32_t)__builtin_amdgcn_readlane((int)wave_sums(v), 63); }
 
