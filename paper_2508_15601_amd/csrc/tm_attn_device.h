@@ -115,6 +115,7 @@ __device__ __forceinline__ void move_reference(float mx, SoftmaxState& st, f32x4
 // sum of the query's 128 values; neg_qbias = minus the sum of the conversion bias of each code position times the query
 // value it meets.  len: tokens the lane's query column attends over (the same in every lane at a decoding step; at prefill
 // every column has its own causal limit).
+// STEP: a wave takes every STEP-th block.
 // HOLES (paged cache): bit i of `present` tells whether run i of the block lies on a page of the pool; without it the run has no tokens.
 //
 // PACK: at most eight query heads share the KV head.  The query operand then carries every head twice
@@ -122,7 +123,7 @@ __device__ __forceinline__ void move_reference(float mx, SoftmaxState& st, f32x4
 // tile c / 8 only - four scores instead of eight, half the softmax arithmetic.  The probabilities of the other tile's
 // tokens reach the lane through one exchange with lane c ^ 8 before the second product; running sums are per lane over
 // its own tokens and meet at the end (xor 8, 16, 32).
-template <int BITS, bool PACK, int N0, int NH, bool HOLES = false>
+template <int BITS, bool PACK, int N0, int NH, bool HOLES = false, int STEP = 4>
 __device__ __forceinline__ void process_runs(const BlockRegs& r, const uint32_t* sz_slot, const f16x8 (&qf)[4],
                                               float scale_log2e, float qsum, const f32x4& neg_qbias, const Magic& mg, int blk, int len,
                                               int lane, SoftmaxState& st, f32x4 (&acc)[8], uint32_t present = ~0u)
@@ -273,7 +274,7 @@ __device__ __forceinline__ void process_runs(const BlockRegs& r, const uint32_t*
             acc[i] = mfma16x16x32(a, pb[n], acc[i]);
         }
     if constexpr (BITS == 8) {
-        if ((blk >> 2 & 3) == 3) {                           // (wave-uniform) a wave takes every fourth block
+        if (((uint32_t)blk / STEP & 3) == 3) {               // (wave-uniform)
 #pragma unroll
             for (int i = 0; i < 8; ++i) acc[i] += st.bias;
             st.bias = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -283,17 +284,17 @@ __device__ __forceinline__ void process_runs(const BlockRegs& r, const uint32_t*
 
 // A whole block.  The two runs of a 4-bit block go through together, which gives each wave two independent chains of
 // instructions; with two score tiles a lane that takes more registers than there are, so there they go one after the other.
-template <int BITS, bool PACK, bool HOLES = false>
+template <int BITS, bool PACK, bool HOLES = false, int STEP = 4>
 __device__ __forceinline__ void process_block(const BlockRegs& r, const uint32_t* sz_slot, const f16x8 (&qf)[4],
                                               float scale_log2e, float qsum, const f32x4& neg_qbias, const Magic& mg, int blk, int len, int len_all,
                                               int lane, SoftmaxState& st, f32x4 (&acc)[8], uint32_t present = ~0u)
 {
     if constexpr (BITS == 8 || PACK) {
-        process_runs<BITS, PACK, 0, BITS == 8 ? 1 : 2, HOLES>(r, sz_slot, qf, scale_log2e, qsum, neg_qbias, mg, blk, len, lane, st, acc, present);
+        process_runs<BITS, PACK, 0, BITS == 8 ? 1 : 2, HOLES, STEP>(r, sz_slot, qf, scale_log2e, qsum, neg_qbias, mg, blk, len, lane, st, acc, present);
     } else {
-        process_runs<BITS, PACK, 0, 1, HOLES>(r, sz_slot, qf, scale_log2e, qsum, neg_qbias, mg, blk, len, lane, st, acc, present);
+        process_runs<BITS, PACK, 0, 1, HOLES, STEP>(r, sz_slot, qf, scale_log2e, qsum, neg_qbias, mg, blk, len, lane, st, acc, present);
         if (blk * 64 + 32 < len_all)                         // (wave-uniform) the second run may lie wholly behind the context
-            process_runs<BITS, PACK, 1, 1, HOLES>(r, sz_slot, qf, scale_log2e, qsum, neg_qbias, mg, blk, len, lane, st, acc, present);
+            process_runs<BITS, PACK, 1, 1, HOLES, STEP>(r, sz_slot, qf, scale_log2e, qsum, neg_qbias, mg, blk, len, lane, st, acc, present);
     }
 }
 

@@ -97,13 +97,13 @@ struct Columns {
 #pragma unroll
         for (int i = 0; i < 8; ++i) acc[i] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
-    template <int PARTS>
+    template <int PARTS, int STEP>
     __device__ __forceinline__ void block(const BlockRegs& r, const uint32_t* words, const Magic& mg, int blk, int len, int len_all, int lane, uint32_t present)
     {
         if constexpr (PARTS == 1)
-            process_block<BITS, PACK>(r, words, qf, scale_log2e, qsum, neg_qbias, mg, blk, present ? len : 0, len_all, lane, st, acc);
+            process_block<BITS, PACK, false, STEP>(r, words, qf, scale_log2e, qsum, neg_qbias, mg, blk, present ? len : 0, len_all, lane, st, acc);
         else
-            process_block<BITS, PACK, true>(r, words, qf, scale_log2e, qsum, neg_qbias, mg, blk, len, len_all, lane, st, acc, present);
+            process_block<BITS, PACK, true, STEP>(r, words, qf, scale_log2e, qsum, neg_qbias, mg, blk, len, len_all, lane, st, acc, present);
     }
     // The four waves that share the columns meet in LDS: wave `wave` gets the unnormalised values o[i] of dimensions 16 * (2 * wave + i) + 4 * (lane / 16) ... of its lane's column, the
     // reference M and the denominator L.  (One barrier; another has to follow before the next segment's.)
@@ -330,7 +330,7 @@ __device__ __forceinline__ void paged_columns(const PagedPool& pool, const Paged
             const int fill = (use + 2) % 3;
             there[fill] = load(g[fill], ring(fill), blk + 2 * kStep, next);
             next = pages_of(blk + 3 * kStep);
-            form.template block<PARTS>(g[use], ring(use), mg, blk, len, len_all, lane, there[use]);
+            form.template block<PARTS, kStep>(g[use], ring(use), mg, blk, len, len_all, lane, there[use]);
             blk += kStep;
             return blk < blk1;
         };
