@@ -140,6 +140,13 @@ def test_contexts_of_very_different_lengths(tm, bits, batch):
     Setup(tm, bits, 32, 1 if batch > 64 else 2, counts.tolist(), positions.tolist(), q_heads=4, max_count=1, max_len=5001, seed=batch).check((8, True, 0, 0))
 
 
+@pytest.mark.parametrize("bits", [8, 4])
+@pytest.mark.parametrize("counts, positions", [([1] * 6, [0, 900, 31, 32, 300, 64]), ([0] * 20 + [19], [100 + i for i in range(20)] + [400])])
+def test_no_hints_and_no_more_tokens_than_sequences(tm, bits, counts, positions):
+    """Taken for a decoding step; right where it is none."""
+    Setup(tm, bits, 64, 2, counts, positions, q_heads=8, before=0, behind=0, seed=len(counts)).check((8, True, 0, 0))
+
+
 def _lengths(batch, longest, seed):
     rng = np.random.default_rng(seed)
     lengths = (40 + 200 * rng.random(batch)).astype(int)
