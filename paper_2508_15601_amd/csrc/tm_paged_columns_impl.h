@@ -220,9 +220,10 @@ __device__ __forceinline__ void paged_columns(const PagedPool& pool, const Paged
             const uint32_t ideal = max((all + ctas - 1) / ctas, kLeastQuads), loose = (all + kSegmentStart * segments) / ctas + kUnaligned;
             uint32_t p = ideal;
             while (p <= loose && wave_total(n * ((q + p - 1) / p)) > ctas) p += 1 + (p >> 4);
-            // up to sixteen pieces are merged in one level, and a second one costs more than a quad; three quads take no longer than a merge
+            // up to sixteen pieces are merged in one level, and a second one costs as much as three quads of 8-bit codes, two of 4-bit ones (one context of 8192, 8 heads, 8-bit: 16 pieces
+            // of four quads 11.8 us, 32 of two 13.8; of 16384, 4-bit: 16 of four 15.1, 32 of two 15.7); three quads take no longer than a merge
             const uint32_t longest = wave_greatest(q), single = (longest + kGroupPieces - 1) / kGroupPieces;
-            if (single <= p + 1) p = max(p, single);
+            if (single <= p + (BITS == 8 ? 3 : 2)) p = max(p, single);
             if (longest <= 3) p = max(p, longest);
             if (p <= loose) piece = p;
         }
