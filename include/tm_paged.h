@@ -27,8 +27,8 @@ extern "C" {
  *
  * The first rot_dim dimensions of a head form rot_dim / 2 pairs (x1, x2); at position p pair i becomes
  *     y1 = amplitude * (x1 cos(p f_i) - x2 sin(p f_i)),    y2 = amplitude * (x2 cos(p f_i) + x1 sin(p f_i)),
- * the other dimensions stay as they are.  Sines and cosines are right to 1e-11 at every int32 position, the result is rounded to fp32 and
- * then to fp16.
+ * the other dimensions stay as they are.  Sines and cosines are right to 1e-11 at every int32 position and for every f_i that is accepted (up to 1e6), the result is rounded to
+ * fp32 and then to fp16.
  */
 typedef enum tm_rope_layout {
     TM_ROPE_HALF = 0,         /* pair i = dimensions (i, i + rot_dim / 2) */
@@ -57,11 +57,11 @@ typedef struct tm_rope_params {
     double original_len;          /* > 0; TM_ROPE_WAVELENGTH and TM_ROPE_RAMP */
     double low, high;             /* 0 < low < high; the same two */
     double amplitude;             /* 0 = the scaling's own (1, or that of TM_ROPE_RAMP) */
-    const double* frequencies;    /* host, rot_dim / 2 radians per position; if not NULL these are the f_i and the scaling counts for nothing but
+    const double* frequencies;    /* host, rot_dim / 2 radians per position, -1e6 .. 1e6; if not NULL these are the f_i and the scaling counts for nothing but
                                      the amplitude */
 } tm_rope_params;
 
-typedef struct tm_rope tm_rope;   /* opaque; owns a table of rot_dim / 2 words on the device */
+typedef struct tm_rope tm_rope;   /* opaque; owns a table of rot_dim / 2 entries on the device */
 TM_API tm_rope* tm_rope_create(const tm_rope_params* params);       /* synchronous copy; NULL on error */
 TM_API void tm_rope_free(tm_rope* rope);
 /* The f_i (host, rot_dim / 2) and the amplitude (host) that the handle works with; either may be NULL. */

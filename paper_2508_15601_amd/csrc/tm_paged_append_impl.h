@@ -43,8 +43,8 @@ __device__ __forceinline__ void append_run(const PagedPool& pool, const PagedSeq
     if (rope.rot) {
         const int pairs = rope.rot / 2, at_once = 64 / pairs, tok = lane / pairs, p = lane - tok * pairs;      // tokens of a wave at a time
         if (tok < at_once) {
-            const uint64_t turns = rope.turns[p];
-            for (int u = u0 + (tid >> 6) * at_once + tok; u < u1; u += 4 * at_once) cs[u * (kHeadDim / 2) + p] = rope_angle(rope, job.run * kRun + u, turns);
+            const RopeTurn turn = rope.turns[p];
+            for (int u = u0 + (tid >> 6) * at_once + tok; u < u1; u += 4 * at_once) cs[u * (kHeadDim / 2) + p] = rope_angle(rope, job.run * kRun + u, turn);
         }
         __syncthreads();
     }

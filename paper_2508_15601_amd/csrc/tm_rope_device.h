@@ -1,7 +1,8 @@
 // Rotary positions on the device: angles without loss at any position, and the rotation of a pair.
 //
-// An angle pos * f is kept in turns, as a fraction of 2^64: F = f / 2 pi * 2^64 (mod 2^64), and pos * F (mod 2^64) is the angle less its whole
-// turns, exactly - the integer multiplication does the argument reduction that a floating-point sine has to do, for every int32 position.
+// An angle pos * f is kept in turns.  Of a frequency the whole turns a position are left out on the host and the rest F is held to 96 bits: pos * F less its whole turns is the
+// angle, and the integer multiplication, whose upper bits run over, does the argument reduction that a floating-point sine has to do.  At 2^31 an F of 64 bits would be
+// off by up to 7e-10 radians, this one by less than 1e-18: the product is kept to 2^-64 of a turn.
 // Sine and cosine are their power series on an eighth of a turn to either side of the nearest quarter (largest error 7e-12), in 64 bits: this
 // chip adds and multiplies 64-bit floats at the rate of 32-bit ones.  A rotated value is then the fp16 number next to the true one (as good as always),
 // which matters where it is quantised afterwards: an error of 2^-24 moves one code in about 3 million.
@@ -12,8 +13,13 @@ namespace tmw4 {
 
 constexpr int kRopeMaxPairs = 128;       // head dimensions up to 256
 
+struct RopeTurn {                        // a fraction of a turn
+    uint64_t high;                       // in units of 2^-64
+    uint32_t low;                        // and of 2^-96
+};
+
 struct RopePlan {
-    const uint64_t* turns;               // [rot / 2] F of every pair (device)
+    const RopeTurn* turns;               // [rot / 2] F of every pair (device)
     double amp;                          // factor of the rotated values
     int rot;                             // dimensions that are rotated, a multiple of 16
     int interleaved;                     // pairs are (2i, 2i + 1); otherwise (i, i + rot / 2)
@@ -23,9 +29,9 @@ struct CosSin {
     double c, s;
 };
 
-__device__ __forceinline__ CosSin rope_angle(const RopePlan& r, int pos, uint64_t turns)
+__device__ __forceinline__ CosSin rope_angle(const RopePlan& r, int pos, const RopeTurn& turn)
 {
-    const uint64_t phase = (uint64_t)(int64_t)pos * turns;
+    const uint64_t phase = (uint64_t)(int64_t)pos * turn.high + (uint64_t)(((int64_t)pos * (int64_t)turn.low) >> 32);
     const uint32_t quarter = (uint32_t)((phase + (1ull << 61)) >> 62) & 3u;           // nearest quarter turn
     const int64_t rest = (int64_t)(phase - ((uint64_t)quarter << 62));                // within 2^61 of it
     const double x = ((double)(int32_t)(rest >> 32) * 4294967296.0 + (double)(uint32_t)rest) * 0x1.921fb54442d18p-62;      // 2 pi / 2^64

@@ -1931,7 +1931,7 @@ struct tm_rope {
     int device, rot, interleaved;
     double amp;
     double f[kRopeMaxPairs];
-    uint64_t* turns;
+    RopeTurn* turns;
 };
 
 struct tm_paged_cache {
@@ -1943,6 +1943,32 @@ struct tm_paged_cache {
 
 static bool valid_rope(const tm_rope* r) { return r && r->magic == 0x746D5250u; }
 static bool valid_paged(const tm_paged_cache* c) { return c && c->magic == 0x746D5047u; }
+
+// f / 2 pi less its whole turns, to the nearest multiple of 2^-96.  f = m * 2^e with a whole m below 2^53, and 1 / 2 pi is held to 192 bits, so that the product is off by less than
+// f * 2^-192.
+static RopeTurn rope_turn(double f)
+{
+    static const uint64_t inv_two_pi[3] = {0x36d8a5664f10e410u, 0x7f09d5f47d4d3770u, 0x28be60db9391054au};       // in units of 2^-192, the lowest word first
+    int e;
+    const uint64_t m = (uint64_t)ldexp(frexp(fabs(f), &e), 53);
+    const int shift = 96 - (e - 53);                         // the product is in units of 2^(e - 53 - 192); at least 129 for f up to 2^20
+    uint64_t w[5] = {};
+    unsigned __int128 carry = 0;
+    for (int i = 0; i < 3; ++i) {
+        carry += (unsigned __int128)m * inv_two_pi[i];
+        w[i] = (uint64_t)carry;
+        carry >>= 64;
+    }
+    w[3] = (uint64_t)carry;
+    auto bits = [&](int at) {                                // 64 bits of the product, from bit `at` on
+        if (at >= 256) return uint64_t(0);
+        return at % 64 ? w[at / 64] >> at % 64 | w[at / 64 + 1] << (64 - at % 64) : w[at / 64];
+    };
+    unsigned __int128 turn = (unsigned __int128)(bits(shift + 64) & 0xffffffffu) << 64 | bits(shift);
+    turn += bits(shift - 1) & 1u;
+    if (f < 0.0) turn = -turn;
+    return RopeTurn{(uint64_t)(turn >> 32), (uint32_t)turn};
+}
 
 // The frequencies of the header's table; false if a parameter is out of range.
 static bool rope_frequencies(const tm_rope_params& p, double* f, double* amp)
@@ -2009,16 +2035,11 @@ tm_rope* tm_rope_create(const tm_rope_params* params)
     }
     r->rot = p.rot_dim;
     r->interleaved = p.layout == TM_ROPE_INTERLEAVED;
-    uint64_t turns[kRopeMaxPairs];
-    for (int i = 0; i < r->rot / 2; ++i) {
-        // the fraction of a turn per position in units of 2^-64 (extended precision: 64 bits of mantissa)
-        long double t = (long double)r->f[i] / 6.283185307179586476925286766559L;
-        t = ldexpl(t - floorl(t), 64);
-        turns[i] = t >= ldexpl(1.0L, 64) ? 0u : (uint64_t)t;
-    }
-    hipError_t e = hipMalloc((void**)&r->turns, sizeof(uint64_t) * (size_t)(r->rot / 2));
+    RopeTurn turns[kRopeMaxPairs] = {};
+    for (int i = 0; i < r->rot / 2; ++i) turns[i] = rope_turn(r->f[i]);
+    hipError_t e = hipMalloc((void**)&r->turns, sizeof(RopeTurn) * (size_t)(r->rot / 2));
     if (e == hipSuccess) {
-        e = hipMemcpy(r->turns, turns, sizeof(uint64_t) * (size_t)(r->rot / 2), hipMemcpyHostToDevice);
+        e = hipMemcpy(r->turns, turns, sizeof(RopeTurn) * (size_t)(r->rot / 2), hipMemcpyHostToDevice);
         if (e != hipSuccess) (void)hipFree(r->turns);
     }
     if (e != hipSuccess) {

@@ -105,6 +105,46 @@ def test_rope(tm, tokens, heads, dim, rot, layout):
     rope.close()
 
 
+def _near_quarters(pos, around, tries=4000):
+    """Frequencies near `around` whose angle at position `pos` is next to a whole number of quarter turns: (f, that number modulo 4, the angle beyond it), the next of the first `tries`."""
+    quarter = op._TWO_PI / 4
+    out = []
+    for f0 in around:
+        k0 = round(op.Fraction(pos) * op.Fraction(f0) / quarter)
+        best = None
+        for k in range(k0, k0 + tries):
+            f = float(k * quarter / pos)
+            rest = op.Fraction(pos) * op.Fraction(f) - k * quarter
+            if best is None or abs(rest) < abs(best[2]):
+                best = (f, k % 4, rest)
+        out.append(best)
+    return out
+
+
+@pytest.mark.parametrize("layout", list(LAYOUTS))
+@pytest.mark.parametrize("pos", [(1 << 31) - 1, -(1 << 31), (1 << 24) + 1, 131072])
+def test_rope_angles_at_the_ends_of_what_is_accepted(tm, pos, layout):
+    """Sines and cosines are right to 1e-11 at every int32 position and for every frequency up to the largest accepted one.  Next to a whole number of quarter turns one of
+    the two is next to zero, where fp16 resolves it: of a pair (16384, 0) it leaves 16384 times the angle beyond the quarters, which is known as a rational number."""
+    import torch
+    found = _near_quarters(pos, [1.0, 0.37, 3e-3, 2e-5, 2500.0, 31415.9, -0.73, 999000.0])
+    f = [x[0] for x in found]
+    _say(f"rope at {pos}: angles beyond the quarters {[float(x[2]) for x in found]}")
+    rope = tm.tm_rope_create(16, layout=LAYOUTS[layout], frequencies=f)
+    x = np.zeros((1, 1, 16), np.float16)
+    first = np.arange(8) * 2 if layout == "interleaved" else np.arange(8)
+    second = first + (1 if layout == "interleaved" else 8)
+    x[0, 0, first] = 16384.0
+    y = _host(tm.tm_rope_apply(_dev(x), _dev(np.array([pos], np.int32)), rope, torch.empty(1, 1, 16, dtype=torch.float16, device="cuda")))[0, 0]
+    # of the quarters 0 .. 3: (cos, sin) = (1, r), (-r, 1), (-1, -r), (r, -1) for a small rest r
+    small = np.array([(-1 if k in (1, 2) else 1) * 16384 * np.sin(float(r)) for _, k, r in found])
+    large = np.array([(-1 if k in (2, 3) else 1) * 16384 * np.cos(float(r)) for _, k, r in found])
+    odd = np.array([k % 2 for _, k, _ in found], bool)
+    got_small, got_large = np.where(odd, y[first], y[second]), np.where(odd, y[second], y[first])
+    assert _near(got_small, small, 16384e-11).all() and _near(got_large, large, 16384e-11).all(), (got_small, small)
+    rope.close()
+
+
 def test_rope_own_frequencies_and_special_values(tm):
     import torch
     f = np.array([0.0, 1.0, -0.25, 2 * np.pi, 3.0, 1e-9, 1e5, 0.5])
