@@ -37,7 +37,7 @@ __global__ __launch_bounds__(256 * TILES) __attribute__((amdgpu_waves_per_eu(BIT
 hipError_t launch_paged_columns(const PagedPool& pool, const PagedSeqs& seqs, const uint16_t* Q, long q_stride, uint16_t* O, int q_heads, float scale, int columns,
                                 int most_rows, int grid, bool alone, void* workspace, hipStream_t stream)
 {
-    static_assert(3 * kPagedMostWaves * sizeof(uint32_t) <= kPagedCounterBytes && 3 * kPagedMostCtas <= 3 * kPagedMostWaves, "three counters a wave or CTA");
+    static_assert(3 * kPagedMostWaves * sizeof(uint32_t) <= kPagedLengthAt && 3 * kPagedMostCtas <= 3 * kPagedMostWaves, "three counters a wave or CTA");
     static_assert(2 * kPagedMostCtas * (2 * 32 + 2 * 2048) * sizeof(float) <= kPagedColumnBytes, "two slots a CTA");
     static_assert(2 * kPagedMostWaves * (2 * 16 + 2048) * sizeof(float) <= kPagedColumnBytes, "two slots a wave");
     if (grid < 1 || grid > (alone ? kPagedMostWaves / 4 : kPagedMostCtas) || (alone && columns == 32)) return hipErrorInvalidValue;

@@ -5,8 +5,9 @@
 
 namespace tmw4 {
 
-// Workspace of tm_paged_attn: arrival counters, then partial results of contexts that are cut into pieces.
+// Workspace of tm_paged_attn: arrival counters and the length of a call's pieces, then partial results of contexts that are cut into pieces.
 constexpr size_t kPagedCounterBytes = 32 * 1024;
+constexpr size_t kPagedLengthAt = kPagedCounterBytes - 64;
 constexpr size_t kPagedColumnBytes = 23u << 20;           // two pieces each of 1408 waves
 constexpr size_t kPagedRowBytes = 33u << 20;              // 259 pieces of 256 rows
 constexpr size_t kPagedWorkspaceBytes = kPagedCounterBytes + kPagedColumnBytes + kPagedRowBytes;

@@ -24,6 +24,7 @@ struct RowsPlan {
     int least_rows;                      // sequences with fewer rows are not this launch's
     int target;                          // CTAs that fill the chip; 0: no context is cut
     uint32_t slots;                      // pieces of cut contexts at most, KV heads counted: the workspace and the grid have room for them
+    int32_t* length;                     // where the launch leaves the stages of a piece for the second kernel
 };
 
 constexpr int kLeastStages = 8;          // of 64 tokens: no piece is shorter, but for the last of a context
@@ -81,8 +82,9 @@ struct RowsWork {
     }
 };
 
-// Stages of a piece, every wave for itself and all alike.  Where tiles are many, the mean work of a compute unit, so that only what would outlast the others is cut.  Where they
-// are few, the length of least cost; a lane tries one, from half that mean to eight times it, the last lane no cut.  CTAs that fit the chip together take as long as the longest.
+// Stages of a piece, every wave for itself and all alike: those of one kernel, that is; another compilation of this arithmetic may round otherwise, so the second kernel reads the
+// number that the first one left.  Where tiles are many, the mean work of a compute unit, so that only what would outlast the others is cut.  Where they are few, the length of
+// least cost; a lane tries one, from half that mean to eight times it, the last lane no cut.  CTAs that fit the chip together take as long as the longest.
 // More of them take their work's share and what the last one sticks out, or in whole rounds if they are alike (their mean length near the longest).
 template <int RW>
 __device__ __forceinline__ int piece_stages(const RowsWork<RW>& w, int heads, const RowsPlan& plan, int lane)
@@ -134,7 +136,7 @@ __device__ __forceinline__ int piece_stages(const RowsWork<RW>& w, int heads, co
 }
 
 // Piece `unit` of the launch, or with MERGE row tile `unit` of those that are cut: its sequence, first row, context, pieces, and where its pieces' results go.  False: there
-// is none, or it has no row to write.
+// is none, or it has no row to write; the length of the pieces is set all the same.
 struct RowsTile {
     PagedSeq s;
     int b, row0, len, stages, pieces, piece, piece_stages;
@@ -145,7 +147,8 @@ __device__ __forceinline__ bool rows_tile(RowsTile& t, const PagedSeqs& seqs, in
 {
     constexpr int ROWS = 32 * RW;
     const RowsWork<RW> w(seqs, plan, G, lane);
-    const int P = piece_stages<RW>(w, heads, plan, lane);
+    const int P = MERGE ? constant_load(plan.length, 0) : piece_stages<RW>(w, heads, plan, lane);
+    t.piece_stages = P;
     auto units = [&](const RowsShape& r) {
         const uint32_t n = pieces_of(r.stages, P);
         return MERGE ? n > 1 ? r.tiles : 0u : r.tiles * n;
@@ -159,7 +162,6 @@ __device__ __forceinline__ bool rows_tile(RowsTile& t, const PagedSeqs& seqs, in
     const uint32_t most = pieces_of(r.stages, P), at = unit - base, tile = MERGE ? at : at / most;
     if (tile >= r.tiles) return false;
     t.piece = MERGE ? 0 : (int)(at - tile * most);
-    t.piece_stages = P;
     t.slot = 0;
     if (most > 1) {
         t.slot = wave_total(w.template sum<uint32_t>(t.b, [&](const RowsShape& o) { return o.stages > (uint32_t)P ? o.tiles * pieces_of(o.stages, P) : 0u; })) + tile * most;
@@ -181,7 +183,9 @@ __device__ __forceinline__ void paged_rows(const PagedPool& pool, const PagedSeq
     const uint32_t heads = (uint32_t)pool.heads, hk = block % heads;
     const int G = q_heads / pool.heads;
     RowsTile t;
-    if (!rows_tile<RW, false>(t, seqs, G, pool.heads, plan, block / heads, threadIdx.x & 63)) return;            // (uniform)
+    const bool any = rows_tile<RW, false>(t, seqs, G, pool.heads, plan, block / heads, threadIdx.x & 63);
+    if (block == 0 && threadIdx.x == 0) *plan.length = t.piece_stages;
+    if (!any) return;                                        // (uniform)
     const int first = t.piece * t.piece_stages;
     const int stages = t.piece == t.pieces - 1 ? t.stages - first : t.piece_stages;
     float* const part = t.pieces > 1 ? partial + ((size_t)(t.slot + t.piece) * heads + hk) * kPieceFloats<RW> : nullptr;
@@ -297,7 +301,8 @@ hipError_t launch(const PagedPool& pool, const PagedSeqs& seqs, const uint16_t* 
     constexpr int ROWS = 32 * RW;
     char* const space = (char*)workspace + kPagedCounterBytes;
     float* const partial = (float*)(space + kPagedColumnBytes);
-    const RowsPlan plan{f.least_rows, f.target, (uint32_t)std::min(kPagedRowBytes / (kPieceFloats<RW> * sizeof(float)), (size_t)f.target * 2)};
+    const RowsPlan plan{f.least_rows, f.target, (uint32_t)std::min(kPagedRowBytes / (kPieceFloats<RW> * sizeof(float)), (size_t)f.target * 2),
+                        (int32_t*)((char*)workspace + kPagedLengthAt)};
     const unsigned long tiles = (unsigned long)f.items * pool.heads, ctas = tiles + plan.slots, cut = std::min(tiles, (unsigned long)plan.slots / 2);
     const float s = scale * 1.4426950408889634f;
     if (ctas < 1 || ctas > 0x7ffff000UL) return hipErrorInvalidValue;
