@@ -9,8 +9,8 @@ namespace tmw4 {
 
 namespace {
 
-// A wave takes `per_wave` heads of one token: it works out the token's sines and cosines once (a lane a pair) and reads them back from LDS for every head.
-__global__ __launch_bounds__(256) void rope_kernel(const uint16_t* __restrict__ X, long x_stride, const int32_t* __restrict__ positions, RopePlan r,
+// A wave takes `per_wave` heads of one token: it works out the token's sines and cosines once (a lane a pair) and reads them back from LDS for every head.  X and Y may be the same.
+__global__ __launch_bounds__(256) void rope_kernel(const uint16_t* X, long x_stride, const int32_t* __restrict__ positions, RopePlan r,
                                                    uint16_t* Y, long y_stride, int tokens, int heads, int dim, int per_wave)
 {
     __shared__ CosSin cs[4][kRopeMaxPairs];
