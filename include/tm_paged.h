@@ -143,6 +143,11 @@ TM_API int tm_paged_attn(const uint16_t* Q, int64_t q_stride, const tm_paged_cac
  * them at a time (8, 16 or 32; 0 = no such launch), the others in CTAs of *rows rows (128 or 256; 0 = no such launch), their contexts in up to *pieces.
  */
 TM_API int tm_get_paged_plan(const tm_paged_cache* cache, const tm_paged_batch* batch, int q_heads, int* columns, int* column_rows, int* rows, int* pieces);
+/*
+ * Further: *launches of a call, *column_ctas, the CTAs that take the columns (0 = none do), and *alone, 1 if every wave of them works by itself.  Columns and rows of a call go in
+ * one launch, the rows' pieces are put together in another.
+ */
+TM_API int tm_get_paged_form(const tm_paged_cache* cache, const tm_paged_batch* batch, int q_heads, int* launches, int* column_ctas, int* alone);
 
 #ifdef __cplusplus
 }

@@ -9,5 +9,5 @@ from .binding import (  # noqa: F401
     tm_gemm_workspace_bytes, tm_reset_workspace, tm_get_plan, tm_last_error, tm_pack_w4, tm_pack_w4_actorder, tm_pack_w4_layout, tm_pack_w8, tm_pack_w8_fp8, tm_packed_raw, tm_set_variant, tm_set_launch, tm_unpack_w4,
     tm_variant_name, tm_version,
     PagedBatch, PagedCache, Rope, TM_ROPE_BASE, TM_ROPE_HALF, TM_ROPE_INTERLEAVED, TM_ROPE_LINEAR, TM_ROPE_PLAIN, TM_ROPE_RAMP, TM_ROPE_WAVELENGTH,
-    tm_get_paged_plan, tm_paged_append, tm_paged_attn, tm_paged_create, tm_paged_pool, tm_paged_read, tm_paged_workspace, tm_rope_apply, tm_rope_create, tm_rope_frequencies,
+    tm_get_paged_form, tm_get_paged_plan, tm_paged_append, tm_paged_attn, tm_paged_create, tm_paged_pool, tm_paged_read, tm_paged_workspace, tm_rope_apply, tm_rope_create, tm_rope_frequencies,
 )

@@ -756,3 +756,8 @@ def tm_paged_attn(Q, cache: PagedCache, batch: PagedBatch, O, scale: float, stre
 def tm_get_paged_plan(cache: PagedCache, batch: PagedBatch, tokens: int, q_heads: int):
     """(columns, column_rows, rows, pieces) of such a tm_paged_attn call, see include/tm_paged.h."""
     return (_calls or _native()).paged_plan(cache, batch, tokens, q_heads)
+
+
+def tm_get_paged_form(cache: PagedCache, batch: PagedBatch, tokens: int, q_heads: int):
+    """(launches, column_ctas, alone) of such a tm_paged_attn call, see include/tm_paged.h."""
+    return (_calls or _native()).paged_form(cache, batch, tokens, q_heads)

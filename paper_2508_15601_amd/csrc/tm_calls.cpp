@@ -493,6 +493,20 @@ PyObject* paged_plan(PyObject*, PyObject* const* a, Py_ssize_t n)    // cache, b
     return Py_BuildValue("(iiii)", v[0], v[1], v[2], v[3]);
 }
 
+PyObject* paged_form(PyObject*, PyObject* const* a, Py_ssize_t n)    // cache, batch, tokens, q_heads -> (launches, column_ctas, alone)
+{
+    int v[3] = {0, 0, 0};
+    PyObject* none = entry(n, 4, Py_None, [&] {
+        const Sequences seqs(a[1], as_int(a[2]));
+        const auto* h = (const tm_paged_cache*)handle_of(a[0], kPagedFreed);
+        const int q_heads = Sequences::whole(as_int(a[3]), "q_heads");
+        call([&] { return tm_get_paged_form(h, &seqs.b, q_heads, &v[0], &v[1], &v[2]); });
+    });
+    if (!none) return nullptr;
+    Py_DECREF(none);
+    return Py_BuildValue("(iiN)", v[0], v[1], PyBool_FromLong(v[2]));
+}
+
 PyObject* set_error(PyObject*, PyObject* type)
 {
     Py_INCREF(type);
@@ -520,6 +534,7 @@ PyMethodDef g_methods[] = {fast<gemm>("gemm"),
                            fast<paged_read>("paged_read"),
                            fast<paged_attn>("paged_attn"),
                            fast<paged_plan>("paged_plan"),
+                           fast<paged_form>("paged_form"),
                            {"set_error", set_error, METH_O, nullptr},
                            {nullptr, nullptr, 0, nullptr}};
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "tm_calls", nullptr, -1, g_methods, nullptr, nullptr, nullptr, nullptr};

@@ -2267,4 +2267,16 @@ int tm_get_paged_plan(const tm_paged_cache* cache, const tm_paged_batch* batch, 
     return TM_OK;
 }
 
+int tm_get_paged_form(const tm_paged_cache* cache, const tm_paged_batch* batch, int q_heads, int* launches, int* column_ctas, int* alone)
+{
+    PagedSeqs seqs;
+    const int rc = check_paged_attn(cache, batch, q_heads, &seqs);
+    if (rc != TM_OK) return rc;
+    const PagedForm f = paged_form(cache->pool, seqs, q_heads, batch->max_count, batch->max_len, g_dev[cache->device].num_cu);
+    if (launches) *launches = (f.row_waves ? f.target ? 2 : 1 : 0) + (f.column_rows && !f.together ? 1 : 0);
+    if (column_ctas) *column_ctas = f.column_rows ? f.column_ctas : 0;
+    if (alone) *alone = f.column_rows && (f.alone || f.together);
+    return TM_OK;
+}
+
 }  // extern "C"
