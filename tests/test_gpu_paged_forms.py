@@ -57,6 +57,25 @@ def test_rows_and_columns(tm, bits):  # noqa: F811
     s.check((True, True, True, 1))
 
 
+def test_widest_tables(tm):  # noqa: F811
+    """The bound on the work of a call that tm_paged.h states: tables of 2^28 tokens for 64 decoding sequences of 8 KV heads and 4 query heads each, and no wider ones."""
+    import torch
+    cache = tm.tm_paged_create(*tm.tm_paged_pool(2, 8, 1024, 8))
+    offsets, positions = torch.arange(65, dtype=torch.int32, device="cuda"), torch.arange(64, dtype=torch.int32, device="cuda")
+    Q = torch.randn(64, 32, 128, device="cuda").half()
+    for columns in (1 << 18, 1 << 19):
+        batch = tm.PagedBatch(torch.full((64, columns), -1, dtype=torch.int32, device="cuda"), offsets, positions)
+        O = torch.full_like(Q, 7.0)
+        if columns == 1 << 18:
+            tm.tm_paged_attn(Q, cache, batch, O, SCALE)
+            assert (O == 0).all()                                          # no page of theirs is there
+        else:
+            for call in (lambda: tm.tm_paged_attn(Q, cache, batch, O, SCALE), lambda: tm.tm_get_paged_plan(cache, batch, 64, 32), lambda: tm.tm_get_paged_form(cache, batch, 64, 32)):
+                with pytest.raises(tm.TmError, match="too much work"):
+                    call()
+            assert (O == 7).all()
+
+
 def test_refusals(tm):  # noqa: F811
     s = Setup(tm, 8, 32, 2, [4], [0], q_heads=4)
     with pytest.raises(tm.TmError, match="q_heads"):
