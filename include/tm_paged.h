@@ -133,6 +133,8 @@ TM_API int tm_paged_read(const tm_paged_cache* cache, const tm_paged_batch* batc
  *     O = softmax(scale * K^ q) V^,   query head h with KV head h / (q_heads / kv_heads),   q_heads = 1 .. 128 times kv_heads.
  * Tokens on pages that the pool does not have are not attended over; a row that is left with none gets O = 0.  Rows whose position lies outside
  * [0, max_pages * page_tokens) are left untouched.  One token a sequence is a decoding step, a few are drafted tokens to be verified, hundreds a prompt; a call takes any mix.
+ * As by tm_attn_decode and tm_attn_prefill, each probability (relative to about the largest) times its value's scale is rounded to fp16, by at most 2^-11 of it or 2^-25; everything else is
+ * held in fp32 up to the result's own rounding.
  * Work is counted in 32 bits, so a call must have less than 2^30 rows (tokens * q_heads / kv_heads), and (rows / 8 + batch) * kv_heads times (max_pages * page_tokens / 128 + 1)
  * must stay below 2^31: 64 decoding sequences of 8 KV heads and 4 query heads each take tables of up to 2^28 tokens.  Others are refused, whatever the lengths.
  * Never allocates.  Partial results go through the cache's workspace.  Results are bit-identical from run to run (same arguments and hints).

@@ -117,3 +117,37 @@ def test_serving_steps_store_what_the_contiguous_cache_does(tm, bits):  # noqa: 
         at += n
         past += n
     slab.close()
+
+
+@pytest.mark.parametrize("bits", [8, 4])
+@pytest.mark.parametrize("counts, positions", [([1, 1], [600, 40]), ([100], [200])])
+@pytest.mark.parametrize("size", [1e-2, 1e-4])
+def test_values_next_to_fp16s_smallest(tm, bits, counts, positions, size):  # noqa: F811
+    """Values so small that a probability times a value's scale is no normal fp16 number: its rounding is then off by 2^-25 and not by 2^-11 of it.  A value meets it (q - z) times, and the
+    denominator is at least the sum of the probabilities relative to the largest.  Sums that carry the codes' bias add 24 steps of 2^-24 of up to 1279 scales, as where V^ is 0."""
+    import torch
+    s = Setup(tm, bits, 32, 1, counts, positions, q_heads=4, seed=11)
+    total = int(s.positions[0]) + counts[0] + (s.positions[1] + counts[1] if len(counts) > 1 else 0)
+    lens = [n + p for n, p in zip(counts, positions)]
+    fill = tm.PagedBatch(s.batch.table, _dev(np.cumsum([0] + lens).astype(np.int32)), torch.zeros(len(counts), dtype=torch.int32, device="cuda"))
+    g = torch.Generator(device="cuda")
+    g.manual_seed(12)
+    K, V = (torch.randn(total, 1, 128, generator=g, device="cuda") for _ in range(2))
+    tm.tm_paged_append(s.cache, fill, K.half(), (V * size).half())
+    O = _host(s.run()).astype(np.float64)
+    want, A = s.want()
+    arrays = op.unpack_pool(_host(s.k), _host(s.v), _host(s.pairs))
+    Q = _host(s.Q).astype(np.float64)
+    for b, (n, p) in enumerate(zip(counts, positions)):
+        Kb, _, ok = op.gather(arrays, s.table[b], p + n)
+        assert ok.all()
+        t = np.arange(p + n)
+        page, slot = s.table[b, t // s.page], t % s.page
+        steps = np.abs(arrays[3][page, 0, slot].astype(np.float64) - arrays[5][page, 0, slot].astype(np.float64)[:, None])          # |q - z| [tokens][128]
+        scale = arrays[4][page, 0, slot].astype(np.float64).max()
+        for i in range(n):
+            row = int(s.offsets[b]) + i
+            x = Kb[:p + i + 1, 0] @ Q[row].T * SCALE                       # [tokens][heads]
+            L = np.exp(x - x.max(0)).sum(0)
+            bound = 1.125 * 2.0 ** -11 * (np.abs(want[row]) + A[row]) + 2.0 ** -25 * steps[:p + i + 1].sum(0)[None] / L[:, None] + 24 * 2.0 ** -24 * 1279 * scale + 2.0 ** -25
+            assert (np.abs(O[row] - want[row]) <= bound).all(), (b, i)
