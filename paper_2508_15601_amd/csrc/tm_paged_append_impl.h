@@ -250,7 +250,7 @@ __global__ __launch_bounds__(256) void paged_append_tokens_kernel(PagedPool pool
 }  // namespace
 
 hipError_t launch_paged_append(const PagedPool& pool, const PagedSeqs& seqs, PagedRows k, PagedRows v, const RopePlan* rope, PagedRows q, uint16_t* q_out,
-                               long q_out_stride, int q_heads, int max_count, hipStream_t stream)
+                               long q_out_stride, int q_heads, int max_count, int num_cu, hipStream_t stream)
 {
     const RopePlan plan = rope ? *rope : RopePlan{nullptr, 1.0, 0, 0};
     // Measured (32 / 8 heads, 8-bit, queries too), in brackets by runs: one token each of 1, 16, 64 and 256 sequences 3.7, 4.0, 4.0 and 5.3 us (5.2, 5.4, 7.2, 19.5); five each of
@@ -263,10 +263,13 @@ hipError_t launch_paged_append(const PagedPool& pool, const PagedSeqs& seqs, Pag
         hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(256), 0, stream, pool, seqs, k, v, plan, q, q_out, q_out_stride, heads, per_token, max_count);
         return hipGetLastError();
     }
-    // KV heads a CTA: they share a run's sines and cosines, but take their turns.  One, two and four of them, 8 heads, 8-bit: 4 x 2000 tokens with queries 47.6 / 45.2 / 42.0 us, without
-    // 24.5 / 22.3 / 24.1, not turned 14.8 / 14.3 / 16.5; 512 tokens with queries 7.4 / 10.0 / 15.4.  Queries fill the chip beside fewer CTAs.
-    const long each = most_runs(seqs) * pool.heads;
-    const int kv_heads = std::min(!plan.rot ? 1 : q.p ? each >= 880 ? 4 : each >= 440 ? 2 : 1 : each >= 1000 ? 2 : 1, pool.heads);
+    // KV heads a CTA: they share a run's sines and cosines, but take their turns, so that only pays where a compute unit has more CTAs than it holds at a time.  By runs x heads (us; one, two
+    // and four heads a CTA; 8 / 32 heads 8-bit, then 4 / 28 heads 4-bit).  Queries too, which fill the chip beside fewer CTAs: 128 11.2 / 13.7 / 19.8, 11.8 / 14.2 / 19.7; 280 14.2 / 15.7 / 21,
+    // 20.0 / 18.0 / 22.4; 400 18.4 / 17.6 / 22.5, 26.2 / 24.8 / 24.5; 650 28.3 / 25.1 / 26.3, 35.0 / 33.0 / 33.0; 744 31.6 / 28.0 / 26.6, 41.5 / 35.4 / 35.3; 944 37.9 / 34.0 / 32.0, 49.2 / 44.8 /
+    // 43.3; 2100 69 / 67 / 63, 94 / 90 / 86.  Keys turned and no queries (three CTAs a compute unit): 496 15.3 / 16.0 / 21, 15.1 / 15.5 / 20; 744 19.1 / 19.0 / 22, 18.6 / 18.4 / 22; 816 21.2 /
+    // 19.6 / 23, 20.8 / 18.6 / 22; 1600 29.2 / 28.8 / 29.3, 28.9 / 27.2 / 28.2.  Not turned one and two are within 5 % of each other.
+    const double each = (double)most_runs(seqs) * pool.heads / num_cu;
+    const int kv_heads = std::min(!plan.rot ? 1 : q.p ? each >= 2.75 ? 4 : each >= 1.2 ? 2 : 1 : each >= 3.0 ? 2 : 1, pool.heads);
     const long kv = most_runs(seqs) * ((pool.heads + kv_heads - 1) / kv_heads);
     const int per_wave = (long)seqs.tokens * q_heads >= 16384L * 8 ? q_heads : 8;
     const long jobs = q.p ? (long)seqs.tokens * ((q_heads + per_wave - 1) / per_wave) : 0, blocks = kv + (jobs + 3) / 4;

@@ -31,7 +31,7 @@ hipError_t launch_rope(const uint16_t* X, long x_stride, const int32_t* position
                        int dim, hipStream_t stream);
 // q.p == nullptr: keys and values only; rope == nullptr: stored as they are
 hipError_t launch_paged_append(const PagedPool& pool, const PagedSeqs& seqs, PagedRows k, PagedRows v, const RopePlan* rope, PagedRows q, uint16_t* q_out,
-                               long q_out_stride, int q_heads, int max_count, hipStream_t stream);
+                               long q_out_stride, int q_heads, int max_count, int num_cu, hipStream_t stream);
 hipError_t launch_paged_read(const PagedPool& pool, const PagedSeqs& seqs, uint16_t* K, uint16_t* V, hipStream_t stream);
 // The new tokens of sequences with up to most_rows (token, query head of a KV head) rows; `columns` of them at a time, 8, 16 or 32.  Every CTA of `grid`, or every wave (alone; not
 // with 32 columns), takes an equal piece of the work.

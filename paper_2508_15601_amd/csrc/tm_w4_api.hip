@@ -2202,7 +2202,7 @@ int tm_paged_append(tm_paged_cache* cache, const tm_paged_batch* batch, const ui
     RopePlan plan{};
     if (rope) plan = rope_plan(rope);
     const hipError_t e = launch_paged_append(cache->pool, seqs, PagedRows{K, (long)k_stride}, PagedRows{V, (long)v_stride}, rope ? &plan : nullptr,
-                                             PagedRows{Q, (long)q_stride}, Q_out, (long)q_out_stride, q_heads, batch->max_count, (hipStream_t)stream);
+                                             PagedRows{Q, (long)q_stride}, Q_out, (long)q_out_stride, q_heads, batch->max_count, g_dev[dev].num_cu, (hipStream_t)stream);
     if (e != hipSuccess) return fail_hip(e, "paged append launch");
     return TM_OK;
 }
