@@ -88,8 +88,9 @@ __device__ __forceinline__ void attn_rows(const RowsJob& job, const uint8_t* kco
     };
     constexpr int kChunks = BITS == 8 ? 256 : 128;                                  // of 16 bytes a run
     const int mine = (BITS == 8 ? wave >> 2 : wave >> 1) & 1;
-    // Entries of the table for 64 pages at a time, a lane each: one wait for the table in 64 pages.  Loading the entry of a run when its turn comes made all
-    // waves stand still twice a stage.
+    // Entries of the table for 64 pages at a time, a lane each; loading the entry of a run when its turn comes made all waves stand still twice a stage.  They still do once: in the
+    // generated code every stage waits for all of its wave's loads in front of the two reads of `ids`, the codes and pairs that it has just requested among them, since one path
+    // to there has loaded `ids` and the compiler keeps one account for all.
     int ids = -1, ids_at = -64;                            // of pages ids_at .. ids_at + 63 of the sequence
     auto runs_of = [&](int st) {
         StageRuns r{{-1, -1}};
@@ -351,7 +352,8 @@ __device__ __forceinline__ void attn_rows(const RowsJob& job, const uint8_t* kco
                 const bool there = is_there(st_n, sub_n);
                 if constexpr (PAGED) {
                     // A row that has met no token yet, all its pages so far being none of the pool's, takes its reference from these scores as from the first ones: a move
-                    // up from the lowest reference would leave nothing of them.  (Its sums are still zero.)
+                    // up from the lowest reference would leave nothing of them.  (Its sums are still zero.  The branch parts the scaling below from the products with V, beside which
+                    // it runs in the kernel of the contiguous cache.)
                     const bool fresh = m_run == kMaskFloor && len > t_n;
                     if (__any(fresh)) {
                         scale_scores(s, 0.f, true, t_n, there);

@@ -14,9 +14,9 @@
 //   - A block is one run of 32 tokens (8-bit codes) or two (4-bit); every run has its own address, from a page number that is requested three blocks ahead.  A run on a
 //     page that the pool does not have is not read and its tokens are masked.
 //
-// Measured (32 / 8 heads unless said): 32 sequences of 8192 tokens, 8-bit 84 us (6.5 TB/s), 4-bit 52 us (5.4 TB/s); 4 of 60000 down to 30000, 64 / 8 heads, 8-bit 63 us (6.0 TB/s); 64
-// skewed ones up to 16384, 4-bit 57 us (5.2 TB/s); one of 2048, 8-bit 8.9 us; 12 x 5 drafted tokens after 3000 to 6000, 40 / 8 heads, 8-bit 36 us (3.3 TB/s).  Long contexts are bound by
-// memory (a large copy reaches 5.2 TB/s, both ways together); short ones by a launch, a plan, a chain of three round trips to memory (lengths, page numbers, blocks) and the
+// Measured (32 / 8 heads unless said): 32 sequences of 4096 to 8192 tokens, 8-bit 71 us (5.9 TB/s), 4-bit 45 us (4.7 TB/s); 4 of 60000 down to 30000, 64 / 8 heads, 8-bit 63 us (6.0 TB/s); 64
+// skewed ones up to 16384, 4-bit 56 us (5.2 TB/s); one of 2048, 8-bit 8.8 us; 12 x 5 drafted tokens after 3000 to 6000, 40 / 8 heads, 8-bit 34 us (3.4 TB/s), 4-bit 27; 32 x 5 after 4000 to
+// 8000, 32 / 8 heads, 91 and 68.  Long contexts are bound by memory (a large copy reaches 5.2 TB/s, both ways together); short ones by a launch, a plan, a chain of three round trips to memory (lengths, page numbers, blocks) and the
 // meeting of the pieces, 8 us together; tiles of 32 columns by instruction issue, the codes being converted for each half.
 #include "tm_paged_columns_impl.h"
 

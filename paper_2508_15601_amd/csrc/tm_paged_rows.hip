@@ -8,8 +8,9 @@
 //     the pieces are every CTA works out by itself from the sequences' lengths (piece_stages), which the host does not know.  A second kernel puts a row's pieces together in
 //     their order, so results do not depend on which is done first.
 //
-// Measured (32 / 8 heads): prompts of 6000, 5000, 4000 and 3000 tokens, 8-bit: 862 us (0.82 PFLOP/s); 512 tokens after 30000, 4-bit: 313 us (0.81 PFLOP/s), 1024 without pieces; 100
-// after 8000, 8-bit: 45 us, 259 without pieces.  What bounds it is the issue of vector and matrix instructions (tm_attn_prefill.hip); a piece of 256 rows leaves 133 KB in memory.
+// Measured (32 / 8 heads): prompts of 6000, 5000, 4000 and 3000 tokens, 8-bit: 860 us (0.82 PFLOP/s), 4-bit 853; 512 tokens after 30000, 4-bit: 297 us (0.85 PFLOP/s), 1024 without
+// pieces; 100 after 8000, 8-bit: 42 us, 259 without pieces; one prompt of 4000: 163.  (Calls in a row; after an idle time, until the clock is up, a sixth more.)  What bounds it is the issue of
+// vector and matrix instructions (tm_attn_prefill.hip) and a wait for memory in every stage (tm_attn_rows_impl.h); a piece of 256 rows leaves 133 KB in memory.
 #include "tm_attn_rows_impl.h"
 #include "tm_paged_columns_impl.h"
 #include "tm_paged_host.h"
@@ -344,9 +345,11 @@ hipError_t paged_rows_setup()
 // 8-bit codes take the memory's time sooner: 256 of 300 / 1000 31 / 86 (48 / 98), 128 of 1000 43 (50), but 64 of 1000 26.9 (25.0), 256 skewed ones up to 9000 212 (200), 64 skewed 97 (87),
 // 256 x 5 after 1000, whose segments need two column tiles, 183 (152): from four segments a compute unit on.  Below that two CTAs a compute unit hide each other's starts if contexts are
 // short: 48 of 300 10.2 us (13.0 with one), 64 of 500 14.2 (15.3), 64 of 2000 42.8 (45), but 40 of 2000 to 4000 50 (45).
-// Both in one call go in one launch, the columns' CTAs (eight waves) first, on half the compute units, or 11 / 16 where row tiles are few (64 decoding at up to 4000 and a chunk of 512 at
-// 4000, 8-bit: 146 us, 154 with 11 / 16, 160 in two launches; 40 decoding and chunks of 1500 and 750: 141, 147, 161; 128 at 1000 and 512 at 2000: 99, 105, 117; 200 at 2000 and a prompt
-// of 256: 157, 143, 147; 300 at 300 and one of 64: 45, 40, 47).  Behind the row tiles the columns' long pieces stick out: 144, 151, 107, 149, 42; on all compute units first 157, 160, 113, 149, 42.
+// Both in one call go in one launch, the columns' CTAs (eight waves) first, on half the compute units, or 11 / 16 where row tiles are few.  With half, 11 / 16 and in two launches (us; 8-bit, then
+// 4-bit; contexts from half of the length given): 40 decoding at 4000 and chunks of 1500 and 750 122, 130, 141 and 113, 122, 131; 64 at 4000 and a chunk of 512 at 4000 116, 136, 141 and 113, 108,
+// 118; 128 at 1000 and 512 at 2000 86, 93, 104 and 78, 82, 92; 200 at 2000 and a prompt of 256, where the rule takes 11 / 16, 147, 133, 137 and 90, 80, 90.  Short contexts beside tiles of 128 rows
+// it does not tell apart, and takes half: 60 at 500 and 400 at 500 23, 30 and 24, 29, but 300 at 300 and a prompt of 64 46, 41, 48 and 37, 31, 43.  Behind the row tiles the columns' long
+// pieces stick out: 2 to 8 % more than with half in the first three; on all compute units first 10 to 14 %.
 // 128 or 256 rows a CTA: a stage of 128 costs 0.66 of one of 256 (the four prompts above: 1154 against 867 us).  So 256, unless the chip does not fill with either and pieces cannot
 // make up for it, a context being short (two prompts of 307 and 161 tokens, 2 / 1 heads: 19 against 20 us; 400 and 150, 16 / 1: 34 against 39).  Over 57 random calls (one chunk after
 // up to 40000 tokens, up to six prompts, up to 30 decoding sequences with chunks; 1 to 8 KV heads, 1 to 16 query heads each) the rule's choice takes 1.02 of the better one's time,

@@ -1,6 +1,6 @@
 // Rotary positions of packed tokens (tm_rope_apply).
 //
-// Bound by memory: 8192 tokens, 32 heads of 128, 64 of them turned: 29.5 us with nothing in the caches, 134 MB at 4.6 TB/s (22 us from the last-level cache); 16 tokens 3.4 us, an
+// Bound by memory: 8192 tokens, 32 heads of 128, 64 of them turned: 29.5 us with nothing in the caches, 134 MB at 4.6 TB/s (22 us from the last-level cache); 16 tokens 4 us, an
 // empty launch and two round trips.  Requesting two or four rounds of a wave's vectors ahead changed nothing.
 #include "tm_rope_device.h"
 #include "tm_paged_host.h"
