@@ -96,7 +96,8 @@ TM_API void tm_paged_free(tm_paged_cache* cache);
  * The sequences of a call.  New tokens are packed: rows offsets[b] .. offsets[b+1] - 1 of the token arrays belong to sequence b (offsets ascending, clamped to
  * [0, tokens]; rows outside them are not touched), row offsets[b] + i is the token at position positions[b] + i of its sequence.  Token t of sequence b lies in
  * page table[b][t / page_tokens]; an entry outside [0, pages) names no page, and what would lie there is not stored, not attended over and reads as zeros.
- * Everything marked device is read when the work runs, so a captured graph follows what the arrays hold at its replay.
+ * Everything marked device is read when the work runs, so a captured graph follows what the arrays hold at its replay.  A call that would take a launch of 2^32 threads or more is
+ * refused: 256 for every 32 tokens and KV head that are stored or read, 512 for every 256 rows (or 128) of a KV head that attend, parts of a sequence counted whole.
  */
 typedef struct tm_paged_batch {
     const int32_t* table;         /* device [batch][max_pages] */

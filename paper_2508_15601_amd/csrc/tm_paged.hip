@@ -84,7 +84,7 @@ __global__ __launch_bounds__(256) void paged_read_kernel(PagedPool pool, PagedSe
 hipError_t launch_paged_read(const PagedPool& pool, const PagedSeqs& seqs, uint16_t* K, uint16_t* V, hipStream_t stream)
 {
     const long blocks = most_runs(seqs) * pool.heads;
-    if (blocks <= 0 || blocks > 0x7fffffffL) return hipErrorInvalidValue;
+    if (blocks <= 0 || blocks > most_ctas(256)) return hipErrorInvalidConfiguration;
     const auto kernel = pool.bits == 8 ? paged_read_kernel<8> : paged_read_kernel<4>;
     hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(256), 0, stream, pool, seqs, K, V);
     return hipGetLastError();

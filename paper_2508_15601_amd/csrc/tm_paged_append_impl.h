@@ -257,7 +257,7 @@ hipError_t launch_paged_append(const PagedPool& pool, const PagedSeqs& seqs, Pag
     // 12, 64 and 256 sequences 4.1, 6.4 and 14.4 us (5.5, 7.9, 27.6), eight 4.4, 7.9 and 20.1 (5.8, 8.5, 31.2).  Beyond that runs, whose tokens share their way to the page;
     // with 4-bit codes from two tokens on (with atomic operations on the shared bytes 64 sequences of five took 11.9 us, by runs 7.8).
     const int heads = q.p ? q_heads : 0, per_token = (2 * pool.heads + heads + 3) / 4;
-    if (max_count >= 1 && max_count <= (pool.bits == 8 ? kFewTokens<8> : kFewTokens<4>) && (long)seqs.batch * max_count * per_token < 0xfffffff0L) {
+    if (max_count >= 1 && max_count <= (pool.bits == 8 ? kFewTokens<8> : kFewTokens<4>) && (long)seqs.batch * max_count * per_token <= 4 * most_ctas(256)) {
         const long blocks = ((long)seqs.batch * max_count * per_token + 3) / 4;
         const auto kernel = pool.bits == 8 ? paged_append_tokens_kernel<8> : paged_append_tokens_kernel<4>;
         hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(256), 0, stream, pool, seqs, k, v, plan, q, q_out, q_out_stride, heads, per_token, max_count);
@@ -273,7 +273,7 @@ hipError_t launch_paged_append(const PagedPool& pool, const PagedSeqs& seqs, Pag
     const long kv = most_runs(seqs) * ((pool.heads + kv_heads - 1) / kv_heads);
     const int per_wave = (long)seqs.tokens * q_heads >= 16384L * 8 ? q_heads : 8;
     const long jobs = q.p ? (long)seqs.tokens * ((q_heads + per_wave - 1) / per_wave) : 0, blocks = kv + (jobs + 3) / 4;
-    if (blocks <= 0 || blocks > 0x7fffffffL) return hipErrorInvalidValue;
+    if (blocks <= 0 || blocks > most_ctas(256)) return hipErrorInvalidConfiguration;
     const auto kernel = pool.bits == 8 ? paged_append_kernel<8> : paged_append_kernel<4>;
     hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(256), 0, stream, pool, seqs, k, v, plan, (unsigned)kv, kv_heads, q, q_out, q_out_stride, q_heads, per_wave);
     return hipGetLastError();

@@ -15,6 +15,9 @@ constexpr size_t kPagedWorkspaceBytes = kPagedCounterBytes + kPagedColumnBytes +
 constexpr int kPagedMostCtas = 512;      // of a launch whose CTAs share contexts
 constexpr int kPagedMostWaves = 1408;    // of one whose waves do
 
+// CTAs that a launch may have at most: its threads are counted in 32 bits.
+constexpr long most_ctas(int threads) { return 0xffffffffL / threads; }
+
 struct PagedRows {                       // a packed array of new tokens: row r at p + r * stride
     const uint16_t* p;
     long stride;

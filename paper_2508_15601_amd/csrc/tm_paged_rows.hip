@@ -306,7 +306,7 @@ hipError_t launch(const PagedPool& pool, const PagedSeqs& seqs, const uint16_t* 
                         (int32_t*)((char*)workspace + kPagedLengthAt)};
     const unsigned long tiles = (unsigned long)f.items * pool.heads, ctas = tiles + plan.slots, cut = std::min(tiles, (unsigned long)plan.slots / 2);
     const float s = scale * 1.4426950408889634f;
-    if (ctas < 1 || ctas > 0x7ffff000UL) return hipErrorInvalidValue;
+    if (ctas < 1 || ctas + kPagedMostCtas > (unsigned long)most_ctas(512)) return hipErrorInvalidConfiguration;
     if (f.together) {
         const ColumnsPart few{f.column_rows, (uint32_t)f.column_ctas, (float*)space, (uint32_t*)workspace};
         auto pick = [&](auto parts) {

@@ -5,6 +5,8 @@
 #include "tm_rope_device.h"
 #include "tm_paged_host.h"
 
+#include <algorithm>
+
 namespace tmw4 {
 
 namespace {
@@ -33,10 +35,15 @@ hipError_t launch_rope(const uint16_t* X, long x_stride, const int32_t* position
     // one round of a wave's lanes at a time where tokens are few
     const int round = 64 / ((dim + 15) / 16);
     const int per_wave = (long)tokens * heads >= 16384L * round ? heads : round;
-    const long jobs = (long)tokens * ((heads + per_wave - 1) / per_wave);
-    if (jobs <= 0 || jobs > 4 * 0x7fffffffL) return hipErrorInvalidValue;
-    hipLaunchKernelGGL(rope_kernel, dim3((unsigned)((jobs + 3) / 4)), dim3(256), 0, stream, X, x_stride, positions, r, Y, y_stride, tokens, heads, dim, per_wave);
-    return hipGetLastError();
+    const long parts = (heads + per_wave - 1) / per_wave, most = 4 * most_ctas(256) / parts;       // tokens of a launch
+    for (long t = 0; t < tokens; t += most) {
+        const int n = (int)std::min(most, tokens - t);
+        hipLaunchKernelGGL(rope_kernel, dim3((unsigned)((n * parts + 3) / 4)), dim3(256), 0, stream, X + t * x_stride, x_stride, positions + t, r, Y + t * y_stride, y_stride, n, heads,
+                           dim, per_wave);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
 }
 
 }  // namespace tmw4

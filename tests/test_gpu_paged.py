@@ -145,6 +145,27 @@ def test_rope_angles_at_the_ends_of_what_is_accepted(tm, pos, layout):
     rope.close()
 
 
+def test_rope_of_more_tokens_than_a_launch_takes(tm):
+    """A wave a token: 2^26 tokens are the threads of a launch."""
+    import torch
+    n = (1 << 26) + 12345
+    g = torch.Generator(device="cuda")
+    g.manual_seed(1)
+    X = torch.randn(n, 1, 16, generator=g, device="cuda", dtype=torch.float16)
+    P = torch.arange(n, dtype=torch.int32, device="cuda")
+    rope = _rope(tm, 16)
+    f, amp = tm.tm_rope_frequencies(rope)
+    Y = torch.full_like(X, float("nan"))
+    tm.tm_rope_apply(X, P, rope, Y)
+    some = np.r_[0:3, (1 << 26) - 6:(1 << 26) + 3, n - 3:n]
+    assert _near(_host(Y[some]), op.rope(_host(X[some]), some, f, amp), 1e-9).all()
+    Z, half = torch.empty_like(X), n // 2
+    tm.tm_rope_apply(X[:half], P[:half], rope, Z[:half])
+    tm.tm_rope_apply(X[half:], P[half:], rope, Z[half:])
+    assert torch.equal(Y, Z)
+    rope.close()
+
+
 def test_rope_own_frequencies_and_special_values(tm):
     import torch
     f = np.array([0.0, 1.0, -0.25, 2 * np.pi, 3.0, 1e-9, 1e5, 0.5])
