@@ -7,9 +7,11 @@
  * are rotated on the way in.
  *
  *     tm_rope_apply    rotary positions of packed tokens
- *     tm_paged_append  (rotates and) quantises new keys and values into their pages, rotates the queries along
+ *     tm_heads_apply   norms of their queries and keys head by head, and the rotation, in one pass
+ *     tm_paged_assign  pages of a free list for the new tokens: tables, offsets, positions and slots; tm_paged_release gives pages back
+ *     tm_paged_append  (rotates and) quantises new keys and values into their pages, rotates the queries along; tm_paged_append_heads with norms and positions of several axes
  *     tm_paged_read    the cached keys and values back as fp16
- *     tm_paged_attn    causal attention of every sequence's new tokens over its pages
+ *     tm_paged_attn    causal attention of every sequence's new tokens over its pages; tm_paged_attn_window in a sliding window
  *
  * Conventions as in tm_w4.h: plain C ABI, DEVICE pointers unless marked host, fp16 as uint16_t bit patterns, nothing synchronises or
  * allocates except the create calls, work is enqueued on the given stream, negative tm_status codes with tm_last_error().
@@ -68,12 +70,50 @@ TM_API void tm_rope_free(tm_rope* rope);
 TM_API int tm_rope_frequencies(const tm_rope* rope, double* frequencies, double* amplitude);
 
 /*
+ * Positions of several axes (time, height and width of images and video): a token has `axes` (1 .. 8) positions, and pair i is turned by the one on axis[i] (host, rot_dim / 2
+ * entries of 0 .. axes - 1; NULL with one axis): y1 = amplitude * (x1 cos(p[axis[i]] f_i) - ...).  Whatever takes a rope takes such a one; its positions are then int32
+ * [tokens][axes].  Where a call turns by the sequences' own positions, they stand on every axis, as text tokens have them.
+ */
+TM_API tm_rope* tm_rope_create_axes(const tm_rope_params* params, int axes, const int32_t* axis);
+TM_API int tm_rope_axes(const tm_rope* rope);       /* axes of a handle; negative on error */
+
+/*
  * X fp16 [tokens][heads][head_dim] -> Y of the same shape; token t at X + t * x_stride and Y + t * y_stride (strides in values, multiples of 8, at least
- * heads * head_dim; both pointers 16-byte aligned), so that parts of a fused projection's output are taken as they lie.  positions int32 [tokens], any value.  head_dim is a
+ * heads * head_dim; both pointers 16-byte aligned), so that parts of a fused projection's output are taken as they lie.  positions int32 [tokens] (or [tokens][axes]), any value.  head_dim is a
  * multiple of 8 from rot_dim to 256.  Y may be X with the same stride; any other overlap is undefined.  tokens == 0 is a successful no-op.
  */
 TM_API int tm_rope_apply(const uint16_t* X, int64_t x_stride, const int32_t* positions, const tm_rope* rope, uint16_t* Y, int64_t y_stride, int tokens,
                          int heads, int head_dim, tm_stream stream);
+
+/* ------------------------------------------------------------------------------------------------ norms of heads
+ *
+ * A head's vector x of head_dim values becomes
+ *     n = (x - m) * (offset + weight) / sqrt(mean((x - m)^2) + eps),   m = 0, or with `centred` the mean of x,
+ * and is then turned for its position, in 64 bits up to the result's rounding (to fp32, then to fp16): nothing is rounded between the norm and the rotation.
+ */
+typedef struct tm_head_norm {
+    const uint16_t* weight;       /* device, fp16 [head_dim], or [heads][head_dim] with a stride; 16-byte aligned; NULL = ones */
+    int64_t weight_stride;        /* values from head to head, a multiple of 8; 0 = every head has the same */
+    double eps;                   /* > 0 */
+    double offset;                /* added to every weight: 0, or 1 where a checkpoint keeps weights less one */
+    int centred;                  /* 0 or 1 */
+} tm_head_norm;
+
+typedef struct tm_head_rows {     /* heads of packed tokens: token t at X + t * x_stride -> Y + t * y_stride, as for tm_rope_apply (Y may be X) */
+    const uint16_t* X;
+    int64_t x_stride;
+    uint16_t* Y;
+    int64_t y_stride;
+    int heads;
+    const tm_head_norm* norm;     /* host; NULL: none */
+} tm_head_rows;
+
+/*
+ * Norms and rotation of queries and keys in one launch; q or k may be NULL (host structures).  rope NULL: not turned, and positions counts for nothing; otherwise positions is as for
+ * tm_rope_apply.  head_dim is a multiple of 8 from rot_dim (8 without a rope) to 256.  What one side writes must not overlap what the other reads or writes.  tokens == 0 is a
+ * successful no-op.
+ */
+TM_API int tm_heads_apply(const tm_head_rows* q, const tm_head_rows* k, const int32_t* positions, const tm_rope* rope, int tokens, int head_dim, tm_stream stream);
 
 /* ------------------------------------------------------------------------------------------------ the paged cache
  *
@@ -111,6 +151,48 @@ typedef struct tm_paged_batch {
 } tm_paged_batch;
 
 /*
+ * Pages for new tokens, worked out on the device from the rows' lengths, so that a step needs nothing from the host and can be captured.  A row of the table is a sequence's for as
+ * long as it lives; rows without new tokens have a count of 0.  The pages that no sequence has are a list: the first *count (clamped to [0, capacity]) of `pages`, the last of them
+ * taken first.  left (which may be count) receives what the list has after the call.
+ */
+typedef struct tm_page_list {
+    int32_t* pages;               /* device [capacity] (NULL with a capacity of 0); tm_paged_assign does not write it */
+    const int32_t* count;         /* device [1] */
+    int32_t* left;                /* device [1] */
+    int capacity;
+} tm_page_list;
+
+typedef struct tm_paged_step {
+    const int32_t* lens;          /* device [batch]: tokens that a row has (clamped to [0, max_pages * page_tokens]); its table entries are those of these tokens */
+    const int32_t* counts;        /* device [batch]: new tokens (negative counts as 0) */
+    int32_t* lens_out;            /* device [batch]: tokens that it has then; may be lens */
+    int32_t* table;               /* device [batch][max_pages]: entries of the pages that new tokens begin are written */
+    int32_t* offsets;             /* device [batch + 1], written: running sums of the counts, at most `tokens` */
+    int32_t* positions;           /* device [batch], written: lens */
+    int64_t* slots;               /* device [tokens], written: page * page_tokens + place in it of every new token, -1 where it has none; rows behind the last stay untouched.  NULL: not
+                                     wanted */
+    int32_t* lacking;             /* device [batch], written: 1 where the list had no pages for a row, else 0.  NULL: not wanted */
+    int batch;                    /* 1 .. 65535 */
+    int max_pages;                /* max_pages * page_tokens < 2^30, batch * max_pages < 2^31 */
+    int tokens;                   /* rows of the packed arrays; new tokens beyond them are none */
+} tm_paged_step;
+
+/*
+ * Gives the rows' new tokens pages, in the order of the rows: table, offsets and positions are then those of a tm_paged_batch.  A row whose pages, with those of all rows before it,
+ * are more than the list has gets none: its new entries become -1, its tokens have no slots, its length stays; rows that need no page are served all the same.  Tokens at positions from
+ * max_pages * page_tokens on have no slots and do not count into lens_out.  Arrays that are written must not overlap others but as said.  Uses the cache's workspace.
+ */
+TM_API int tm_paged_assign(tm_paged_cache* cache, const tm_page_list* list, const tm_paged_step* step, tm_stream stream);
+
+/*
+ * Gives pages back: those of row b whose tokens all lie in [from[b], to[b]) (int32 [batch], device; from NULL: 0, to NULL or from max_pages * page_tokens on: to the end of the row).  Whole
+ * rows of sequences that ended, what lies behind a length (drafts that were refused), what lies before a window.  Their entries become -1; entries that name no page of the pool are
+ * passed over.  They come onto the list so that the first row's first page is taken first; what the list has no room for is lost.  A page that several rows share must not be given
+ * back through more than one.  Uses the cache's workspace.
+ */
+TM_API int tm_paged_release(tm_paged_cache* cache, const tm_page_list* list, int32_t* table, int batch, int max_pages, const int32_t* from, const int32_t* to, tm_stream stream);
+
+/*
  * Stores the new tokens: K, V fp16 [tokens][kv_heads][128], row r at K + r * k_stride and V + r * v_stride (strides in values, multiples of 8, at least
  * kv_heads * 128; pointers 16-byte aligned).  With a rope (rot_dim <= 128) keys are rotated for their positions and rounded to fp16 before they are quantised, as by
  * tm_rope_apply, and if Q is not NULL so are the queries, Q fp16 [tokens][q_heads][128] -> Q_out (strides as for tm_rope_apply; Q_out may be Q).  Without one Q must be NULL.
@@ -120,6 +202,20 @@ typedef struct tm_paged_batch {
  */
 TM_API int tm_paged_append(tm_paged_cache* cache, const tm_paged_batch* batch, const uint16_t* K, int64_t k_stride, const uint16_t* V, int64_t v_stride,
                            const tm_rope* rope, const uint16_t* Q, int64_t q_stride, uint16_t* Q_out, int64_t q_out_stride, int q_heads, tm_stream stream);
+
+/*
+ * tm_paged_append with norms of the heads before the rotation, and with positions for it that are not the sequences' own: a key is normed, turned, rounded to fp16 as by tm_heads_apply,
+ * and quantised.  Q is allowed with a rope or a q_norm.  With everything NULL but the rope it is tm_paged_append.
+ */
+typedef struct tm_append_heads {
+    const tm_rope* rope;          /* NULL: not turned */
+    const int32_t* positions;     /* device [tokens][axes of the rope]: what row r is turned by; NULL: a token's position in its sequence, on every axis.  Where it is stored goes by the
+                                     sequences alone */
+    const tm_head_norm* q_norm;   /* host; NULL: none */
+    const tm_head_norm* k_norm;
+} tm_append_heads;
+TM_API int tm_paged_append_heads(tm_paged_cache* cache, const tm_paged_batch* batch, const uint16_t* K, int64_t k_stride, const uint16_t* V, int64_t v_stride,
+                                 const tm_append_heads* heads, const uint16_t* Q, int64_t q_stride, uint16_t* Q_out, int64_t q_out_stride, int q_heads, tm_stream stream);
 
 /*
  * Reads cached tokens back: row offsets[b] + i of K and V, fp16 [tokens][kv_heads][128] (16-byte aligned), becomes fp16((q - z) * s) of the token at

@@ -140,6 +140,10 @@ def load_library():
     lib.tm_bench_read_shape.argtypes = [vp, sz, vp, i, i, i, i, vp]
     lib.tm_rope_create.restype = vp
     lib.tm_rope_create.argtypes = [c.POINTER(TmRopeParams)]
+    lib.tm_rope_create_axes.restype = vp
+    lib.tm_rope_create_axes.argtypes = [c.POINTER(TmRopeParams), i, c.POINTER(c.c_int32)]
+    lib.tm_rope_axes.restype = i
+    lib.tm_rope_axes.argtypes = [vp]
     lib.tm_rope_free.restype = None
     lib.tm_rope_free.argtypes = [vp]
     lib.tm_rope_frequencies.restype = i
@@ -614,9 +618,9 @@ TM_ROPE_PLAIN, TM_ROPE_LINEAR, TM_ROPE_BASE, TM_ROPE_WAVELENGTH, TM_ROPE_RAMP = 
 class Rope:
     """Owner of a tm_rope handle."""
 
-    def __init__(self, handle: int, rot_dim: int):
+    def __init__(self, handle: int, rot_dim: int, axes: int = 1):
         self._h = handle
-        self.rot_dim = rot_dim
+        self.rot_dim, self.axes = rot_dim, axes
 
     @property
     def handle(self):
@@ -639,19 +643,26 @@ class Rope:
 
 
 def tm_rope_create(rot_dim: int = 128, layout: int = TM_ROPE_HALF, base: float = 10000.0, scaling: int = TM_ROPE_PLAIN, factor: float = 1.0,
-                   original_len: float = 0.0, low: float = 0.0, high: float = 0.0, amplitude: float = 0.0, frequencies=None) -> Rope:
+                   original_len: float = 0.0, low: float = 0.0, high: float = 0.0, amplitude: float = 0.0, frequencies=None, axis=None) -> Rope:
     """Rotary positions over the first rot_dim dimensions of a head (see include/tm_paged.h); `frequencies`: rot_dim / 2 numbers,
-    radians per position, instead of those that base and scaling give."""
+    radians per position, instead of those that base and scaling give; `axis`: rot_dim / 2 whole numbers, the axis whose position turns
+    a pair, where positions have several (positions are then [tokens][max(axis) + 1])."""
     p = TmRopeParams(rot_dim, layout, scaling, base, factor, original_len, low, high, amplitude, None)
     if frequencies is not None:
         f = [float(x) for x in frequencies]
         if len(f) != rot_dim // 2:
             raise ValueError(f"need {rot_dim // 2} frequencies, got {len(f)}")
         p.frequencies = (ctypes.c_double * len(f))(*f)
-    h = load_library().tm_rope_create(ctypes.byref(p))
+    axes, of_pair = 1, None
+    if axis is not None:
+        a = [int(x) for x in axis]
+        if len(a) != rot_dim // 2:
+            raise ValueError(f"need the axis of {rot_dim // 2} pairs, got {len(a)}")
+        axes, of_pair = max(a) + 1, (ctypes.c_int32 * len(a))(*a)
+    h = load_library().tm_rope_create_axes(ctypes.byref(p), axes, of_pair)
     if not h:
         raise TmError(-1, tm_last_error())
-    return Rope(h, rot_dim)
+    return Rope(h, rot_dim, axes)
 
 
 def tm_rope_frequencies(rope: Rope):
@@ -662,8 +673,23 @@ def tm_rope_frequencies(rope: Rope):
 
 
 def tm_rope_apply(X, positions, rope: Rope, Y, stream=None):
-    """X, Y float16 [tokens, heads, dim] (rows may lie apart, Y may be X), positions int32 [tokens], all on the device -> Y."""
+    """X, Y float16 [tokens, heads, dim] (rows may lie apart, Y may be X), positions int32 [tokens] or [tokens, axes], all on the device -> Y."""
     return (_calls or _native()).rope_apply(X, positions, rope, Y, stream)
+
+
+class HeadNorm:
+    """Norm of heads: weight float16 [dim], or [heads, dim], on the device, or None (ones); see tm_head_norm in include/tm_paged.h."""
+
+    __slots__ = ("weight", "eps", "offset", "centred")
+
+    def __init__(self, weight=None, eps: float = 1e-6, offset: float = 0.0, centred: bool = False):
+        self.weight, self.eps, self.offset, self.centred = weight, eps, offset, centred
+
+
+def tm_heads_apply(rope: Rope = None, positions=None, Q=None, Q_out=None, q_norm: HeadNorm = None, K=None, K_out=None, k_norm: HeadNorm = None, stream=None):
+    """Norms of Q -> Q_out float16 [tokens, q_heads, dim] and K -> K_out [tokens, k_heads, dim] head by head (rows may lie apart, an output may be its
+    input), and their rotation for positions int32 [tokens] or [tokens, axes], in one pass; either pair, the norms and the rope may be left out."""
+    return (_calls or _native()).heads_apply(rope, positions, Q, Q_out, q_norm, K, K_out, k_norm, stream)
 
 
 def tm_paged_workspace(device="cuda"):
@@ -737,10 +763,39 @@ class PagedBatch:
         self.table, self.offsets, self.positions, self.max_count, self.max_len = table, offsets, positions, max_count, max_len
 
 
-def tm_paged_append(cache: PagedCache, batch: PagedBatch, K, V, rope: Rope = None, Q=None, Q_out=None, stream=None):
+class PageList:
+    """The pages that no sequence has: the first count of `pages` int32 [capacity], the last of them taken first; count int32 [1], both on the device."""
+
+    __slots__ = ("pages", "count")
+
+    def __init__(self, pages, count):
+        self.pages, self.count = pages, count
+
+
+def tm_page_list(pages: int, device="cuda") -> PageList:
+    """All pages of a pool, page 0 first to be taken."""
+    import torch
+    return PageList(torch.arange(pages - 1, -1, -1, dtype=torch.int32, device=device), torch.full((1,), pages, dtype=torch.int32, device=device))
+
+
+def tm_paged_assign(cache: PagedCache, free: PageList, batch: PagedBatch, lens, counts, slots=None, short=None, lens_out=None, left=None, tokens: int = None, stream=None):
+    """Pages of the list for counts[b] (int32 [batch]) new tokens of rows that have lens[b]: writes the batch's table, offsets and positions, slots int64 [tokens]
+    (page * page_tokens + place, -1: none) and short int32 [batch] (1: the list had too few) if given, and the new lengths and the list's count in place, or to lens_out and left.
+    tokens: rows of the packed arrays if not slots.numel()."""
+    return (_calls or _native()).paged_assign(cache, free, batch, lens, counts, slots, short, lens_out, left, tokens, stream)
+
+
+def tm_paged_release(cache: PagedCache, free: PageList, table, first=None, last=None, left=None, stream=None):
+    """Gives back the pages of every row whose tokens all lie in [first[b], last[b]) (int32 [batch]; None: from 0, to the end); their entries become -1.  The list's
+    count is updated in place, or goes to left."""
+    return (_calls or _native()).paged_release(cache, free, table, first, last, left, stream)
+
+
+def tm_paged_append(cache: PagedCache, batch: PagedBatch, K, V, rope: Rope = None, Q=None, Q_out=None, stream=None, q_norm: HeadNorm = None, k_norm: HeadNorm = None, positions=None):
     """Store the new tokens' K, V float16 [tokens, kv_heads, 128] (rows may lie apart) in their pages; with a rope keys are rotated first, and
-    Q [tokens, q_heads, 128] -> Q_out along with them.  -> Q_out"""
-    return (_calls or _native()).paged_append(cache, batch, K, V, rope, Q, Q_out, stream)
+    Q [tokens, q_heads, 128] -> Q_out along with them; with norms they are normed before that.  positions int32 [tokens] or [tokens, axes]: what the rope turns
+    by, if not the tokens' positions in their sequences.  -> Q_out"""
+    return (_calls or _native()).paged_append(cache, batch, K, V, rope, Q, Q_out, stream, q_norm, k_norm, positions)
 
 
 def tm_paged_read(cache: PagedCache, batch: PagedBatch, K, V, stream=None):

@@ -23,7 +23,7 @@ namespace {
 
 PyObject* g_tm_error = nullptr;                          // binding.TmError
 PyObject *s_h, *s_K, *s_N, *s_experts, *s_batch, *s_kv_heads, *s_stream, *s_table, *s_offsets, *s_positions,
-    *s_max_count, *s_max_len;                            // attribute names, interned
+    *s_max_count, *s_max_len, *s_weight, *s_eps, *s_offset, *s_centred, *s_pages, *s_count;    // attribute names, interned
 
 struct Failed {};                                        // a Python exception is set
 
@@ -93,7 +93,7 @@ void* device_ptr(const at::Tensor& t, at::ScalarType type, const char* what)
     }
     if (t.scalar_type() != type) {
         PyErr_Format(PyExc_TypeError, "%s must have dtype torch.%s, got %S", what,
-                     type == at::kHalf ? "float16" : type == at::kInt ? "int32" : "uint8",
+                     type == at::kHalf ? "float16" : type == at::kInt ? "int32" : type == at::kLong ? "int64" : "uint8",
                      (PyObject*)torch::getTHPDtype(t.scalar_type()));
         throw Failed{};
     }
@@ -393,17 +393,200 @@ struct Sequences {
     }
 };
 
+// int32 [tokens], or [tokens][axes] where a rope has several.
+bool positions_fit(const at::Tensor& pos, int64_t tokens)
+{
+    return (pos.dim() == 1 || (pos.dim() == 2 && pos.size(1) > 1)) && pos.size(0) == tokens;
+}
+void check_axes(const at::Tensor& pos, const tm_rope* rope)
+{
+    const int axes = tm_rope_axes(rope);
+    if ((pos.dim() == 1 ? 1 : pos.size(1)) != axes) {
+        PyErr_Format(PyExc_ValueError, "the rope has %d axes, positions must be [tokens]%s", axes, axes == 1 ? "" : "[axes]");
+        throw Failed{};
+    }
+}
+
 PyObject* rope_apply(PyObject*, PyObject* const* a, Py_ssize_t n)    // X, positions, rope, Y, stream
 {
     return entry(n, 5, n > 3 ? a[3] : Py_None, [&] {
         const at::Tensor &X = tensor(a[0], "X"), &pos = tensor(a[1], "positions"), &Y = tensor(a[3], "Y");
-        if (X.dim() != 3 || Y.sizes() != X.sizes() || pos.dim() != 1 || pos.numel() != X.size(0)) raise(PyExc_ValueError, "need X and Y [tokens][heads][dim], positions [tokens]");
+        if (X.dim() != 3 || Y.sizes() != X.sizes() || !positions_fit(pos, X.size(0))) raise(PyExc_ValueError, "need X and Y [tokens][heads][dim], positions [tokens] or [tokens][axes]");
         const TokenRows x(X, "X"), y(Y, "Y");
         const int32_t* p = int_ptr(pos, "positions");
         const auto* h = (const tm_rope*)handle_of(a[2], kRopeFreed);
+        check_axes(pos, h);
         const int tokens = Sequences::whole(X.size(0), "tokens"), heads = Sequences::whole(X.size(1), "heads"), dim = Sequences::whole(X.size(2), "dim");
         const tm_stream st = stream_of(a[4]);
         call([&] { return tm_rope_apply(x.p, x.stride, p, h, y.p, y.stride, tokens, heads, dim, st); });
+    });
+}
+
+// A binding.HeadNorm, or None.  `held` keeps its weight.
+struct Norm {
+    PyObject* held = nullptr;
+    tm_head_norm n{};
+    bool on = false;
+    Norm() = default;
+    Norm(const Norm&) = delete;
+    ~Norm() { Py_XDECREF(held); }
+    void read(PyObject* o, int64_t heads, int64_t dim, const char* what)
+    {
+        if (o == Py_None) return;
+        held = attr(o, s_weight);
+        if (held != Py_None) {
+            const at::Tensor& w = tensor(held, what);
+            n.weight = half_ptr(w, what);
+            on_current_device(w, what);
+            if (!shape_is(w, {dim}) && !shape_is(w, {heads, dim})) {
+                PyErr_Format(PyExc_ValueError, "%s must be [%lld] or [%lld][%lld]", what, (long long)dim, (long long)heads, (long long)dim);
+                throw Failed{};
+            }
+            n.weight_stride = w.dim() == 2 ? dim : 0;
+        }
+        PyObject* values[3] = {nullptr, nullptr, nullptr};
+        try {
+            values[0] = attr(o, s_eps), values[1] = attr(o, s_offset), values[2] = attr(o, s_centred);
+            n.eps = as_double(values[0]);
+            n.offset = as_double(values[1]);
+            const int centred = PyObject_IsTrue(values[2]);
+            if (centred < 0) throw Failed{};
+            n.centred = centred;
+        } catch (...) {
+            for (PyObject* v : values) Py_XDECREF(v);
+            throw;
+        }
+        for (PyObject* v : values) Py_DECREF(v);
+        on = true;
+    }
+    const tm_head_norm* get() const { return on ? &n : nullptr; }
+};
+
+PyObject* heads_apply(PyObject*, PyObject* const* a, Py_ssize_t n)   // rope, positions, Q, Q_out, q_norm, K, K_out, k_norm, stream
+{
+    return entry(n, 9, Py_None, [&] {
+        const at::Tensor* given[2][2] = {};
+        int64_t tokens = -1, dim = 0;
+        static const char* const names[2][3] = {{"Q", "Q_out", "q_norm's weight"}, {"K", "K_out", "k_norm's weight"}};
+        for (int i = 0; i < 2; ++i) {
+            PyObject *x = a[2 + 3 * i], *y = a[3 + 3 * i];
+            if ((x == Py_None) != (y == Py_None)) raise(PyExc_ValueError, i ? "K and K_out go together" : "Q and Q_out go together");
+            if (x == Py_None) {
+                if (a[4 + 3 * i] != Py_None) raise(PyExc_ValueError, i ? "k_norm without K" : "q_norm without Q");
+                continue;
+            }
+            given[i][0] = &tensor(x, names[i][0]), given[i][1] = &tensor(y, names[i][1]);
+            const at::Tensor& t = *given[i][0];
+            if (t.dim() != 3 || given[i][1]->sizes() != t.sizes() || (tokens >= 0 && (t.size(0) != tokens || t.size(2) != dim)))
+                raise(PyExc_ValueError, "need Q, Q_out [tokens][q_heads][dim] and K, K_out [tokens][k_heads][dim]");
+            tokens = t.size(0), dim = t.size(2);
+        }
+        if (tokens < 0) raise(PyExc_ValueError, "neither Q nor K");
+        if ((a[0] == Py_None) != (a[1] == Py_None)) raise(PyExc_ValueError, "a rope and positions go together");
+        const int32_t* p = nullptr;
+        const tm_rope* rope = nullptr;
+        if (a[0] != Py_None) {
+            const at::Tensor& pos = tensor(a[1], "positions");
+            if (!positions_fit(pos, tokens)) raise(PyExc_ValueError, "need positions [tokens] or [tokens][axes]");
+            p = int_ptr(pos, "positions");
+            rope = (const tm_rope*)handle_of(a[0], kRopeFreed);
+            check_axes(pos, rope);
+        }
+        Norm norms[2];
+        tm_head_rows rows[2] = {};
+        for (int i = 0; i < 2; ++i) {
+            if (!given[i][0]) continue;
+            const TokenRows x(*given[i][0], names[i][0]), y(*given[i][1], names[i][1]);
+            norms[i].read(a[4 + 3 * i], given[i][0]->size(1), dim, names[i][2]);
+            rows[i] = tm_head_rows{x.p, x.stride, y.p, y.stride, Sequences::whole(given[i][0]->size(1), "heads"), norms[i].get()};
+        }
+        const int count = Sequences::whole(tokens, "tokens"), width = Sequences::whole(dim, "dim");
+        const tm_stream st = stream_of(a[8]);
+        call([&] { return tm_heads_apply(given[0][0] ? &rows[0] : nullptr, given[1][0] ? &rows[1] : nullptr, p, rope, count, width, st); });
+    });
+}
+
+// A binding.PageList, and where the count goes: `left`, or its own count.
+struct Pages {
+    PyObject* held[2] = {nullptr, nullptr};
+    tm_page_list l{};
+    Pages(const Pages&) = delete;
+    Pages(PyObject* list, PyObject* left)
+    {
+        try {
+            held[0] = attr(list, s_pages), held[1] = attr(list, s_count);
+            const at::Tensor &pages = tensor(held[0], "pages"), &count = tensor(held[1], "count"), &out = left == Py_None ? count : tensor(left, "left");
+            if (pages.dim() != 1 || count.numel() != 1 || out.numel() != 1) raise(PyExc_ValueError, "need pages [capacity], count [1], left [1]");
+            l.pages = (int32_t*)int_ptr(pages, "pages");
+            l.count = int_ptr(count, "count");
+            l.left = (int32_t*)int_ptr(out, "left");
+            l.capacity = Sequences::whole(pages.size(0), "capacity");
+        } catch (...) {
+            drop();
+            throw;
+        }
+    }
+    ~Pages() { drop(); }
+    void drop()
+    {
+        for (PyObject*& o : held) Py_CLEAR(o);
+    }
+};
+
+const int32_t* row_ints(PyObject* o, int64_t rows, const char* what)
+{
+    const at::Tensor& t = tensor(o, what);
+    if (!shape_is(t, {rows})) {
+        PyErr_Format(PyExc_ValueError, "%s must be [%lld]", what, (long long)rows);
+        throw Failed{};
+    }
+    return int_ptr(t, what);
+}
+
+PyObject* paged_assign(PyObject*, PyObject* const* a, Py_ssize_t n)  // cache, list, batch, lens, counts, slots, short, lens_out, left, tokens, stream
+{
+    return entry(n, 11, Py_None, [&] {
+        int64_t tokens = a[9] == Py_None ? -1 : as_int(a[9]);
+        int64_t* slots = nullptr;
+        if (a[5] != Py_None) {
+            const at::Tensor& t = tensor(a[5], "slots");
+            if (t.dim() != 1 || t.numel() < tokens) raise(PyExc_ValueError, "slots must be [tokens]");
+            slots = (int64_t*)device_ptr(t, at::kLong, "slots");
+            on_current_device(t, "slots");
+            if (tokens < 0) tokens = t.numel();
+        }
+        if (tokens < 0) raise(PyExc_ValueError, "need slots or tokens");
+        const Sequences seqs(a[2], tokens);
+        const Pages list(a[1], a[8]);
+        tm_paged_step s{};
+        s.lens = row_ints(a[3], seqs.b.batch, "lens");
+        s.counts = row_ints(a[4], seqs.b.batch, "counts");
+        s.lens_out = (int32_t*)(a[7] == Py_None ? s.lens : row_ints(a[7], seqs.b.batch, "lens_out"));
+        s.lacking = a[6] == Py_None ? nullptr : (int32_t*)row_ints(a[6], seqs.b.batch, "short");
+        s.table = (int32_t*)seqs.b.table;
+        s.offsets = (int32_t*)seqs.b.offsets;
+        s.positions = (int32_t*)seqs.b.positions;
+        s.slots = slots;
+        s.batch = seqs.b.batch, s.max_pages = seqs.b.max_pages, s.tokens = seqs.b.tokens;
+        auto* h = (tm_paged_cache*)handle_of(a[0], kPagedFreed);
+        const tm_stream st = stream_of(a[10]);
+        call([&] { return tm_paged_assign(h, &list.l, &s, st); });
+    });
+}
+
+PyObject* paged_release(PyObject*, PyObject* const* a, Py_ssize_t n) // cache, list, table, from, to, left, stream
+{
+    return entry(n, 7, Py_None, [&] {
+        const at::Tensor& table = tensor(a[2], "table");
+        if (table.dim() != 2) raise(PyExc_ValueError, "need table [batch][max_pages]");
+        auto* entries = (int32_t*)int_ptr(table, "table");
+        const int batch = Sequences::whole(table.size(0), "batch"), max_pages = Sequences::whole(table.size(1), "max_pages");
+        const int32_t* from = a[3] == Py_None ? nullptr : row_ints(a[3], batch, "first");
+        const int32_t* to = a[4] == Py_None ? nullptr : row_ints(a[4], batch, "last");
+        const Pages list(a[1], a[5]);
+        auto* h = (tm_paged_cache*)handle_of(a[0], kPagedFreed);
+        const tm_stream st = stream_of(a[6]);
+        call([&] { return tm_paged_release(h, &list.l, entries, batch, max_pages, from, to, st); });
     });
 }
 
@@ -415,9 +598,9 @@ void check_tokens(const at::Tensor& t, int64_t tokens, int64_t heads, const char
     }
 }
 
-PyObject* paged_append(PyObject*, PyObject* const* a, Py_ssize_t n)  // cache, batch, K, V, rope, Q, Q_out, stream
+PyObject* paged_append(PyObject*, PyObject* const* a, Py_ssize_t n)  // cache, batch, K, V, rope, Q, Q_out, stream, q_norm, k_norm, positions
 {
-    return entry(n, 8, n > 6 ? a[6] : Py_None, [&] {
+    return entry(n, 11, n > 6 ? a[6] : Py_None, [&] {
         const at::Tensor &K = tensor(a[2], "K"), &V = tensor(a[3], "V");
         const int64_t tokens = K.dim() ? K.size(0) : 0, heads = int_attr(a[0], s_kv_heads);
         check_tokens(K, tokens, heads, "K");
@@ -440,8 +623,20 @@ PyObject* paged_append(PyObject*, PyObject* const* a, Py_ssize_t n)  // cache, b
             q = in.p, q_stride = in.stride, q_out = out.p, q_out_stride = out.stride;
             q_heads = Sequences::whole(Q.size(1), "q_heads");
         }
+        Norm q_norm, k_norm;
+        if (a[8] != Py_None && !q) raise(PyExc_ValueError, "q_norm without Q");
+        q_norm.read(a[8], q_heads, 128, "q_norm's weight");
+        k_norm.read(a[9], heads, 128, "k_norm's weight");
+        tm_append_heads of{rope, nullptr, q_norm.get(), k_norm.get()};
+        if (a[10] != Py_None) {
+            const at::Tensor& pos = tensor(a[10], "positions");
+            if (!rope) raise(PyExc_ValueError, "positions without a rope");
+            if (!positions_fit(pos, tokens)) raise(PyExc_ValueError, "need positions [tokens] or [tokens][axes]");
+            of.positions = int_ptr(pos, "positions");
+            check_axes(pos, rope);
+        }
         const tm_stream st = stream_of(a[7]);
-        call([&] { return tm_paged_append(h, &seqs.b, k.p, k.stride, v.p, v.stride, rope, q, q_stride, q_out, q_out_stride, q_heads, st); });
+        call([&] { return tm_paged_append_heads(h, &seqs.b, k.p, k.stride, v.p, v.stride, &of, q, q_stride, q_out, q_out_stride, q_heads, st); });
     });
 }
 
@@ -530,6 +725,9 @@ PyMethodDef g_methods[] = {fast<gemm>("gemm"),
                            fast<attn_decode>("attn_decode"),
                            fast<attn_prefill>("attn_prefill"),
                            fast<rope_apply>("rope_apply"),
+                           fast<heads_apply>("heads_apply"),
+                           fast<paged_assign>("paged_assign"),
+                           fast<paged_release>("paged_release"),
                            fast<paged_append>("paged_append"),
                            fast<paged_read>("paged_read"),
                            fast<paged_attn>("paged_attn"),
@@ -543,9 +741,10 @@ PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "tm_calls", nullptr, -1, g_method
 
 extern "C" __attribute__((visibility("default"))) PyObject* PyInit_tm_calls()
 {
-    PyObject** names[] = {&s_h, &s_K, &s_N, &s_experts, &s_batch, &s_kv_heads, &s_stream, &s_table, &s_offsets, &s_positions, &s_max_count, &s_max_len};
-    const char* texts[] = {"_h", "K", "N", "experts", "batch", "kv_heads", "cuda_stream", "table", "offsets", "positions", "max_count", "max_len"};
-    for (int i = 0; i < 12; ++i)
+    PyObject** names[] = {&s_h, &s_K, &s_N, &s_experts, &s_batch, &s_kv_heads, &s_stream, &s_table, &s_offsets, &s_positions, &s_max_count, &s_max_len,
+                           &s_weight, &s_eps, &s_offset, &s_centred, &s_pages, &s_count};
+    const char* texts[] = {"_h", "K", "N", "experts", "batch", "kv_heads", "cuda_stream", "table", "offsets", "positions", "max_count", "max_len", "weight", "eps", "offset", "centred", "pages", "count"};
+    for (int i = 0; i < 18; ++i)
         if (!(*names[i] = PyUnicode_InternFromString(texts[i]))) return nullptr;
     return PyModule_Create(&g_module);
 }

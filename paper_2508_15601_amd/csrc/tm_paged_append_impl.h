@@ -17,10 +17,11 @@ constexpr int kAppendLds = 2 * 4096;
 // 256 threads, heads h0 .. h1 - 1.  Sixteen lanes hold a token's vector, eight dimensions each; a thread takes two tokens, keys then values (the layout of the block-wise append
 // of the contiguous cache).  All four vectors are requested before the angles are worked out, which hides behind them: sines and cosines of the run's new tokens,
 // a thread a pair at a time, go through LDS.  The next head's vectors are requested while this one's codes are stored.
-template <int BITS>
-__device__ __forceinline__ void append_run(const PagedPool& pool, const PagedSeqs& seqs, PagedRows k, PagedRows v, const RopePlan& rope, uint32_t item, int h0,
+template <int BITS, class Heads>
+__device__ __forceinline__ void append_run(const PagedPool& pool, const PagedSeqs& seqs, PagedRows k, PagedRows v, const RopePlan& rope, const Heads& heads, uint32_t item, int h0,
                                            int h1, unsigned char* lds, CosSin* cs)
 {
+    constexpr bool kHeads = std::is_same<Heads, AppendHeads>::value;
     const int tid = threadIdx.x, lane = tid & 63, sub = tid & 15;
     const RunJob job = run_job(pool, seqs, item, lane);
     if (!job.live || job.page < 0) return;                             // CTA-uniform
@@ -44,7 +45,13 @@ __device__ __forceinline__ void append_run(const PagedPool& pool, const PagedSeq
         const int pairs = rope.rot / 2, at_once = 64 / pairs, tok = lane / pairs, p = lane - tok * pairs;      // tokens of a wave at a time
         if (tok < at_once) {
             const RopeTurn turn = rope.turns[p];
-            for (int u = u0 + (tid >> 6) * at_once + tok; u < u1; u += 4 * at_once) cs[u * (kHeadDim / 2) + p] = rope_angle(rope, job.run * kRun + u, turn);
+            for (int u = u0 + (tid >> 6) * at_once + tok; u < u1; u += 4 * at_once) {
+                int pos = job.run * kRun + u;
+                if constexpr (kHeads) {
+                    if (heads.positions) pos = heads.positions[(job.row + u) * rope.axes + turn.axis];
+                }
+                cs[u * (kHeadDim / 2) + p] = rope_angle(rope, pos, turn);
+            }
         }
         __syncthreads();
     }
@@ -57,7 +64,11 @@ __device__ __forceinline__ void append_run(const PagedPool& pool, const PagedSeq
         for (int it = 0; it < 4; ++it) {
             const int which = it >> 1, u = slot[it & 1];
             const bool live = u >= u0 && u < u1;
-            if (which == 0 && rope.rot) raw[it] = rope_sixteenth(raw[it], rope, cs + (live ? u : u0) * (kHeadDim / 2), lane);
+            if constexpr (kHeads) {
+                if (which == 0) raw[it] = head_sixteenth(raw[it], h, heads.k, rope, cs + (live ? u : u0) * (kHeadDim / 2), lane);
+            } else {
+                if (which == 0 && rope.rot) raw[it] = rope_sixteenth(raw[it], rope, cs + (live ? u : u0) * (kHeadDim / 2), lane);
+            }
             uint32_t q[8];
             const uint32_t pair = quantise_row8<BITS>(raw[it], q);
             u32x2 bytes;
@@ -141,9 +152,11 @@ __device__ __forceinline__ void append_run(const PagedPool& pool, const PagedSeq
 }
 
 // Queries of one token, heads h0 .. h1 - 1, by one wave.
-__device__ __forceinline__ void rotate_row(const PagedSeqs& seqs, PagedRows q, uint16_t* out, long out_stride, int q_heads, const RopePlan& rope, uint32_t row, int h0,
-                                           int h1, CosSin* cs, int lane)
+template <class Heads>
+__device__ __forceinline__ void rotate_row(const PagedSeqs& seqs, PagedRows q, uint16_t* out, long out_stride, int q_heads, const RopePlan& rope, const Heads& heads, uint32_t row,
+                                           int h0, int h1, CosSin* cs, int lane)
 {
+    constexpr bool kHeads = std::is_same<Heads, AppendHeads>::value;
     const SeqFinder finder([&](int b) { return (uint32_t)paged_seq(seqs, b).count; }, seqs.batch, lane);
     const bool live = row < finder.total;
     long at = 0;
@@ -151,15 +164,24 @@ __device__ __forceinline__ void rotate_row(const PagedSeqs& seqs, PagedRows q, u
         uint32_t base;
         const PagedSeq s = paged_seq(seqs, finder.find(row, base));
         at = min((long)s.row + (row - base), (long)seqs.tokens - 1);
-        rope_angles(cs, rope, (int)((uint32_t)s.pos + (row - base)), lane);
+        bool own = true;
+        if constexpr (kHeads) own = !heads.positions;
+        if (own) rope_angles(cs, rope, (int)((uint32_t)s.pos + (row - base)), lane);
+        if constexpr (kHeads) {
+            if (!own) rope_angles_of(cs, rope, heads.positions + at * rope.axes, lane);
+        }
     }
     __syncthreads();
-    if (live) rope_heads(q.p + at * q.stride, out + at * out_stride, h0, h1, kHeadDim, rope, cs, lane);
+    if constexpr (kHeads) {
+        if (live) turn_heads(q.p + at * q.stride, out + at * out_stride, h0, h1, heads.q, rope, cs, lane);
+    } else {
+        if (live) rope_heads(q.p + at * q.stride, out + at * out_stride, h0, h1, kHeadDim, rope, cs, lane);
+    }
 }
 
 // Blocks 0 .. kv_blocks - 1: runs of keys and values, heads of a run next to each other; the blocks behind them: queries, a wave `per_wave` heads of a row.
-template <int BITS>
-__global__ __launch_bounds__(256) void paged_append_kernel(PagedPool pool, PagedSeqs seqs, PagedRows k, PagedRows v, RopePlan rope, unsigned kv_blocks, int kv_heads,
+template <int BITS, class Heads>
+__global__ __launch_bounds__(256) void paged_append_kernel(PagedPool pool, PagedSeqs seqs, PagedRows k, PagedRows v, RopePlan rope, Heads heads, unsigned kv_blocks, int kv_heads,
                                                            PagedRows q, uint16_t* q_out, long q_out_stride, int q_heads, int per_wave)
 {
     __shared__ __align__(16) unsigned char lds[kAppendLds];
@@ -167,7 +189,7 @@ __global__ __launch_bounds__(256) void paged_append_kernel(PagedPool pool, Paged
     if (blockIdx.x < kv_blocks) {
         const unsigned groups = (unsigned)((pool.heads + kv_heads - 1) / kv_heads), run = blockIdx.x / groups;
         const int h0 = (int)(blockIdx.x - run * groups) * kv_heads;
-        append_run<BITS>(pool, seqs, k, v, rope, run, h0, min(h0 + kv_heads, pool.heads), lds, cs);
+        append_run<BITS>(pool, seqs, k, v, rope, heads, run, h0, min(h0 + kv_heads, pool.heads), lds, cs);
         return;
     }
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -175,7 +197,7 @@ __global__ __launch_bounds__(256) void paged_append_kernel(PagedPool pool, Paged
     const unsigned long job = (unsigned long)(blockIdx.x - kv_blocks) * 4 + wave;
     const unsigned row = (unsigned)(job / parts);
     const int h0 = (int)(job - (unsigned long)row * parts) * per_wave;
-    rotate_row(seqs, q, q_out, q_out_stride, q_heads, rope, row, h0, min(h0 + per_wave, q_heads), cs + wave * (kHeadDim / 2), lane);
+    rotate_row(seqs, q, q_out, q_out_stride, q_heads, rope, heads, row, h0, min(h0 + per_wave, q_heads), cs + wave * (kHeadDim / 2), lane);
 }
 
 // Few new tokens a sequence (a decoding step, drafts): a wave takes four of a token's vectors - keys of the KV heads, their values, then query heads - and puts codes where they
@@ -183,10 +205,11 @@ __global__ __launch_bounds__(256) void paged_append_kernel(PagedPool pool, Paged
 // ones follow in the same waves.  4-bit values of a sequence's tokens share bytes, so there a sequence's tokens all go through the same waves (step = 1).
 template <int BITS>
 constexpr int kFewTokens = BITS == 8 ? 8 : 1;
-template <int BITS>
-__global__ __launch_bounds__(256) void paged_append_tokens_kernel(PagedPool pool, PagedSeqs seqs, PagedRows k, PagedRows v, RopePlan rope, PagedRows q, uint16_t* q_out,
+template <int BITS, class Heads>
+__global__ __launch_bounds__(256) void paged_append_tokens_kernel(PagedPool pool, PagedSeqs seqs, PagedRows k, PagedRows v, RopePlan rope, Heads heads, PagedRows q, uint16_t* q_out,
                                                                   long q_out_stride, int q_heads, int per_token, int step)
 {
+    constexpr bool kHeads = std::is_same<Heads, AppendHeads>::value;
     __shared__ CosSin cs[4][kHeadDim / 2];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), sub = lane & 15;
     const uint32_t job = blockIdx.x * 4 + wave;
@@ -202,12 +225,21 @@ __global__ __launch_bounds__(256) void paged_append_tokens_kernel(PagedPool pool
         const PagedRows& from = which == 0 ? k : which == 1 ? v : q;
         u32x4 raw = {0u, 0u, 0u, 0u};
         if (which < 2 || h < q_heads) raw = *(const u32x4*)(from.p + row * from.stride + h * kHeadDim + 8 * sub);
-        if (rope.rot) {
-            rope_angles(cs[wave], rope, pos, lane);
+        if (kHeads || rope.rot) {
+            bool own = true;
+            if constexpr (kHeads) {
+                own = !heads.positions;
+                if (!own) rope_angles_of(cs[wave], rope, heads.positions + row * rope.axes, lane);
+            }
+            if (own) rope_angles(cs[wave], rope, pos, lane);
             __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
             __builtin_amdgcn_wave_barrier();
-            const u32x4 turned = rope_sixteenth(raw, rope, cs[wave], lane);
-            if (which != 1) raw = turned;
+            if constexpr (kHeads) {
+                if (which != 1) raw = head_sixteenth(raw, which == 2 ? max(min(h, q_heads - 1), 0) : h, which == 2 ? heads.q : heads.k, rope, cs[wave], lane);
+            } else {
+                const u32x4 turned = rope_sixteenth(raw, rope, cs[wave], lane);
+                if (which != 1) raw = turned;
+            }
             __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
             __builtin_amdgcn_wave_barrier();
         }
@@ -249,18 +281,20 @@ __global__ __launch_bounds__(256) void paged_append_tokens_kernel(PagedPool pool
 
 }  // namespace
 
-hipError_t launch_paged_append(const PagedPool& pool, const PagedSeqs& seqs, PagedRows k, PagedRows v, const RopePlan* rope, PagedRows q, uint16_t* q_out,
-                               long q_out_stride, int q_heads, int max_count, int num_cu, hipStream_t stream)
+namespace {
+
+template <class Heads>
+hipError_t launch_append(const PagedPool& pool, const PagedSeqs& seqs, PagedRows k, PagedRows v, const RopePlan& plan, const Heads& of_heads, PagedRows q, uint16_t* q_out,
+                         long q_out_stride, int q_heads, int max_count, int num_cu, hipStream_t stream)
 {
-    const RopePlan plan = rope ? *rope : RopePlan{nullptr, 1.0, 0, 0};
     // Measured (32 / 8 heads, 8-bit, queries too), in brackets by runs: one token each of 1, 16, 64 and 256 sequences 3.7, 4.0, 4.0 and 5.3 us (5.2, 5.4, 7.2, 19.5); five each of
     // 12, 64 and 256 sequences 4.1, 6.4 and 14.4 us (5.5, 7.9, 27.6), eight 4.4, 7.9 and 20.1 (5.8, 8.5, 31.2).  Beyond that runs, whose tokens share their way to the page;
     // with 4-bit codes from two tokens on (with atomic operations on the shared bytes 64 sequences of five took 11.9 us, by runs 7.8).
     const int heads = q.p ? q_heads : 0, per_token = (2 * pool.heads + heads + 3) / 4;
     if (max_count >= 1 && max_count <= (pool.bits == 8 ? kFewTokens<8> : kFewTokens<4>) && (long)seqs.batch * max_count * per_token <= 4 * most_ctas(256)) {
         const long blocks = ((long)seqs.batch * max_count * per_token + 3) / 4;
-        const auto kernel = pool.bits == 8 ? paged_append_tokens_kernel<8> : paged_append_tokens_kernel<4>;
-        hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(256), 0, stream, pool, seqs, k, v, plan, q, q_out, q_out_stride, heads, per_token, max_count);
+        const auto kernel = pool.bits == 8 ? paged_append_tokens_kernel<8, Heads> : paged_append_tokens_kernel<4, Heads>;
+        hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(256), 0, stream, pool, seqs, k, v, plan, of_heads, q, q_out, q_out_stride, heads, per_token, max_count);
         return hipGetLastError();
     }
     // KV heads a CTA: they share a run's sines and cosines, but take their turns, so that only pays where a compute unit has more CTAs than it holds at a time.  By runs x heads (us; one, two
@@ -274,9 +308,19 @@ hipError_t launch_paged_append(const PagedPool& pool, const PagedSeqs& seqs, Pag
     const int per_wave = (long)seqs.tokens * q_heads >= 16384L * 8 ? q_heads : 8;
     const long jobs = q.p ? (long)seqs.tokens * ((q_heads + per_wave - 1) / per_wave) : 0, blocks = kv + (jobs + 3) / 4;
     if (blocks <= 0 || blocks > most_ctas(256)) return hipErrorInvalidConfiguration;
-    const auto kernel = pool.bits == 8 ? paged_append_kernel<8> : paged_append_kernel<4>;
-    hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(256), 0, stream, pool, seqs, k, v, plan, (unsigned)kv, kv_heads, q, q_out, q_out_stride, q_heads, per_wave);
+    const auto kernel = pool.bits == 8 ? paged_append_kernel<8, Heads> : paged_append_kernel<4, Heads>;
+    hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(256), 0, stream, pool, seqs, k, v, plan, of_heads, (unsigned)kv, kv_heads, q, q_out, q_out_stride, q_heads, per_wave);
     return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_paged_append(const PagedPool& pool, const PagedSeqs& seqs, PagedRows k, PagedRows v, const RopePlan* rope, const AppendHeads* heads, PagedRows q, uint16_t* q_out,
+                               long q_out_stride, int q_heads, int max_count, int num_cu, hipStream_t stream)
+{
+    const RopePlan plan = rope ? *rope : RopePlan{nullptr, 1.0, 0, 0, 1};
+    return heads ? launch_append(pool, seqs, k, v, plan, *heads, q, q_out, q_out_stride, q_heads, max_count, num_cu, stream)
+                 : launch_append(pool, seqs, k, v, plan, NoHeads{}, q, q_out, q_out_stride, q_heads, max_count, num_cu, stream);
 }
 
 }  // namespace tmw4

@@ -21,7 +21,8 @@ __global__ __launch_bounds__(256) void rope_kernel(const uint16_t* X, long x_str
     const long job = (long)blockIdx.x * 4 + wave;
     const long token = job / parts;
     const int h0 = (int)(job - token * parts) * per_wave;
-    if (token < tokens) rope_angles(cs[wave], r, positions[token], lane);
+    if (token < tokens && r.axes == 1) rope_angles(cs[wave], r, positions[token], lane);
+    if (token < tokens && r.axes != 1) rope_angles_of(cs[wave], r, positions + token * r.axes, lane);
     __syncthreads();
     if (token >= tokens) return;
     rope_heads(X + token * x_stride, Y + token * y_stride, h0, min(h0 + per_wave, heads), dim, r, cs[wave], lane);
@@ -38,7 +39,7 @@ hipError_t launch_rope(const uint16_t* X, long x_stride, const int32_t* position
     const long parts = (heads + per_wave - 1) / per_wave, most = 4 * most_ctas(256) / parts;       // tokens of a launch
     for (long t = 0; t < tokens; t += most) {
         const int n = (int)std::min(most, tokens - t);
-        hipLaunchKernelGGL(rope_kernel, dim3((unsigned)((n * parts + 3) / 4)), dim3(256), 0, stream, X + t * x_stride, x_stride, positions + t, r, Y + t * y_stride, y_stride, n, heads,
+        hipLaunchKernelGGL(rope_kernel, dim3((unsigned)((n * parts + 3) / 4)), dim3(256), 0, stream, X + t * x_stride, x_stride, positions + t * r.axes, r, Y + t * y_stride, y_stride, n, heads,
                            dim, per_wave);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;

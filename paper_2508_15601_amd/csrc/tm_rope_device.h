@@ -16,6 +16,7 @@ constexpr int kRopeMaxPairs = 128;       // head dimensions up to 256
 struct RopeTurn {                        // a fraction of a turn
     uint64_t high;                       // in units of 2^-64
     uint32_t low;                        // and of 2^-96
+    uint32_t axis = 0;                   // of the position that turns the pair
 };
 
 struct RopePlan {
@@ -23,6 +24,7 @@ struct RopePlan {
     double amp;                          // factor of the rotated values
     int rot;                             // dimensions that are rotated, a multiple of 16
     int interleaved;                     // pairs are (2i, 2i + 1); otherwise (i, i + rot / 2)
+    int axes;                            // positions of a token
 };
 
 struct CosSin {
@@ -50,6 +52,15 @@ __device__ __forceinline__ _Float16 rope_round(double x)
     float f = (float)x;
     asm("" : "+v"(f));
     return (_Float16)f;
+}
+
+// Cosines and sines of a token's pairs, by one wave; every pair by the position on its axis.
+__device__ __forceinline__ void rope_angles_of(CosSin* cs, const RopePlan& r, const int32_t* positions, int lane)
+{
+    for (int i = lane; i < r.rot / 2; i += 64) {
+        const RopeTurn turn = r.turns[i];
+        cs[i] = rope_angle(r, positions[turn.axis], turn);
+    }
 }
 
 // Rotates the pairs (a[i], b[i]) of eight values each by cs[i].

@@ -1928,7 +1928,7 @@ int tm_kv_raw(const tm_kv_cache* cache, void** k_codes, void** v_codes, void** p
 
 struct tm_rope {
     uint32_t magic;
-    int device, rot, interleaved;
+    int device, rot, interleaved, axes;
     double amp;
     double f[kRopeMaxPairs];
     RopeTurn* turns;
@@ -2007,7 +2007,9 @@ static bool rope_frequencies(const tm_rope_params& p, double* f, double* amp)
     return true;
 }
 
-tm_rope* tm_rope_create(const tm_rope_params* params)
+tm_rope* tm_rope_create(const tm_rope_params* params) { return tm_rope_create_axes(params, 1, nullptr); }
+
+tm_rope* tm_rope_create_axes(const tm_rope_params* params, int axes, const int32_t* axis)
 {
     if (!params) {
         fail(TM_EINVAL, "params is null");
@@ -2019,6 +2021,15 @@ tm_rope* tm_rope_create(const tm_rope_params* params)
         fail(TM_EINVAL, "need rot_dim a multiple of 16 in 16 .. %d, a known layout and scaling (got %d, %d, %d)", 2 * kRopeMaxPairs, p.rot_dim, p.layout, p.scaling);
         return nullptr;
     }
+    if (axes < 1 || axes > 8 || (axes > 1 && !axis)) {
+        fail(TM_EINVAL, "need 1 <= axes <= 8 and the axis of every pair where there are several (got %d)", axes);
+        return nullptr;
+    }
+    for (int i = 0; axis && i < p.rot_dim / 2; ++i)
+        if (axis[i] < 0 || axis[i] >= axes) {
+            fail(TM_EINVAL, "axis[%d] = %d, there are %d", i, (int)axis[i], axes);
+            return nullptr;
+        }
     tm_rope* r = new (std::nothrow) tm_rope();
     if (!r) {
         fail(TM_ENOMEM, "host allocation failed");
@@ -2035,8 +2046,12 @@ tm_rope* tm_rope_create(const tm_rope_params* params)
     }
     r->rot = p.rot_dim;
     r->interleaved = p.layout == TM_ROPE_INTERLEAVED;
+    r->axes = axes;
     RopeTurn turns[kRopeMaxPairs] = {};
-    for (int i = 0; i < r->rot / 2; ++i) turns[i] = rope_turn(r->f[i]);
+    for (int i = 0; i < r->rot / 2; ++i) {
+        turns[i] = rope_turn(r->f[i]);
+        turns[i].axis = axis ? (uint32_t)axis[i] : 0u;
+    }
     hipError_t e = hipMalloc((void**)&r->turns, sizeof(RopeTurn) * (size_t)(r->rot / 2));
     if (e == hipSuccess) {
         e = hipMemcpy(r->turns, turns, sizeof(RopeTurn) * (size_t)(r->rot / 2), hipMemcpyHostToDevice);
@@ -2067,7 +2082,13 @@ int tm_rope_frequencies(const tm_rope* rope, double* frequencies, double* amplit
     return TM_OK;
 }
 
-static RopePlan rope_plan(const tm_rope* r) { return RopePlan{r->turns, r->amp, r->rot, r->interleaved}; }
+int tm_rope_axes(const tm_rope* rope)
+{
+    if (!valid_rope(rope)) return fail(TM_EINVAL, "rope handle is null or invalid");
+    return rope->axes;
+}
+
+static RopePlan rope_plan(const tm_rope* r) { return r ? RopePlan{r->turns, r->amp, r->rot, r->interleaved, r->axes} : RopePlan{nullptr, 1.0, 0, 0, 1}; }
 
 // A packed array of [rows][values]: alignment and stride.
 static int check_rows(const char* what, const void* p, int64_t stride, int64_t values)
@@ -2097,6 +2118,54 @@ int tm_rope_apply(const uint16_t* X, int64_t x_stride, const int32_t* positions,
     if (dev != rope->device) return fail(TM_EINVAL, "rope lives on device %d, current device is %d", rope->device, dev);
     const hipError_t e = launch_rope(X, x_stride, positions, rope_plan(rope), Y, y_stride, tokens, heads, head_dim, (hipStream_t)stream);
     if (e != hipSuccess) return fail_hip(e, "rope launch");
+    return TM_OK;
+}
+
+// The kernels' view of a norm of `heads` heads.
+static int check_norm(const char* what, const tm_head_norm* n, int dim, HeadNorm* out)
+{
+    *out = HeadNorm{nullptr, 0, 1.0, 0.0, 0, 0};
+    if (!n) return TM_OK;
+    if (!(n->eps > 0.0) || !isfinite(n->eps) || !isfinite(n->offset)) return fail(TM_EINVAL, "%s: need eps > 0 and a finite offset (got %g, %g)", what, n->eps, n->offset);
+    if (n->centred != 0 && n->centred != 1) return fail(TM_EINVAL, "%s: centred = %d", what, n->centred);
+    if ((uintptr_t)n->weight & 15) return fail(TM_EINVAL, "%s: weight must be 16-byte aligned", what);
+    if (n->weight_stride && (n->weight_stride % 8 || n->weight_stride < dim || n->weight_stride >= (int64_t(1) << 31)))
+        return fail(TM_EINVAL, "%s: weight_stride %lld must be 0, or a multiple of 8, at least %d and below 2^31", what, (long long)n->weight_stride, dim);
+    *out = HeadNorm{n->weight, (long)n->weight_stride, n->eps, n->offset, 1, n->centred};
+    return TM_OK;
+}
+
+int tm_heads_apply(const tm_head_rows* q, const tm_head_rows* k, const int32_t* positions, const tm_rope* rope, int tokens, int head_dim, tm_stream stream)
+{
+    if (!q && !k) return fail(TM_EINVAL, "neither queries nor keys");
+    if (rope && !valid_rope(rope)) return fail(TM_EINVAL, "rope handle is invalid");
+    const int least = rope ? rope->rot : 8;
+    if (tokens < 0) return fail(TM_EINVAL, "tokens = %d", tokens);
+    if (head_dim % 8 || head_dim < least || head_dim > 256) return fail(TM_EINVAL, "head_dim = %d must be a multiple of 8 from %d to 256", head_dim, least);
+    HeadRows rows[2] = {};
+    const tm_head_rows* const given[2] = {q, k};
+    static const char* const names[2][2] = {{"Q", "Q_out"}, {"K", "K_out"}};
+    for (int i = 0; i < 2; ++i) {
+        const tm_head_rows* const g = given[i];
+        int rc = check_norm(names[i][0], g ? g->norm : nullptr, head_dim, &rows[i].norm);
+        if (rc != TM_OK) return rc;
+        if (!g) continue;
+        if (g->heads <= 0 || g->heads > 65535) return fail(TM_EINVAL, "%s: need 1 <= heads <= 65535 (got %d)", names[i][0], g->heads);
+        if (tokens == 0) continue;
+        rc = check_rows(names[i][0], g->X, g->x_stride, (int64_t)g->heads * head_dim);
+        if (rc == TM_OK) rc = check_rows(names[i][1], g->Y, g->y_stride, (int64_t)g->heads * head_dim);
+        if (rc != TM_OK) return rc;
+        if (g->X == g->Y && g->x_stride != g->y_stride) return fail(TM_EINVAL, "%s: in place needs equal strides", names[i][0]);
+        rows[i].x = g->X, rows[i].x_stride = g->x_stride, rows[i].y = g->Y, rows[i].y_stride = g->y_stride, rows[i].heads = g->heads;
+    }
+    if (tokens == 0) return TM_OK;
+    if (rope && (!positions || ((uintptr_t)positions & 3))) return fail(TM_EINVAL, "positions is null or misaligned");
+    int dev;
+    const int rc = check_device(&dev);
+    if (rc != TM_OK) return rc;
+    if (rope && dev != rope->device) return fail(TM_EINVAL, "rope lives on device %d, current device is %d", rope->device, dev);
+    const hipError_t e = launch_heads(rows[0], rows[1], positions, rope_plan(rope), tokens, head_dim, (hipStream_t)stream);
+    if (e != hipSuccess) return fail_hip(e, "heads launch");
     return TM_OK;
 }
 
@@ -2179,12 +2248,29 @@ static int check_paged_device(const tm_paged_cache* cache, int* dev)
 int tm_paged_append(tm_paged_cache* cache, const tm_paged_batch* batch, const uint16_t* K, int64_t k_stride, const uint16_t* V, int64_t v_stride, const tm_rope* rope,
                     const uint16_t* Q, int64_t q_stride, uint16_t* Q_out, int64_t q_out_stride, int q_heads, tm_stream stream)
 {
+    const tm_append_heads heads{rope, nullptr, nullptr, nullptr};
+    return tm_paged_append_heads(cache, batch, K, k_stride, V, v_stride, &heads, Q, q_stride, Q_out, q_out_stride, q_heads, stream);
+}
+
+int tm_paged_append_heads(tm_paged_cache* cache, const tm_paged_batch* batch, const uint16_t* K, int64_t k_stride, const uint16_t* V, int64_t v_stride, const tm_append_heads* heads,
+                          const uint16_t* Q, int64_t q_stride, uint16_t* Q_out, int64_t q_out_stride, int q_heads, tm_stream stream)
+{
     PagedSeqs seqs;
     int rc = check_paged(cache, batch, &seqs);
     if (rc != TM_OK) return rc;
+    if (!heads) return fail(TM_EINVAL, "heads is null");
+    const tm_rope* const rope = heads->rope;
     if (rope && !valid_rope(rope)) return fail(TM_EINVAL, "rope handle is invalid");
     if (rope && rope->rot > 128) return fail(TM_EINVAL, "rot_dim = %d, the cache's heads have 128 dimensions", rope->rot);
-    if (Q && !rope) return fail(TM_EINVAL, "Q without a rope");
+    if (Q && !rope && !heads->q_norm) return fail(TM_EINVAL, "Q without a rope or a norm");
+    if (!Q && heads->q_norm) return fail(TM_EINVAL, "a norm of queries without Q");
+    if (heads->positions && !rope) return fail(TM_EINVAL, "positions without a rope");
+    if ((uintptr_t)heads->positions & 3) return fail(TM_EINVAL, "misaligned positions");
+    AppendHeads with{};
+    rc = check_norm("q_norm", heads->q_norm, 128, &with.q);
+    if (rc == TM_OK) rc = check_norm("k_norm", heads->k_norm, 128, &with.k);
+    if (rc != TM_OK) return rc;
+    with.positions = heads->positions;
     if (seqs.tokens == 0) return TM_OK;
     const int64_t values = (int64_t)cache->pool.heads * 128;
     rc = check_rows("K", K, k_stride, values);
@@ -2199,9 +2285,9 @@ int tm_paged_append(tm_paged_cache* cache, const tm_paged_batch* batch, const ui
     if (rc == TM_OK) rc = check_paged_device(cache, &dev);
     if (rc != TM_OK) return rc;
     if (rope && rope->device != dev) return fail(TM_EINVAL, "rope lives on device %d, current device is %d", rope->device, dev);
-    RopePlan plan{};
-    if (rope) plan = rope_plan(rope);
-    const hipError_t e = launch_paged_append(cache->pool, seqs, PagedRows{K, (long)k_stride}, PagedRows{V, (long)v_stride}, rope ? &plan : nullptr,
+    const RopePlan plan = rope_plan(rope);
+    const bool plain = !with.q.on && !with.k.on && !with.positions;
+    const hipError_t e = launch_paged_append(cache->pool, seqs, PagedRows{K, (long)k_stride}, PagedRows{V, (long)v_stride}, rope ? &plan : nullptr, plain ? nullptr : &with,
                                              PagedRows{Q, (long)q_stride}, Q_out, (long)q_out_stride, q_heads, batch->max_count, g_dev[dev].num_cu, (hipStream_t)stream);
     if (e != hipSuccess) return fail_hip(e, "paged append launch");
     return TM_OK;
@@ -2219,6 +2305,57 @@ int tm_paged_read(const tm_paged_cache* cache, const tm_paged_batch* batch, uint
     if (rc != TM_OK) return rc;
     const hipError_t e = launch_paged_read(cache->pool, seqs, K, V, (hipStream_t)stream);
     if (e != hipSuccess) return fail_hip(e, "paged read launch");
+    return TM_OK;
+}
+
+// The pages of a list and the rows of a table.
+static int check_pages(const tm_paged_cache* cache, const tm_page_list* list, const int32_t* table, int batch, int max_pages)
+{
+    if (!valid_paged(cache)) return fail(TM_EINVAL, "cache handle is null or invalid");
+    if (!list || (!list->pages && list->capacity) || !list->count || !list->left || !table) return fail(TM_EINVAL, "list, its pages, count or left, or table is null");
+    if (((uintptr_t)list->pages | (uintptr_t)list->count | (uintptr_t)list->left | (uintptr_t)table) & 3) return fail(TM_EINVAL, "misaligned list or table");
+    const int page_log = cache->pool.run_log + 5;
+    if (list->capacity < 0 || batch <= 0 || batch > 65535 || max_pages <= 0 || ((int64_t)max_pages << page_log) >= (int64_t(1) << 30) || (int64_t)batch * max_pages >= (int64_t(1) << 31))
+        return fail(TM_EINVAL, "need capacity >= 0, 1 <= batch <= 65535, max_pages > 0, max_pages * %d < 2^30, batch * max_pages < 2^31 (got %d, %d, %d)", 1 << page_log, list->capacity,
+                    batch, max_pages);
+    return TM_OK;
+}
+
+int tm_paged_assign(tm_paged_cache* cache, const tm_page_list* list, const tm_paged_step* step, tm_stream stream)
+{
+    if (!step) return fail(TM_EINVAL, "step is null");
+    const tm_paged_step& s = *step;
+    int rc = check_pages(cache, list, s.table, s.batch, s.max_pages);
+    if (rc != TM_OK) return rc;
+    if (!s.lens || !s.counts || !s.lens_out || !s.offsets || !s.positions) return fail(TM_EINVAL, "lens, counts, lens_out, offsets or positions is null");
+    if (((uintptr_t)s.lens | (uintptr_t)s.counts | (uintptr_t)s.lens_out | (uintptr_t)s.offsets | (uintptr_t)s.positions | (uintptr_t)s.lacking) & 3 || (uintptr_t)s.slots & 7)
+        return fail(TM_EINVAL, "misaligned lens, counts, lens_out, offsets, positions, lacking or slots");
+    if (s.tokens < 0) return fail(TM_EINVAL, "tokens = %d", s.tokens);
+    if (s.positions == s.lens || s.positions == s.lens_out || s.positions == s.counts || s.lens_out == s.counts)
+        return fail(TM_EINVAL, "positions and counts must be arrays of their own");
+    int dev;
+    rc = check_paged_device(cache, &dev);
+    if (rc != TM_OK) return rc;
+    const int page_log = cache->pool.run_log + 5;
+    const AssignJob job{list->pages, list->count, list->left, s.lens, s.counts, s.lens_out, s.table, s.offsets, s.positions, s.slots, s.lacking, list->capacity, cache->pool.pages,
+                        page_log, s.batch, s.max_pages, s.tokens, s.max_pages << page_log};
+    const hipError_t e = launch_assign(job, g_dev[dev].num_cu, cache->workspace, (hipStream_t)stream);
+    if (e != hipSuccess) return fail_hip(e, "page assignment launch");
+    return TM_OK;
+}
+
+int tm_paged_release(tm_paged_cache* cache, const tm_page_list* list, int32_t* table, int batch, int max_pages, const int32_t* from, const int32_t* to, tm_stream stream)
+{
+    int rc = check_pages(cache, list, table, batch, max_pages);
+    if (rc != TM_OK) return rc;
+    if (((uintptr_t)from | (uintptr_t)to) & 3) return fail(TM_EINVAL, "misaligned from or to");
+    int dev;
+    rc = check_paged_device(cache, &dev);
+    if (rc != TM_OK) return rc;
+    const int page_log = cache->pool.run_log + 5;
+    const ReleaseJob job{list->pages, list->count, list->left, table, from, to, list->capacity, cache->pool.pages, page_log, batch, max_pages, max_pages << page_log};
+    const hipError_t e = launch_release(job, cache->workspace, (hipStream_t)stream);
+    if (e != hipSuccess) return fail_hip(e, "page release launch");
     return TM_OK;
 }
 
