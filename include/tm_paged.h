@@ -240,6 +240,14 @@ TM_API int tm_paged_attn(const uint16_t* Q, int64_t q_stride, const tm_paged_cac
                          tm_stream stream);
 
 /*
+ * tm_paged_attn in a sliding window: the query at position p attends over the cached tokens t <= p with t > p - window, its own among them, or t < sinks: the last `window` tokens (>= 1) and the first
+ * `sinks` (>= 0; INT_MAX as a window is tm_paged_attn).  What no new token of a sequence sees is not read, so its pages may have gone back to the pool and its table entries may
+ * be anything.  Everything else as for tm_paged_attn; batch->max_len stays the most tokens of a sequence.
+ */
+TM_API int tm_paged_attn_window(const uint16_t* Q, int64_t q_stride, const tm_paged_cache* cache, const tm_paged_batch* batch, uint16_t* O, int q_heads, float scale, int window,
+                                int sinks, tm_stream stream);
+
+/*
  * Query hook: how tm_paged_attn divides such a call (host out-pointers, any may be NULL).  Sequences with up to *column_rows (token, query head of a KV head) rows, *columns of
  * them at a time (8, 16 or 32; 0 = no such launch), the others in CTAs of *rows rows (128 or 256; 0 = no such launch), their contexts in up to *pieces.
  */

@@ -91,11 +91,12 @@ def seen(p, window, sinks):
 
 
 def attention(Q, arrays, table, offsets, positions, scale, window, sinks):
-    """oracle_paged.attention where a row at position p attends over the tokens of seen(p, window, sinks)."""
+    """oracle_paged.attention where a row at position p attends over the tokens of seen(p, window, sinks).  (O, A, S): S is the same average over the values' scales, what fp32 sums of
+    codes are off by is measured in."""
     Q = np.asarray(Q, np.float64)
     heads, page = arrays[0].shape[1], arrays[0].shape[2]
     cap = table.shape[1] * page
-    O, A = np.full(Q.shape, np.nan), np.full(Q.shape, np.nan)
+    O, A, S = np.full(Q.shape, np.nan), np.full(Q.shape, np.nan), np.full(Q.shape, np.nan)
     G = Q.shape[1] // heads
     for b in range(len(positions)):
         n = int(offsets[b + 1]) - int(offsets[b])
@@ -104,6 +105,8 @@ def attention(Q, arrays, table, offsets, positions, scale, window, sinks):
             continue
         with np.errstate(invalid="ignore", over="ignore"):
             K, V, ok = op.gather(arrays, table[b], last)
+        t = np.arange(last)
+        scales = np.abs(arrays[4].astype(np.float64))[np.where(ok, np.asarray(table[b])[t // page], 0), :, t % page]
         for i in range(n):
             p, row = int(positions[b]) + i, int(offsets[b]) + i
             if not 0 <= p < cap:
@@ -113,10 +116,11 @@ def attention(Q, arrays, table, offsets, positions, scale, window, sinks):
             for hk in range(heads):
                 rows = slice(hk * G, (hk + 1) * G)
                 if not len(use):
-                    O[row, rows] = A[row, rows] = 0.0
+                    O[row, rows] = A[row, rows] = S[row, rows] = 0.0
                     continue
                 x = Q[row, rows] @ K[use, hk].T * float(scale)
                 e = np.exp(x - x.max(1, keepdims=True))
                 e /= e.sum(1, keepdims=True)
                 O[row, rows], A[row, rows] = e @ V[use, hk], e @ np.abs(V[use, hk])
-    return O, A
+                S[row, rows] = (e @ scales[use, hk])[:, None]
+    return O, A, S

@@ -803,9 +803,10 @@ def tm_paged_read(cache: PagedCache, batch: PagedBatch, K, V, stream=None):
     return (_calls or _native()).paged_read(cache, batch, K, V, stream)
 
 
-def tm_paged_attn(Q, cache: PagedCache, batch: PagedBatch, O, scale: float, stream=None):
-    """Causal attention of the batch's new tokens over their pages: Q (rows may lie apart), O float16 [tokens, q_heads, 128] -> O."""
-    return (_calls or _native()).paged_attn(Q, cache, batch, O, scale, stream)
+def tm_paged_attn(Q, cache: PagedCache, batch: PagedBatch, O, scale: float, stream=None, window: int = None, sinks: int = 0):
+    """Causal attention of the batch's new tokens over their pages: Q (rows may lie apart), O float16 [tokens, q_heads, 128] -> O.  With a window (>= 1) a
+    token sees the last `window` tokens, its own among them, and the first `sinks` (tm_paged_attn_window)."""
+    return (_calls or _native()).paged_attn(Q, cache, batch, O, scale, stream, window, sinks)
 
 
 def tm_get_paged_plan(cache: PagedCache, batch: PagedBatch, tokens: int, q_heads: int):

@@ -34,7 +34,9 @@ struct PagedWhere {
     int b, hk;
 };
 
-template <int BITS, int RW, bool PAGED>
+// WINDOW (paged): a row attends over the first tokens and those of its window; stages that no row of the CTA sees are left out (`hidden`), and job.first_stage and job.stages count what
+// is left.  Runs of a stage that none sees are not read either.
+template <int BITS, int RW, bool PAGED, bool WINDOW = false>
 __device__ __forceinline__ void attn_rows(const RowsJob& job, const uint8_t* kcodes, const uint8_t* vcodes, const uint32_t* words, const PagedWhere& where, int len_all,
                                           float scale_log2e, unsigned char* smem)
 {
@@ -52,7 +54,10 @@ __device__ __forceinline__ void attn_rows(const RowsJob& job, const uint8_t* kco
     const long pos0 = job.pos0;
     const int tok_first = row0 / G;
     const int nst = job.stages;
-    const int tok0 = PAGED ? job.first_stage * ST : 0;      // first token of the piece
+    const int tok0 = PAGED && !WINDOW ? job.first_stage * ST : 0;      // first token of the piece
+    const int sinks = WINDOW ? where.seqs.sinks : 0, tile_first = WINDOW ? (int)min(max(pos0 + tok_first, 0L), (long)job.cap) : 0;
+    const Hidden hidden(where.seqs, tile_first, ST);
+    auto token_of = [&](int st) { return WINDOW ? hidden.real(job.first_stage + st) * ST : tok0 + st * ST; };      // first of a stage
 
     // this wave's rows, and this lane's
     const int w0 = row0 + rg * 32;
@@ -66,6 +71,7 @@ __device__ __forceinline__ void attn_rows(const RowsJob& job, const uint8_t* kco
     const long pos = pos0 + tok;
     const bool real = tok < cnt && pos >= 0 && pos < job.cap;
     const int len = real ? (int)pos + 1 : 0;
+    const int lo = WINDOW ? len - where.seqs.window : 0, most_lo = WINDOW ? wlen - where.seqs.window : 0;      // the row's window begins there, the wave's last one
     if (!real) tok = tok_first;                                                     // an address that exists
     const uint16_t* const qrow = job.q + tok * job.q_stride + head * kHeadDim;
 
@@ -97,8 +103,9 @@ __device__ __forceinline__ void attn_rows(const RowsJob& job, const uint8_t* kco
         if constexpr (PAGED) {
 #pragma unroll
             for (int n = 0; n < 2; ++n) {
-                const int run = (tok0 >> 5) + 2 * st + n;
+                const int run = (token_of(st) >> 5) + n;
                 if (run * kRun >= len_all) continue;
+                if (WINDOW && run * kRun >= sinks && (run + 1) * kRun <= tile_first - where.seqs.window + 1) continue;
                 const int page = run >> where.pool.run_log;
                 if (page >= ids_at + 64) {
                     ids_at = page;
@@ -286,13 +293,19 @@ __device__ __forceinline__ void attn_rows(const RowsJob& job, const uint8_t* kco
         for (int e = 0; e < 16; ++e) x[e] = __builtin_fmaf(s[e], ks[e >> 2][e & 3], -ref);
         if (masked) {
 #pragma unroll
-            for (int e = 0; e < 16; ++e) x[e] = ((e >> 2) & 1) * 16 + (e >> 3) * 8 + (e & 3) < rem ? x[e] : kNegBig;
+            for (int e = 0; e < 16; ++e) {
+                const int at = ((e >> 2) & 1) * 16 + (e >> 3) * 8 + (e & 3);
+                bool live = at < rem;
+                if constexpr (WINDOW) live = live && (at + t0 + 4 * hl >= lo || at + t0 + 4 * hl < sinks);
+                x[e] = live ? x[e] : kNegBig;
+            }
         }
         mx = x[0];
 #pragma unroll
         for (int e = 1; e < 16; ++e) mx = fmaxf(mx, x[e]);
     };
-    auto first_token = [&](int st, int sub) { return tok0 + st * ST + (KS > 1 ? ksg : sub) * 32; };
+    auto first_token = [&](int st, int sub) { return token_of(st) + (KS > 1 ? ksg : sub) * 32; };
+    auto at_edge = [&](int t0) { return t0 + 32 > wmin || (WINDOW && t0 < most_lo && t0 + 32 > sinks); };           // not every row sees all 32
     auto is_there = [&](int st, int sub) { return !PAGED || (present >> (2 * (st & 3) + (KS > 1 ? ksg : sub)) & 1u); };
 
     {
@@ -361,7 +374,7 @@ __device__ __forceinline__ void attn_rows(const RowsJob& job, const uint8_t* kco
                         if (fresh) m_run = ref;
                     }
                 }
-                scale_scores(s, m_run, t_n + 32 > wmin || !there, t_n, there);
+                scale_scores(s, m_run, at_edge(t_n) || !there, t_n, there);
             }
         }
     }

@@ -657,9 +657,9 @@ PyObject* paged_read(PyObject*, PyObject* const* a, Py_ssize_t n)    // cache, b
     });
 }
 
-PyObject* paged_attn(PyObject*, PyObject* const* a, Py_ssize_t n)    // Q, cache, batch, O, scale, stream
+PyObject* paged_attn(PyObject*, PyObject* const* a, Py_ssize_t n)    // Q, cache, batch, O, scale, stream, window (None: none), sinks
 {
-    return entry(n, 6, n > 3 ? a[3] : Py_None, [&] {
+    return entry(n, 8, n > 3 ? a[3] : Py_None, [&] {
         const at::Tensor &Q = tensor(a[0], "Q"), &O = tensor(a[3], "O");
         if (Q.dim() != 3 || Q.size(2) != 128 || O.sizes() != Q.sizes()) raise(PyExc_ValueError, "Q and O must be [tokens][q_heads][128]");
         const Sequences seqs(a[2], Q.size(0));
@@ -670,7 +670,17 @@ PyObject* paged_attn(PyObject*, PyObject* const* a, Py_ssize_t n)    // Q, cache
         const int q_heads = Sequences::whole(Q.size(1), "q_heads");
         const float scale = (float)as_double(a[4]);
         const tm_stream st = stream_of(a[5]);
-        call([&] { return tm_paged_attn(q.p, q.stride, h, &seqs.b, o, q_heads, scale, st); });
+        auto whole = [](PyObject* v, const char* what) {
+            const long long x = as_int(v);
+            if (x < -0x7fffffffLL || x > 0x7fffffffLL) {
+                PyErr_Format(PyExc_ValueError, "%s = %lld out of range", what, x);
+                throw Failed{};
+            }
+            return (int)x;
+        };
+        const int window = a[6] == Py_None ? 0x7fffffff : whole(a[6], "window"), sinks = whole(a[7], "sinks");
+        if (a[6] == Py_None && sinks) raise(PyExc_ValueError, "sinks without a window");
+        call([&] { return tm_paged_attn_window(q.p, q.stride, h, &seqs.b, o, q_heads, scale, window, sinks, st); });
     });
 }
 

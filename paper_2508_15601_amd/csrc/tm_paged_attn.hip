@@ -18,45 +18,14 @@
 // skewed ones up to 16384, 4-bit 56 us (5.2 TB/s); one of 2048, 8-bit 8.8 us; 12 x 5 drafted tokens after 3000 to 6000, 40 / 8 heads, 8-bit 34 us (3.4 TB/s), 4-bit 27; 32 x 5 after 4000 to
 // 8000, 32 / 8 heads, 91 and 68.  Long contexts are bound by memory (a large copy reaches 5.2 TB/s, both ways together); short ones by a launch, a plan, a chain of three round trips to memory (lengths, page numbers, blocks) and the
 // meeting of the pieces, 8 us together; tiles of 32 columns by instruction issue, the codes being converted for each half.
-#include "tm_paged_columns_impl.h"
+#include "tm_paged_columns_launch.h"
 
 namespace tmw4 {
-
-namespace {
-
-template <int BITS, bool PACK, int PARTS, int TILES, bool ALONE>
-__global__ __launch_bounds__(256 * TILES) __attribute__((amdgpu_waves_per_eu(BITS == 4 && PACK ? 1 : 2, 2))) void paged_columns_kernel(
-    PagedPool pool, PagedSeqs seqs, const uint16_t* __restrict__ Q, long q_stride, uint16_t* __restrict__ O, int q_heads, float scale_log2e, int most_rows,
-    float* __restrict__ partial, uint32_t* __restrict__ counters)
-{
-    paged_columns<BITS, PACK, PARTS, TILES, ALONE, 4 * TILES>(pool, seqs, Q, q_stride, O, q_heads, scale_log2e, most_rows, partial, counters, blockIdx.x, gridDim.x);
-}
-
-}  // namespace
 
 hipError_t launch_paged_columns(const PagedPool& pool, const PagedSeqs& seqs, const uint16_t* Q, long q_stride, uint16_t* O, int q_heads, float scale, int columns,
                                 int most_rows, int grid, bool alone, void* workspace, hipStream_t stream)
 {
-    static_assert(3 * kPagedMostWaves * sizeof(uint32_t) <= kPagedLengthAt && 3 * kPagedMostCtas <= 3 * kPagedMostWaves, "three counters a wave or CTA");
-    static_assert(2 * kPagedMostCtas * (2 * 32 + 2 * 2048) * sizeof(float) <= kPagedColumnBytes, "two slots a CTA");
-    static_assert(2 * kPagedMostWaves * (2 * 16 + 2048) * sizeof(float) <= kPagedColumnBytes, "two slots a wave");
-    if (grid < 1 || grid > (alone ? kPagedMostWaves / 4 : kPagedMostCtas) || (alone && columns == 32)) return hipErrorInvalidValue;
-    uint32_t* const counters = (uint32_t*)workspace;
-    float* const partial = (float*)((char*)workspace + kPagedCounterBytes);
-    const float s = scale * 1.4426950408889634f;
-    auto pick = [&](auto bits, auto parts) {
-        constexpr int BITS = decltype(bits)::value, PARTS = decltype(parts)::value;
-        if (alone) return columns == 8 ? paged_columns_kernel<BITS, true, PARTS, 1, true> : paged_columns_kernel<BITS, false, PARTS, 1, true>;
-        return columns == 8    ? paged_columns_kernel<BITS, true, PARTS, 1, false>
-               : columns == 16 ? paged_columns_kernel<BITS, false, PARTS, 1, false>
-                               : paged_columns_kernel<BITS, false, PARTS, 2, false>;
-    };
-    typedef std::integral_constant<int, 1> One;
-    typedef std::integral_constant<int, 2> Two;
-    const auto kernel = pool.bits == 8 ? pick(std::integral_constant<int, 8>{}, One{})
-                        : pool.run_log == 0 ? pick(std::integral_constant<int, 4>{}, Two{}) : pick(std::integral_constant<int, 4>{}, One{});
-    hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(columns == 32 ? 512 : 256), 0, stream, pool, seqs, Q, q_stride, O, q_heads, s, most_rows, partial, counters);
-    return hipGetLastError();
+    return launch_columns<false>(pool, seqs, Q, q_stride, O, q_heads, scale, columns, most_rows, grid, alone, workspace, stream);
 }
 
 }  // namespace tmw4

@@ -97,13 +97,13 @@ struct Columns {
 #pragma unroll
         for (int i = 0; i < 8; ++i) acc[i] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
-    template <int PARTS, int STEP>
-    __device__ __forceinline__ void block(const BlockRegs& r, const uint32_t* words, const Magic& mg, int blk, int len, int len_all, int lane, uint32_t present)
+    template <int PARTS, int STEP, bool WINDOW>
+    __device__ __forceinline__ void block(const BlockRegs& r, const uint32_t* words, const Magic& mg, int blk, int len, int len_all, int lane, uint32_t present, int lo)
     {
         if constexpr (PARTS == 1)
-            process_block<BITS, PACK, false, STEP>(r, words, qf, scale_log2e, qsum, neg_qbias, mg, blk, present ? len : 0, len_all, lane, st, acc);
+            process_block<BITS, PACK, false, STEP, WINDOW>(r, words, qf, scale_log2e, qsum, neg_qbias, mg, blk, present ? len : 0, len_all, lane, st, acc, ~0u, lo);
         else
-            process_block<BITS, PACK, true, STEP>(r, words, qf, scale_log2e, qsum, neg_qbias, mg, blk, len, len_all, lane, st, acc, present);
+            process_block<BITS, PACK, true, STEP, WINDOW>(r, words, qf, scale_log2e, qsum, neg_qbias, mg, blk, len, len_all, lane, st, acc, present, lo);
     }
     // The four waves that share the columns meet in LDS: wave `wave` gets the unnormalised values o[i] of dimensions 16 * (2 * wave + i) + 4 * (lane / 16) ... of its lane's column, the
     // reference M and the denominator L.  (One barrier; another has to follow before the next segment's.)
@@ -173,7 +173,9 @@ struct Columns {
 // the other read it twice: 12 x 5 drafted tokens after 6000, 25 columns, 8-bit codes: 45 us, like this 36.  The codes are then not loaded as data that nobody else wants, which
 // cost the second wave a quarter of its hits: 32 x 5 after 8000 120 us, so 104.)
 // block, blocks: the CTA and how many there are; WAVES: of a CTA.
-template <int BITS, bool PACK, int PARTS, int TILES, bool ALONE, int WAVES>
+// WINDOW: quads that none of a sequence's new tokens sees are left out, and what is left is numbered through; a block that its tile does not see is not read.  A block that holds
+// first tokens and tokens of windows is taken in two steps, so that the tokens a column sees are a range in each.
+template <int BITS, bool PACK, int PARTS, int TILES, bool ALONE, int WAVES, bool WINDOW = false>
 __device__ __forceinline__ void paged_columns(const PagedPool& pool, const PagedSeqs& seqs, const uint16_t* __restrict__ Q, long q_stride, uint16_t* __restrict__ O, int q_heads,
                                               float scale_log2e, int most_rows, float* __restrict__ partial, uint32_t* __restrict__ counters, uint32_t block, uint32_t blocks)
 {
@@ -202,7 +204,10 @@ __device__ __forceinline__ void paged_columns(const PagedPool& pool, const Paged
 
     // ---- this CTA's piece of the work
     auto tiles_of = [&](const PagedSeq& s) { return s.count * G <= most_rows ? (s.count * G + COLS - 1) / COLS : 0; };
-    auto quads_of = [&](const PagedSeq& s) { return (max(s.last(seqs.cap), 0) + kStep * TOK - 1) / (kStep * TOK); };
+    auto quads_of = [&](const PagedSeq& s) {
+        const int quads = (max(s.last(seqs.cap), 0) + kStep * TOK - 1) / (kStep * TOK);
+        return WINDOW ? quads - Hidden(seqs, s.first(), kStep * TOK).count : quads;
+    };
     const uint32_t ctas = ALONE ? WAVES * blocks : blocks, me = ALONE ? WAVES * block + any_wave : block;      // CTAs, or waves, that share the work
     // Up to 64 sequences a lane holds one, loaded once: a launch of few short contexts is a chain of memory round trips, and this one is its first.
     const bool one_each = seqs.batch <= 64;
@@ -277,7 +282,12 @@ __device__ __forceinline__ void paged_columns(const PagedPool& pool, const Paged
         const int len_all = (int)min(max((long)s.pos + last_tok + 1, 0L), (long)seqs.cap);
         Form form;
         form.request_query(Q + (size_t)(s.row + col.tok) * q_stride + ((size_t)hk * G + col.head) * kHeadDim, lane);
-        const int blk1 = min((int)qb * kStep, (len_all + TOK - 1) / TOK);
+        const Hidden hidden(seqs, WINDOW ? s.first() : 0, kStep * TOK);
+        const int hidden_from = hidden.from * kStep, hidden_blocks = hidden.count * kStep;
+        auto real = [&](int k) { return WINDOW && k >= hidden_from ? k + hidden_blocks : k; };
+        const int tile_lo = WINDOW ? (int)min(max((long)s.pos + r0 / G, 0L), (long)seqs.cap) - seqs.window + 1 : 0;      // of the tile's first row; the lane's:
+        const int lo = WINDOW ? len - seqs.window : 0;
+        const int blk1 = min((int)qb * kStep, (len_all + TOK - 1) / TOK - (WINDOW ? hidden_blocks : 0));
         int blk = (int)qa * kStep + wave;
 
         constexpr uint32_t kPart = 4096 / PARTS, kPartTokens = TOK / PARTS;
@@ -286,7 +296,7 @@ __device__ __forceinline__ void paged_columns(const PagedPool& pool, const Paged
         auto pages_of = [&](int k) {
             BlockPages<PARTS> p;
 #pragma unroll
-            for (int n = 0; n < PARTS; ++n) p.id[n] = paged_entry(pool, seqs, b, min(k * PARTS + n, last_part) * (RUNS / PARTS));
+            for (int n = 0; n < PARTS; ++n) p.id[n] = paged_entry(pool, seqs, b, min(real(k) * PARTS + n, last_part) * (RUNS / PARTS));
             return p;
         };
         // Requests a block; a part that is not there is a buffer of no bytes, whose loads return zeros without memory traffic.  Returns which parts are there.
@@ -296,9 +306,11 @@ __device__ __forceinline__ void paged_columns(const PagedPool& pool, const Paged
             asm volatile("" : "+v"(off));
 #pragma unroll
             for (int n = 0; n < PARTS; ++n) {
-                const bool ok = k < blk1 && k * PARTS + n <= last_part && (uint32_t)p.id[n] < (uint32_t)pool.pages;
+                const int at = real(k) * PARTS + n;
+                bool ok = k < blk1 && at <= last_part && (uint32_t)p.id[n] < (uint32_t)pool.pages;
+                if constexpr (WINDOW) ok = ok && ((at + 1) * (int)kPartTokens > tile_lo || at * (int)kPartTokens < seqs.sinks);
                 present |= (uint32_t)ok << n;
-                const size_t run = paged_run(pool, ok ? p.id[n] : 0, hk, k * RUNS + n);
+                const size_t run = paged_run(pool, ok ? p.id[n] : 0, hk, real(k) * RUNS + n);
                 const __amdgpu_buffer_rsrc_t rk = make_rsrc(pool.k + run * (512 * BITS), ok ? kPart : 0u), rv = make_rsrc(pool.v + run * (512 * BITS), ok ? kPart : 0u),
                                              rz = make_rsrc(pool.pairs + run * kRun * 2, ok ? kPartTokens * 8u : 0u);
 #if defined(__HIP_DEVICE_COMPILE__)
@@ -331,7 +343,16 @@ __device__ __forceinline__ void paged_columns(const PagedPool& pool, const Paged
             const int fill = (use + 2) % 3;
             there[fill] = load(g[fill], ring(fill), blk + 2 * kStep, next);
             next = pages_of(blk + 3 * kStep);
-            form.template block<PARTS, kStep>(g[use], ring(use), mg, blk, len, len_all, lane, there[use]);
+            if constexpr (WINDOW) {
+                const int k = real(blk);
+                // first tokens, then the window's; both parts may be there (uniform)
+                for (int part = k * TOK < seqs.sinks ? 0 : 1; part < ((k + 1) * TOK > seqs.sinks ? 2 : 1); ++part) {
+                    const int from = part ? max(lo, seqs.sinks) : 0, to = part ? len : min(len, seqs.sinks);
+                    form.template block<PARTS, kStep, true>(g[use], ring(use), mg, k, max(to, from), len_all, lane, there[use], from);
+                }
+            } else {
+                form.template block<PARTS, kStep, false>(g[use], ring(use), mg, blk, len, len_all, lane, there[use], 0);
+            }
             blk += kStep;
             return blk < blk1;
         };

@@ -23,6 +23,18 @@ struct PagedSeqs {
     const int32_t* offsets;              // [batch + 1]
     const int32_t* positions;            // [batch]
     int batch, max_pages, tokens, cap;   // cap = tokens a row of the table can hold
+    int window, sinks;                   // kernels of a sliding window: the token at p sees tokens p - window + 1 .. p and 0 .. sinks - 1, both at most cap
+};
+
+// Pieces of `size` tokens that nobody from position `first` on sees: between the first tokens and the window.  What is left is numbered through.
+struct Hidden {
+    int from, count;                     // pieces 0 .. from - 1 are seen, the next `count` are not
+    __device__ __forceinline__ Hidden(const PagedSeqs& s, int first, int size)
+    {
+        from = (s.sinks + size - 1) / size;
+        count = max(max(min(first, s.cap - 1) - s.window + 1, 0) / size - from, 0);
+    }
+    __device__ __forceinline__ int real(int piece) const { return piece < from ? piece : piece + count; }
 };
 
 // An element of an array that no kernel of the launch writes.  With a wave-uniform index it is a scalar load, whatever the kernel stores elsewhere: as a vector load it would

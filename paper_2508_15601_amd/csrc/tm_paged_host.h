@@ -79,6 +79,10 @@ hipError_t launch_paged_read(const PagedPool& pool, const PagedSeqs& seqs, uint1
 hipError_t launch_paged_columns(const PagedPool& pool, const PagedSeqs& seqs, const uint16_t* Q, long q_stride, uint16_t* O, int q_heads, float scale, int columns,
                                 int most_rows, int grid, bool alone, void* workspace, hipStream_t stream);
 
+// The same in a sliding window.
+hipError_t launch_paged_columns_window(const PagedPool& pool, const PagedSeqs& seqs, const uint16_t* Q, long q_stride, uint16_t* O, int q_heads, float scale, int columns,
+                                       int most_rows, int grid, bool alone, void* workspace, hipStream_t stream);
+
 // How a call is divided: sequences with at least least_rows rows in CTAs of 32 * row_waves rows (row_waves = 0: none), the others by columns (column_rows = 0: none).
 struct PagedForm {
     int columns, column_rows, column_ctas;
@@ -88,6 +92,12 @@ struct PagedForm {
 };
 PagedForm paged_form(const PagedPool& pool, const PagedSeqs& seqs, int q_heads, int max_count, int max_len, int num_cu);
 hipError_t paged_rows_setup();                                         // once per device, outside any capture
+hipError_t paged_rows_window_setup();
+hipError_t launch_paged_rows(const PagedPool& pool, const PagedSeqs& seqs, const uint16_t* Q, long q_stride, uint16_t* O, int q_heads, float scale, const PagedForm& f, void* workspace,
+                             hipStream_t stream);
+hipError_t launch_paged_rows_window(const PagedPool& pool, const PagedSeqs& seqs, const uint16_t* Q, long q_stride, uint16_t* O, int q_heads, float scale, const PagedForm& f,
+                                    void* workspace, hipStream_t stream);
+// seqs.window = seqs.cap: without a window
 hipError_t launch_paged_attn(const PagedPool& pool, const PagedSeqs& seqs, const uint16_t* Q, long q_stride, uint16_t* O, int q_heads, float scale, int max_count, int max_len,
                              int num_cu, void* workspace, hipStream_t stream);
 

@@ -1,4 +1,5 @@
 // C ABI of libtm_w4: argument checking, handle and workspace management, kernel selection.
+#include <limits.h>
 #include <math.h>
 #include <stdarg.h>
 #include <stdio.h>
@@ -2233,7 +2234,7 @@ static int check_paged(const tm_paged_cache* cache, const tm_paged_batch* b, Pag
         b->max_len < 0)
         return fail(TM_EINVAL, "need 1 <= batch <= 65535, max_pages > 0, max_pages * %d < 2^30, tokens, max_count, max_len >= 0 (got %d, %d, %d, %d, %d)", 1 << page_log,
                     b->batch, b->max_pages, b->tokens, b->max_count, b->max_len);
-    *seqs = PagedSeqs{b->table, b->offsets, b->positions, b->batch, b->max_pages, b->tokens, b->max_pages << page_log};
+    *seqs = PagedSeqs{b->table, b->offsets, b->positions, b->batch, b->max_pages, b->tokens, b->max_pages << page_log, b->max_pages << page_log, 0};
     return TM_OK;
 }
 
@@ -2375,9 +2376,17 @@ static int check_paged_attn(const tm_paged_cache* cache, const tm_paged_batch* b
 
 int tm_paged_attn(const uint16_t* Q, int64_t q_stride, const tm_paged_cache* cache, const tm_paged_batch* batch, uint16_t* O, int q_heads, float scale, tm_stream stream)
 {
+    return tm_paged_attn_window(Q, q_stride, cache, batch, O, q_heads, scale, INT_MAX, 0, stream);
+}
+
+int tm_paged_attn_window(const uint16_t* Q, int64_t q_stride, const tm_paged_cache* cache, const tm_paged_batch* batch, uint16_t* O, int q_heads, float scale, int window, int sinks,
+                         tm_stream stream)
+{
     PagedSeqs seqs;
     int rc = check_paged_attn(cache, batch, q_heads, &seqs);
     if (rc != TM_OK) return rc;
+    if (window < 1 || sinks < 0) return fail(TM_EINVAL, "need window >= 1 and sinks >= 0 (got %d, %d)", window, sinks);
+    if ((int64_t)window + sinks < seqs.cap) seqs.window = window, seqs.sinks = sinks;      // otherwise every token sees all before it
     if (!(scale > 0.0f) || !(scale < 1.0e6f)) return fail(TM_EINVAL, "scale out of range");
     if (seqs.tokens == 0) return TM_OK;
     rc = check_rows("Q", Q, q_stride, (int64_t)q_heads * 128);
