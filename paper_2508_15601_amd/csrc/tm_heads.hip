@@ -8,33 +8,31 @@ namespace tmw4 {
 
 namespace {
 
-// Heads 0 .. q.heads - 1 are queries, those behind them keys.  A wave takes `rounds` times 64 / LANES heads of one token; LANES lanes hold a head, sixteen dimensions each.  A lane's dimensions
-// are the same in every round, so the cosines and sines of its pairs stay in registers.  X and Y of a side may be the same.
-template <int LANES>
+// A wave takes `rounds` times 64 / LANES heads of one token, queries first; LANES lanes hold a head, sixteen dimensions each.  A lane's dimensions are the same in every round, so
+// the cosines and sines of its pairs stay in registers, and so do weights that all heads of a side share.  X and Y of a side may be the same.
+template <int LANES, bool NORM, bool INTERLEAVED>
 __global__ __launch_bounds__(256) void heads_kernel(HeadRows q, HeadRows k, const int32_t* __restrict__ positions, RopePlan r, int tokens, int dim, int rounds)
 {
     constexpr int AT_ONCE = 64 / LANES;
     __shared__ CosSin cs[4][kRopeMaxPairs];
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), u = lane & (LANES - 1);
-    const int heads = q.heads + k.heads, parts = (heads + AT_ONCE * rounds - 1) / (AT_ONCE * rounds);
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), u = lane & (LANES - 1), slot = lane / LANES;
+    const int q_rounds = (q.heads + AT_ONCE - 1) / AT_ONCE, all = q_rounds + (k.heads + AT_ONCE - 1) / AT_ONCE, parts = (all + rounds - 1) / rounds;
     const long job = (long)blockIdx.x * 4 + wave;
     const long token = job / parts;
     if (token >= tokens) return;
-    const int h0 = (int)(job - token * parts) * AT_ONCE * rounds, h1 = min(h0 + AT_ONCE * rounds, heads);
+    const int first = (int)(job - token * parts) * rounds, last = min(first + rounds, all);
     const HeadPart part(u, dim, r);
     f16x8 a, b, wa, wb;
-    auto side = [&](int h) -> const HeadRows& { return h < q.heads ? q : k; };
-    auto request = [&](int h) {
-        h = min(h, heads - 1);                               // (a head that exists)
-        const HeadRows& s = side(h);
-        if (h >= q.heads) h -= q.heads;
+    auto request = [&](int round) {
+        const bool keys = round >= q_rounds;
+        const HeadRows& s = keys ? k : q;
+        const int h = min((round - (keys ? q_rounds : 0)) * AT_ONCE + slot, s.heads - 1);      // (a head that exists)
         const uint16_t* const x = s.x + token * s.x_stride + (long)h * dim;
         a = *(const f16x8*)(x + part.d0);
         b = *(const f16x8*)(x + part.d1);
-        wa = head_weights(s.norm, h, part.d0);
-        wb = head_weights(s.norm, h, part.d1);
+        if (NORM && (s.norm.stride || round == first || round == q_rounds)) wa = head_weights(s.norm, h, part.d0), wb = head_weights(s.norm, h, part.d1);
     };
-    request(h0 + lane / LANES);
+    request(first);
     CosSin c[8] = {};
     if (r.rot) {
         rope_angles_of(cs[wave], r, positions + token * r.axes, lane);
@@ -45,28 +43,40 @@ __global__ __launch_bounds__(256) void heads_kernel(HeadRows q, HeadRows k, cons
             for (int i = 0; i < 8; ++i) c[i] = cs[wave][8 * u + i];
         }
     }
-    for (int h = h0 + lane / LANES; h < h1 + lane / LANES; h += AT_ONCE) {       // (the same number of rounds in every lane)
+    for (int round = first; round < last; ++round) {
         f16x8 y0 = a, y1 = b;
         const f16x8 w0 = wa, w1 = wb;
-        if (h + AT_ONCE < h1 + lane / LANES) request(h + AT_ONCE);
-        const HeadRows& s = side(min(h, heads - 1));
-        head_turn<LANES>(y0, y1, w0, w1, part, s.norm, dim, r, c);
-        if (h >= h1 || !part.any) continue;
-        uint16_t* const y = s.y + token * s.y_stride + (long)(h < q.heads ? h : h - q.heads) * dim;
+        if (round + 1 < last) request(round + 1);
+        const bool keys = round >= q_rounds;
+        const HeadRows& s = keys ? k : q;
+        const int h = (round - (keys ? q_rounds : 0)) * AT_ONCE + slot;
+        if (!NORM || s.norm.on) head_turn<LANES, NORM, INTERLEAVED>(y0, y1, w0, w1, part, s.norm, dim, c);
+        else head_turn<LANES, false, INTERLEAVED>(y0, y1, w0, w1, part, s.norm, dim, c);
+        if (h >= s.heads || !part.any) continue;
+        uint16_t* const y = s.y + token * s.y_stride + (long)h * dim;
         *(f16x8*)(y + part.d0) = y0;
         if (part.whole) *(f16x8*)(y + part.d1) = y1;
     }
+}
+
+template <int LANES>
+auto pick(bool norm, bool interleaved)
+{
+    return norm ? interleaved ? heads_kernel<LANES, true, true> : heads_kernel<LANES, true, false>
+                : interleaved ? heads_kernel<LANES, false, true> : heads_kernel<LANES, false, false>;
 }
 
 }  // namespace
 
 hipError_t launch_heads(const HeadRows& q, const HeadRows& k, const int32_t* positions, const RopePlan& r, int tokens, int dim, hipStream_t stream)
 {
-    const int lanes = dim <= 16 ? 1 : dim <= 32 ? 2 : dim <= 64 ? 4 : dim <= 128 ? 8 : 16, at_once = 64 / lanes, heads = q.heads + k.heads;
+    const int lanes = dim <= 16 ? 1 : dim <= 32 ? 2 : dim <= 64 ? 4 : dim <= 128 ? 8 : 16, at_once = 64 / lanes;
+    const int all = (q.heads + at_once - 1) / at_once + (k.heads + at_once - 1) / at_once;
     // one round of a wave's lanes at a time where tokens are few
-    const int all = (heads + at_once - 1) / at_once, rounds = (long)tokens * all >= 16384L ? all : 1;
-    const long parts = (heads + at_once * rounds - 1) / (at_once * rounds), most = 4 * most_ctas(256) / parts;       // tokens of a launch
-    const auto kernel = lanes == 1 ? heads_kernel<1> : lanes == 2 ? heads_kernel<2> : lanes == 4 ? heads_kernel<4> : lanes == 8 ? heads_kernel<8> : heads_kernel<16>;
+    const int rounds = (long)tokens * all >= 16384L ? all : 1;
+    const long parts = (all + rounds - 1) / rounds, most = 4 * most_ctas(256) / parts;       // tokens of a launch
+    const auto of = lanes == 1 ? pick<1> : lanes == 2 ? pick<2> : lanes == 4 ? pick<4> : lanes == 8 ? pick<8> : pick<16>;
+    const auto kernel = of(q.norm.on || k.norm.on, r.interleaved);
     for (long t = 0; t < tokens; t += most) {
         const int n = (int)std::min(most, tokens - t);
         auto from = [&](HeadRows s) {

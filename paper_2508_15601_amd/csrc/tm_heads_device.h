@@ -43,24 +43,46 @@ __device__ __forceinline__ double lanes_sum(double v)
     return v;
 }
 
+// 1 / sqrt(v) for v of at least 1e-300: the hardware's approximation and two steps of Newton's iteration.
+__device__ __forceinline__ double inverse_root(double v)
+{
+#if defined(__HIP_DEVICE_COMPILE__)
+    double y = __builtin_amdgcn_rsq(v);
+    const double half = 0.5 * v;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) y = __builtin_fma(y, __builtin_fma(-half * y, y, 0.5), y);
+    return v < __builtin_inf() ? y : v != v ? v : 0.0;       // (the steps make an infinity times zero)
+#else
+    return v;
+#endif
+}
+
 // Mean (0 unless centred) and factor of a head of dim values, `count` of them this lane's.
 template <int LANES, int N>
 __device__ __forceinline__ void head_norm(const double (&x)[N], int count, const HeadNorm& n, int dim, double& mean, double& factor)
 {
+    const bool full = dim == LANES * N;                      // (uniform) every lane has N
+    const double share = 1.0 / dim;
     mean = 0.0;
-    if (n.centred) {
-        double s = 0.0;
-#pragma unroll
-        for (int i = 0; i < N; ++i) s += i < count ? x[i] : 0.0;
-        mean = lanes_sum<LANES>(s) / dim;
-    }
     double s = 0.0;
+    if (n.centred) {
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-        const double d = x[i] - mean;
-        s += i < count ? d * d : 0.0;
+        for (int i = 0; i < N; ++i) s += full || i < count ? x[i] : 0.0;
+        mean = lanes_sum<LANES>(s) * share;
+        s = 0.0;
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const double d = x[i] - mean;
+            s += full || i < count ? d * d : 0.0;
+        }
+    } else if (full) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) s = __builtin_fma(x[i], x[i], s);
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; ++i) s += i < count ? x[i] * x[i] : 0.0;
     }
-    factor = 1.0 / sqrt(lanes_sum<LANES>(s) / dim + n.eps);
+    factor = inverse_root(__builtin_fma(lanes_sum<LANES>(s), share, n.eps));
 }
 
 __device__ __forceinline__ f16x8 head_weights(const HeadNorm& n, int head, int d)
@@ -88,39 +110,53 @@ struct HeadPart {
 };
 
 // a, b: the part's vectors, wa, wb: their weights; cs: cosines and sines of the token's pairs.  Every lane of a head takes part.
-template <int LANES>
-__device__ __forceinline__ void head_turn(f16x8& a, f16x8& b, const f16x8& wa, const f16x8& wb, const HeadPart& p, const HeadNorm& n, int dim, const RopePlan& r, const CosSin (&cs)[8])
+template <int LANES, bool NORM, bool INTERLEAVED>
+__device__ __forceinline__ void head_turn(f16x8& a, f16x8& b, const f16x8& wa, const f16x8& wb, const HeadPart& p, const HeadNorm& n, int dim, const CosSin (&cs)[8])
 {
     double x[16];
 #pragma unroll
     for (int i = 0; i < 8; ++i) x[i] = (double)(float)a[i], x[8 + i] = (double)(float)b[i];
-    if (n.on) {
+    if constexpr (NORM) {
         double mean, factor;
         head_norm<LANES>(x, !p.any ? 0 : p.whole ? 16 : 8, n, dim, mean, factor);
+        if (n.centred) {                                     // (uniform)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) x[i] = (x[i] - mean) * (factor * (n.offset + (double)(float)(i < 8 ? wa[i] : wb[i - 8])));
-    } else if (!p.turned) {
-        return;
+            for (int i = 0; i < 16; ++i) x[i] -= mean;
+        }
+#pragma unroll
+        for (int i = 0; i < 16; ++i) x[i] *= factor * (n.offset + (double)(float)(i < 8 ? wa[i] : wb[i - 8]));
     }
     if (p.turned) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            if (r.interleaved) {
-                const double u = x[2 * i], v = x[2 * i + 1];
-                x[2 * i] = u * cs[i].c - v * cs[i].s;
-                x[2 * i + 1] = v * cs[i].c + u * cs[i].s;
-            } else {
-                const double u = x[i], v = x[8 + i];
-                x[i] = u * cs[i].c - v * cs[i].s;
-                x[8 + i] = v * cs[i].c + u * cs[i].s;
-            }
+            constexpr int STEP = INTERLEAVED ? 2 : 1, OTHER = INTERLEAVED ? 1 : 8;
+            const double u = x[STEP * i], v = x[STEP * i + OTHER];
+            x[STEP * i] = u * cs[i].c - v * cs[i].s;
+            x[STEP * i + OTHER] = v * cs[i].c + u * cs[i].s;
         }
+    } else if (!NORM) {
+        return;
     }
 #pragma unroll
     for (int i = 0; i < 8; ++i) a[i] = rope_round(x[i]), b[i] = rope_round(x[8 + i]);
 }
 
 // Heads h0 .. h1 - 1 of 128 dimensions of one token, by one wave; x and y may be the same.
+template <bool NORM, bool INTERLEAVED>
+__device__ __forceinline__ void turn_heads(const uint16_t* x, uint16_t* y, int h0, int h1, const HeadNorm& n, const HeadPart& part, const CosSin (&c)[8], int lane)
+{
+    f16x8 wa = head_weights(n, h0, part.d0), wb = head_weights(n, h0, part.d1);
+    for (int at = h0; at < h1; at += 8) {
+        const int h = min(at + (lane >> 3), h1 - 1);
+        const uint16_t* const from = x + (size_t)h * 128;
+        f16x8 a = *(const f16x8*)(from + part.d0), b = *(const f16x8*)(from + part.d1);
+        if (n.stride) wa = head_weights(n, h, part.d0), wb = head_weights(n, h, part.d1);
+        head_turn<8, NORM, INTERLEAVED>(a, b, wa, wb, part, n, 128, c);
+        if (at + (lane >> 3) >= h1) continue;
+        *(f16x8*)(y + (size_t)h * 128 + part.d0) = a;
+        *(f16x8*)(y + (size_t)h * 128 + part.d1) = b;
+    }
+}
 __device__ __forceinline__ void turn_heads(const uint16_t* x, uint16_t* y, int h0, int h1, const HeadNorm& n, const RopePlan& r, const CosSin* cs, int lane)
 {
     const HeadPart part(lane & 7, 128, r);
@@ -129,15 +165,10 @@ __device__ __forceinline__ void turn_heads(const uint16_t* x, uint16_t* y, int h
 #pragma unroll
         for (int i = 0; i < 8; ++i) c[i] = cs[8 * (lane & 7) + i];
     }
-    for (int at = h0; at < h1; at += 8) {
-        const int h = min(at + (lane >> 3), h1 - 1);
-        const uint16_t* const from = x + (size_t)h * 128;
-        f16x8 a = *(const f16x8*)(from + part.d0), b = *(const f16x8*)(from + part.d1);
-        head_turn<8>(a, b, head_weights(n, h, part.d0), head_weights(n, h, part.d1), part, n, 128, r, c);
-        if (at + (lane >> 3) >= h1) continue;
-        *(f16x8*)(y + (size_t)h * 128 + part.d0) = a;
-        *(f16x8*)(y + (size_t)h * 128 + part.d1) = b;
-    }
+    if (n.on && r.interleaved) turn_heads<true, true>(x, y, h0, h1, n, part, c, lane);
+    else if (n.on) turn_heads<true, false>(x, y, h0, h1, n, part, c, lane);
+    else if (r.interleaved) turn_heads<false, true>(x, y, h0, h1, n, part, c, lane);
+    else turn_heads<false, false>(x, y, h0, h1, n, part, c, lane);
 }
 
 // A lane's eight dimensions 8 * sub .. of head h of 128 dimensions that sixteen neighbouring lanes hold.
