@@ -94,7 +94,7 @@ TM_API int tm_rope_apply(const uint16_t* X, int64_t x_stride, const int32_t* pos
 typedef struct tm_head_norm {
     const uint16_t* weight;       /* device, fp16 [head_dim], or [heads][head_dim] with a stride; 16-byte aligned; NULL = ones */
     int64_t weight_stride;        /* values from head to head, a multiple of 8; 0 = every head has the same */
-    double eps;                   /* > 0 */
+    double eps;                   /* >= 1e-300 */
     double offset;                /* added to every weight: 0, or 1 where a checkpoint keeps weights less one */
     int centred;                  /* 0 or 1 */
 } tm_head_norm;

@@ -8,19 +8,19 @@ namespace tmw4 {
 
 namespace {
 
-// A wave takes `rounds` times 64 / LANES heads of one token, queries first; LANES lanes hold a head, sixteen dimensions each.  A lane's dimensions are the same in every round, so
-// the cosines and sines of its pairs stay in registers, and so do weights that all heads of a side share.  X and Y of a side may be the same.
-template <int LANES, bool NORM, bool INTERLEAVED>
+// A wave takes `rounds` times 64 / LANES heads of one token, queries first; LANES lanes hold a head, sixteen dimensions each.  Weights that all
+// heads of a side share stay in registers.  X and Y of a side may be the same.
+template <int LANES, int MODE, bool INTERLEAVED>
 __global__ __launch_bounds__(256) void heads_kernel(HeadRows q, HeadRows k, const int32_t* __restrict__ positions, RopePlan r, int tokens, int dim, int rounds)
 {
     constexpr int AT_ONCE = 64 / LANES;
-    __shared__ CosSin cs[4][kRopeMaxPairs];
+    __shared__ CosSin cs[4][turns_of(8 * LANES)];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), u = lane & (LANES - 1), slot = lane / LANES;
-    const int q_rounds = (q.heads + AT_ONCE - 1) / AT_ONCE, all = q_rounds + (k.heads + AT_ONCE - 1) / AT_ONCE, parts = (all + rounds - 1) / rounds;
-    const long job = (long)blockIdx.x * 4 + wave;
+    const int q_rounds = (q.heads + AT_ONCE - 1) / AT_ONCE, all = q_rounds + (k.heads + AT_ONCE - 1) / AT_ONCE;
+    const uint32_t parts = (uint32_t)(all + rounds - 1) / (uint32_t)rounds, job = blockIdx.x * 4 + wave;       // (a launch has fewer than 2^32 threads)
     const long token = job / parts;
     if (token >= tokens) return;
-    const int first = (int)(job - token * parts) * rounds, last = min(first + rounds, all);
+    const int first = (int)(job % parts) * rounds, last = min(first + rounds, all);
     const HeadPart part(u, dim, r);
     f16x8 a, b, wa, wb;
     auto request = [&](int round) {
@@ -30,18 +30,13 @@ __global__ __launch_bounds__(256) void heads_kernel(HeadRows q, HeadRows k, cons
         const uint16_t* const x = s.x + token * s.x_stride + (long)h * dim;
         a = *(const f16x8*)(x + part.d0);
         b = *(const f16x8*)(x + part.d1);
-        if (NORM && (s.norm.stride || round == first || round == q_rounds)) wa = head_weights(s.norm, h, part.d0), wb = head_weights(s.norm, h, part.d1);
+        if (MODE != kNoNorm && (s.norm.stride || round == first || round == q_rounds)) wa = head_weights(s.norm, h, part.d0), wb = head_weights(s.norm, h, part.d1);
     };
     request(first);
-    CosSin c[8] = {};
     if (r.rot) {
-        rope_angles_of(cs[wave], r, positions + token * r.axes, lane);
+        rope_angles_of<true>(cs[wave], r, positions + token * r.axes, lane);
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         __builtin_amdgcn_wave_barrier();
-        if (part.turned) {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) c[i] = cs[wave][8 * u + i];
-        }
     }
     for (int round = first; round < last; ++round) {
         f16x8 y0 = a, y1 = b;
@@ -50,8 +45,7 @@ __global__ __launch_bounds__(256) void heads_kernel(HeadRows q, HeadRows k, cons
         const bool keys = round >= q_rounds;
         const HeadRows& s = keys ? k : q;
         const int h = (round - (keys ? q_rounds : 0)) * AT_ONCE + slot;
-        if (!NORM || s.norm.on) head_turn<LANES, NORM, INTERLEAVED>(y0, y1, w0, w1, part, s.norm, dim, c);
-        else head_turn<LANES, false, INTERLEAVED>(y0, y1, w0, w1, part, s.norm, dim, c);
+        head_turn<LANES, MODE, INTERLEAVED>(y0, y1, w0, w1, part, s.norm, cs[wave] + turn_at(8 * u));
         if (h >= s.heads || !part.any) continue;
         uint16_t* const y = s.y + token * s.y_stride + (long)h * dim;
         *(f16x8*)(y + part.d0) = y0;
@@ -60,10 +54,11 @@ __global__ __launch_bounds__(256) void heads_kernel(HeadRows q, HeadRows k, cons
 }
 
 template <int LANES>
-auto pick(bool norm, bool interleaved)
+auto pick(int mode, bool interleaved)
 {
-    return norm ? interleaved ? heads_kernel<LANES, true, true> : heads_kernel<LANES, true, false>
-                : interleaved ? heads_kernel<LANES, false, true> : heads_kernel<LANES, false, false>;
+    if (mode == kNoNorm) return interleaved ? heads_kernel<LANES, kNoNorm, true> : heads_kernel<LANES, kNoNorm, false>;
+    if (mode == kPlainNorm) return interleaved ? heads_kernel<LANES, kPlainNorm, true> : heads_kernel<LANES, kPlainNorm, false>;
+    return interleaved ? heads_kernel<LANES, kAnyNorm, true> : heads_kernel<LANES, kAnyNorm, false>;
 }
 
 }  // namespace
@@ -76,7 +71,7 @@ hipError_t launch_heads(const HeadRows& q, const HeadRows& k, const int32_t* pos
     const int rounds = (long)tokens * all >= 16384L ? all : 1;
     const long parts = (all + rounds - 1) / rounds, most = 4 * most_ctas(256) / parts;       // tokens of a launch
     const auto of = lanes == 1 ? pick<1> : lanes == 2 ? pick<2> : lanes == 4 ? pick<4> : lanes == 8 ? pick<8> : pick<16>;
-    const auto kernel = of(q.norm.on || k.norm.on, r.interleaved);
+    const auto kernel = of(!q.norm.on && !k.norm.on ? kNoNorm : !q.norm.centred && !k.norm.centred ? kPlainNorm : kAnyNorm, r.interleaved);
     for (long t = 0; t < tokens; t += most) {
         const int n = (int)std::min(most, tokens - t);
         auto from = [&](HeadRows s) {

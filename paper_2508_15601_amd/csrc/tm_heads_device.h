@@ -12,7 +12,7 @@ namespace tmw4 {
 struct HeadNorm {                        // off: a head's values as they are
     const uint16_t* w;                   // fp16 weights of head 0, nullptr: ones
     long stride;                         // from head to head, 0: all have the same
-    double eps, offset;
+    double eps, offset, share;           // share: 1 / dimensions of a head
     int on, centred;
 };
 
@@ -57,32 +57,26 @@ __device__ __forceinline__ double inverse_root(double v)
 #endif
 }
 
-// Mean (0 unless centred) and factor of a head of dim values, `count` of them this lane's.
-template <int LANES, int N>
-__device__ __forceinline__ void head_norm(const double (&x)[N], int count, const HeadNorm& n, int dim, double& mean, double& factor)
+// Mean (0 unless CENTRED) and factor of a head, of which this lane holds x[0 .. N - 1]: the first half if `any`, the second if `whole`.
+template <int LANES, bool CENTRED, int N>
+__device__ __forceinline__ void head_norm(const double (&x)[N], bool any, bool whole, const HeadNorm& n, double& mean, double& factor)
 {
-    const bool full = dim == LANES * N;                      // (uniform) every lane has N
-    const double share = 1.0 / dim;
+    auto sum = [&](auto f) {
+        double a = 0.0, b = 0.0;
+#pragma unroll
+        for (int i = 0; i < N / 2; ++i) a = f(x[i], a), b = f(x[N / 2 + i], b);
+        return lanes_sum<LANES>((any ? a : 0.0) + (whole ? b : 0.0)) * n.share;
+    };
     mean = 0.0;
-    double s = 0.0;
-    if (n.centred) {
-#pragma unroll
-        for (int i = 0; i < N; ++i) s += full || i < count ? x[i] : 0.0;
-        mean = lanes_sum<LANES>(s) * share;
-        s = 0.0;
-#pragma unroll
-        for (int i = 0; i < N; ++i) {
-            const double d = x[i] - mean;
-            s += full || i < count ? d * d : 0.0;
-        }
-    } else if (full) {
-#pragma unroll
-        for (int i = 0; i < N; ++i) s = __builtin_fma(x[i], x[i], s);
-    } else {
-#pragma unroll
-        for (int i = 0; i < N; ++i) s += i < count ? x[i] * x[i] : 0.0;
+    if constexpr (CENTRED) {
+        mean = sum([](double v, double s) { return s + v; });
+        mean = n.centred ? mean : 0.0;
     }
-    factor = inverse_root(__builtin_fma(lanes_sum<LANES>(s), share, n.eps));
+    factor = inverse_root(sum([&](double v, double s) {
+                              const double d = CENTRED ? v - mean : v;
+                              return __builtin_fma(d, d, s);
+                          }) +
+                          n.eps);
 }
 
 __device__ __forceinline__ f16x8 head_weights(const HeadNorm& n, int head, int d)
@@ -109,49 +103,51 @@ struct HeadPart {
     }
 };
 
-// a, b: the part's vectors, wa, wb: their weights; cs: cosines and sines of the token's pairs.  Every lane of a head takes part.
-template <int LANES, bool NORM, bool INTERLEAVED>
-__device__ __forceinline__ void head_turn(f16x8& a, f16x8& b, const f16x8& wa, const f16x8& wb, const HeadPart& p, const HeadNorm& n, int dim, const CosSin (&cs)[8])
+// Norms of the heads of a launch: none, those without a mean, any.
+constexpr int kNoNorm = 0, kPlainNorm = 1, kAnyNorm = 2;
+
+// Cosines and sines in LDS: eight pairs, which a lane reads, begin 144 bytes behind the eight before them, so that the lanes of a head meet no banks of each other's.
+__device__ __forceinline__ int turn_at(int pair) { return pair + pair / 8; }
+constexpr int turns_of(int pairs) { return pairs + pairs / 8; }
+
+// a, b: the part's vectors, wa, wb: their weights; cs: cosines and sines of the part's pairs.  Every lane of a head takes part.
+template <int LANES, int MODE, bool INTERLEAVED>
+__device__ __forceinline__ void head_turn(f16x8& a, f16x8& b, const f16x8& wa, const f16x8& wb, const HeadPart& p, const HeadNorm& n, const CosSin* cs)
 {
+    constexpr int STEP = INTERLEAVED ? 2 : 1, OTHER = INTERLEAVED ? 1 : 8;           // of a pair's values
+    if ((MODE == kNoNorm || !n.on) && !p.turned) return;
     double x[16];
 #pragma unroll
     for (int i = 0; i < 8; ++i) x[i] = (double)(float)a[i], x[8 + i] = (double)(float)b[i];
-    if constexpr (NORM) {
+    if (MODE != kNoNorm && n.on) {
         double mean, factor;
-        head_norm<LANES>(x, !p.any ? 0 : p.whole ? 16 : 8, n, dim, mean, factor);
-        if (n.centred) {                                     // (uniform)
+        head_norm<LANES, MODE == kAnyNorm>(x, p.any, p.whole, n, mean, factor);
 #pragma unroll
-            for (int i = 0; i < 16; ++i) x[i] -= mean;
-        }
-#pragma unroll
-        for (int i = 0; i < 16; ++i) x[i] *= factor * (n.offset + (double)(float)(i < 8 ? wa[i] : wb[i - 8]));
+        for (int i = 0; i < 16; ++i) x[i] = (MODE == kAnyNorm ? x[i] - mean : x[i]) * (factor * (n.offset + (double)(float)(i < 8 ? wa[i & 7] : wb[i & 7])));
     }
     if (p.turned) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            constexpr int STEP = INTERLEAVED ? 2 : 1, OTHER = INTERLEAVED ? 1 : 8;
+            const CosSin t = cs[i];
             const double u = x[STEP * i], v = x[STEP * i + OTHER];
-            x[STEP * i] = u * cs[i].c - v * cs[i].s;
-            x[STEP * i + OTHER] = v * cs[i].c + u * cs[i].s;
+            x[STEP * i] = u * t.c - v * t.s;
+            x[STEP * i + OTHER] = v * t.c + u * t.s;
         }
-    } else if (!NORM) {
-        return;
     }
 #pragma unroll
     for (int i = 0; i < 8; ++i) a[i] = rope_round(x[i]), b[i] = rope_round(x[8 + i]);
 }
 
-// Heads h0 .. h1 - 1 of 128 dimensions of one token, by one wave; x and y may be the same.
-template <bool NORM, bool INTERLEAVED>
-__device__ __forceinline__ void turn_heads(const uint16_t* x, uint16_t* y, int h0, int h1, const HeadNorm& n, const HeadPart& part, const CosSin (&c)[8], int lane)
+// Heads h0 .. h1 - 1 of 128 dimensions of one token, by one wave; x and y may be the same; cs as turn_at() has it.
+template <int MODE, bool INTERLEAVED>
+__device__ __forceinline__ void turn_heads(const uint16_t* x, uint16_t* y, int h0, int h1, const HeadNorm& n, const RopePlan& r, const CosSin* cs, int lane)
 {
-    f16x8 wa = head_weights(n, h0, part.d0), wb = head_weights(n, h0, part.d1);
+    const HeadPart part(lane & 7, 128, r);
     for (int at = h0; at < h1; at += 8) {
         const int h = min(at + (lane >> 3), h1 - 1);
         const uint16_t* const from = x + (size_t)h * 128;
         f16x8 a = *(const f16x8*)(from + part.d0), b = *(const f16x8*)(from + part.d1);
-        if (n.stride) wa = head_weights(n, h, part.d0), wb = head_weights(n, h, part.d1);
-        head_turn<8, NORM, INTERLEAVED>(a, b, wa, wb, part, n, 128, c);
+        head_turn<8, MODE, INTERLEAVED>(a, b, head_weights(n, h, part.d0), head_weights(n, h, part.d1), part, n, cs + turn_at(8 * (lane & 7)));
         if (at + (lane >> 3) >= h1) continue;
         *(f16x8*)(y + (size_t)h * 128 + part.d0) = a;
         *(f16x8*)(y + (size_t)h * 128 + part.d1) = b;
@@ -159,16 +155,10 @@ __device__ __forceinline__ void turn_heads(const uint16_t* x, uint16_t* y, int h
 }
 __device__ __forceinline__ void turn_heads(const uint16_t* x, uint16_t* y, int h0, int h1, const HeadNorm& n, const RopePlan& r, const CosSin* cs, int lane)
 {
-    const HeadPart part(lane & 7, 128, r);
-    CosSin c[8] = {};
-    if (part.turned) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) c[i] = cs[8 * (lane & 7) + i];
-    }
-    if (n.on && r.interleaved) turn_heads<true, true>(x, y, h0, h1, n, part, c, lane);
-    else if (n.on) turn_heads<true, false>(x, y, h0, h1, n, part, c, lane);
-    else if (r.interleaved) turn_heads<false, true>(x, y, h0, h1, n, part, c, lane);
-    else turn_heads<false, false>(x, y, h0, h1, n, part, c, lane);
+    if (!n.centred && r.interleaved) turn_heads<kPlainNorm, true>(x, y, h0, h1, n, r, cs, lane);
+    else if (!n.centred) turn_heads<kPlainNorm, false>(x, y, h0, h1, n, r, cs, lane);
+    else if (r.interleaved) turn_heads<kAnyNorm, true>(x, y, h0, h1, n, r, cs, lane);
+    else turn_heads<kAnyNorm, false>(x, y, h0, h1, n, r, cs, lane);
 }
 
 // A lane's eight dimensions 8 * sub .. of head h of 128 dimensions that sixteen neighbouring lanes hold.
@@ -187,7 +177,7 @@ __device__ __forceinline__ u32x4 head_sixteenth(u32x4 raw, int h, const HeadNorm
     double x[8], mean, factor;
 #pragma unroll
     for (int i = 0; i < 8; ++i) x[i] = (double)(float)a[i];
-    head_norm<16>(x, 8, n, 128, mean, factor);
+    head_norm<16, true>(x, true, true, n, mean, factor);
 #pragma unroll
     for (int i = 0; i < 8; ++i) x[i] = (x[i] - mean) * (factor * (n.offset + (double)(float)wa[i]));
     f16x8 y;

@@ -166,9 +166,9 @@ __device__ __forceinline__ void rotate_row(const PagedSeqs& seqs, PagedRows q, u
         at = min((long)s.row + (row - base), (long)seqs.tokens - 1);
         bool own = true;
         if constexpr (kHeads) own = !heads.positions;
-        if (own) rope_angles(cs, rope, (int)((uint32_t)s.pos + (row - base)), lane);
+        if (own) rope_angles<kHeads>(cs, rope, (int)((uint32_t)s.pos + (row - base)), lane);
         if constexpr (kHeads) {
-            if (!own) rope_angles_of(cs, rope, heads.positions + at * rope.axes, lane);
+            if (!own) rope_angles_of<true>(cs, rope, heads.positions + at * rope.axes, lane);
         }
     }
     __syncthreads();
@@ -197,7 +197,7 @@ __global__ __launch_bounds__(256) void paged_append_kernel(PagedPool pool, Paged
     const unsigned long job = (unsigned long)(blockIdx.x - kv_blocks) * 4 + wave;
     const unsigned row = (unsigned)(job / parts);
     const int h0 = (int)(job - (unsigned long)row * parts) * per_wave;
-    rotate_row(seqs, q, q_out, q_out_stride, q_heads, rope, heads, row, h0, min(h0 + per_wave, q_heads), cs + wave * (kHeadDim / 2), lane);
+    rotate_row(seqs, q, q_out, q_out_stride, q_heads, rope, heads, row, h0, min(h0 + per_wave, q_heads), cs + wave * turns_of(kHeadDim / 2), lane);
 }
 
 // Few new tokens a sequence (a decoding step, drafts): a wave takes four of a token's vectors - keys of the KV heads, their values, then query heads - and puts codes where they

@@ -54,12 +54,13 @@ __device__ __forceinline__ _Float16 rope_round(double x)
     return (_Float16)f;
 }
 
-// Cosines and sines of a token's pairs, by one wave; every pair by the position on its axis.
+// Cosines and sines of a token's pairs, by one wave; every pair by the position on its axis.  SPREAD: a place is left free behind every eight.
+template <bool SPREAD = false>
 __device__ __forceinline__ void rope_angles_of(CosSin* cs, const RopePlan& r, const int32_t* positions, int lane)
 {
     for (int i = lane; i < r.rot / 2; i += 64) {
         const RopeTurn turn = r.turns[i];
-        cs[i] = rope_angle(r, positions[turn.axis], turn);
+        cs[SPREAD ? i + i / 8 : i] = rope_angle(r, positions[turn.axis], turn);
     }
 }
 
@@ -75,9 +76,10 @@ __device__ __forceinline__ void rope_pairs(f16x8& a, f16x8& b, const CosSin (&cs
 }
 
 // Cosines and sines of a token's pairs, by one wave.
+template <bool SPREAD = false>
 __device__ __forceinline__ void rope_angles(CosSin* cs, const RopePlan& r, int pos, int lane)
 {
-    for (int i = lane; i < r.rot / 2; i += 64) cs[i] = rope_angle(r, pos, r.turns[i]);
+    for (int i = lane; i < r.rot / 2; i += 64) cs[SPREAD ? i + i / 8 : i] = rope_angle(r, pos, r.turns[i]);
 }
 
 // Heads h0 .. h1 - 1 of one token, by one wave: x -> y (which may be the same).  A lane takes sixteen dimensions at a time: the eight pairs of

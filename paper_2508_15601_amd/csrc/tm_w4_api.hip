@@ -2125,14 +2125,14 @@ int tm_rope_apply(const uint16_t* X, int64_t x_stride, const int32_t* positions,
 // The kernels' view of a norm of `heads` heads.
 static int check_norm(const char* what, const tm_head_norm* n, int dim, HeadNorm* out)
 {
-    *out = HeadNorm{nullptr, 0, 1.0, 0.0, 0, 0};
+    *out = HeadNorm{nullptr, 0, 1.0, 0.0, 1.0 / dim, 0, 0};
     if (!n) return TM_OK;
-    if (!(n->eps > 0.0) || !isfinite(n->eps) || !isfinite(n->offset)) return fail(TM_EINVAL, "%s: need eps > 0 and a finite offset (got %g, %g)", what, n->eps, n->offset);
+    if (!(n->eps >= 1e-300) || !isfinite(n->eps) || !isfinite(n->offset)) return fail(TM_EINVAL, "%s: need eps >= 1e-300 and a finite offset (got %g, %g)", what, n->eps, n->offset);
     if (n->centred != 0 && n->centred != 1) return fail(TM_EINVAL, "%s: centred = %d", what, n->centred);
     if ((uintptr_t)n->weight & 15) return fail(TM_EINVAL, "%s: weight must be 16-byte aligned", what);
     if (n->weight_stride && (n->weight_stride % 8 || n->weight_stride < dim || n->weight_stride >= (int64_t(1) << 31)))
         return fail(TM_EINVAL, "%s: weight_stride %lld must be 0, or a multiple of 8, at least %d and below 2^31", what, (long long)n->weight_stride, dim);
-    *out = HeadNorm{n->weight, (long)n->weight_stride, n->eps, n->offset, 1, n->centred};
+    *out = HeadNorm{n->weight, (long)n->weight_stride, n->eps, n->offset, 1.0 / dim, 1, n->centred};
     return TM_OK;
 }
 
