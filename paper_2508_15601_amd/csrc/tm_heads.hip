@@ -1,4 +1,8 @@
 // Norms of queries and keys head by head with their rotation in the same pass (tm_heads_apply).
+//
+// Bound by memory where tokens are many: 8192 tokens of 32 / 8 heads of 128, nothing in the caches: 35.2 us, 168 MB at 4.8 TB/s (a large copy reaches 5.2; without norms 33.8 us); 64-bit arithmetic
+// and a wave's chain of load, sums over lanes, root and store bound the middle (1024 tokens 7.3 us, 21 MB), a launch the small (16 tokens 3.5 us).  Weights multiplied into the sines and
+// cosines once a token, which saves a third of the arithmetic, took registers and with them waves: 38 us.  Keeping the cosines in registers 35.1, but 8.6 for 1024.
 #include "tm_heads_device.h"
 #include "tm_paged_host.h"
 
@@ -67,8 +71,11 @@ hipError_t launch_heads(const HeadRows& q, const HeadRows& k, const int32_t* pos
 {
     const int lanes = dim <= 16 ? 1 : dim <= 32 ? 2 : dim <= 64 ? 4 : dim <= 128 ? 8 : 16, at_once = 64 / lanes;
     const int all = (q.heads + at_once - 1) / at_once + (k.heads + at_once - 1) / at_once;
-    // one round of a wave's lanes at a time where tokens are few
-    const int rounds = (long)tokens * all >= 16384L ? all : 1;
+    // Rounds a wave takes, which work out the token's angles once but follow one another.  Measured with 1, 2, 3 and 5 (us; heads of 128): 32 / 8 heads, 5 rounds a token: 512 tokens 4.8, 5.6, 5.7,
+    // 7.5; 1024 7.3, 7.7, 7.8, 8.4; 1500 10.2, 10.3, 9.5, 10.8; 2048 12.2, 12.0, 10.9, 11.4; 3000 16.3, 15.4, 14.2, 13.6; 8192 43.1, 36.8, 35.2, 35.4.  64 / 4 heads, 9 rounds: 1024 11.1, 10.4, 10.0,
+    // 10.6, 2048 18.9, 16.9, 15.6, 15.3, and 17.0 with all nine.
+    const long total = (long)tokens * all, least_parts = total < 6144 ? all : total < 12288 ? (all + 2) / 3 : (all + 4) / 5;
+    const int rounds = (int)((all + least_parts - 1) / least_parts);
     const long parts = (all + rounds - 1) / rounds, most = 4 * most_ctas(256) / parts;       // tokens of a launch
     const auto of = lanes == 1 ? pick<1> : lanes == 2 ? pick<2> : lanes == 4 ? pick<4> : lanes == 8 ? pick<8> : pick<16>;
     const auto kernel = of(!q.norm.on && !k.norm.on ? kNoNorm : !q.norm.centred && !k.norm.centred ? kPlainNorm : kAnyNorm, r.interleaved);
