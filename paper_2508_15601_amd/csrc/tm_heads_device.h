@@ -9,6 +9,8 @@
 
 namespace tmw4 {
 
+typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
+
 struct HeadNorm {                        // off: a head's values as they are
     const uint16_t* w;                   // fp16 weights of head 0, nullptr: ones
     long stride;                         // from head to head, 0: all have the same
@@ -143,14 +145,24 @@ template <int MODE, bool INTERLEAVED>
 __device__ __forceinline__ void turn_heads(const uint16_t* x, uint16_t* y, int h0, int h1, const HeadNorm& n, const RopePlan& r, const CosSin* cs, int lane)
 {
     const HeadPart part(lane & 7, 128, r);
-    for (int at = h0; at < h1; at += 8) {
+    f16x8 a, b, wa, wb;
+    auto request = [&](int at) {
         const int h = min(at + (lane >> 3), h1 - 1);
         const uint16_t* const from = x + (size_t)h * 128;
-        f16x8 a = *(const f16x8*)(from + part.d0), b = *(const f16x8*)(from + part.d1);
-        head_turn<8, MODE, INTERLEAVED>(a, b, head_weights(n, h, part.d0), head_weights(n, h, part.d1), part, n, cs + turn_at(8 * (lane & 7)));
-        if (at + (lane >> 3) >= h1) continue;
-        *(f16x8*)(y + (size_t)h * 128 + part.d0) = a;
-        *(f16x8*)(y + (size_t)h * 128 + part.d1) = b;
+        a = *(const f16x8*)(from + part.d0);
+        b = *(const f16x8*)(from + part.d1);
+        if (n.stride || at == h0) wa = head_weights(n, h, part.d0), wb = head_weights(n, h, part.d1);
+    };
+    request(h0);
+    for (int at = h0; at < h1; at += 8) {
+        f16x8 y0 = a, y1 = b;
+        const f16x8 w0 = wa, w1 = wb;
+        if (at + 8 < h1) request(at + 8);
+        head_turn<8, MODE, INTERLEAVED>(y0, y1, w0, w1, part, n, cs + turn_at(8 * (lane & 7)));
+        const int h = at + (lane >> 3);
+        if (h >= h1) continue;
+        *(f16x8*)(y + (size_t)h * 128 + part.d0) = y0;
+        *(f16x8*)(y + (size_t)h * 128 + part.d1) = y1;
     }
 }
 __device__ __forceinline__ void turn_heads(const uint16_t* x, uint16_t* y, int h0, int h1, const HeadNorm& n, const RopePlan& r, const CosSin* cs, int lane)
@@ -161,45 +173,83 @@ __device__ __forceinline__ void turn_heads(const uint16_t* x, uint16_t* y, int h
     else turn_heads<kAnyNorm, false>(x, y, h0, h1, n, r, cs, lane);
 }
 
-// A lane's eight dimensions 8 * sub .. of head h of 128 dimensions that sixteen neighbouring lanes hold.
-__device__ __forceinline__ u32x4 head_sixteenth(u32x4 raw, int h, const HeadNorm& n, const RopePlan& r, const CosSin* cs, int lane)
+// Sixteen neighbouring lanes hold a head of 128 dimensions, a lane eight of them.  Where two lanes hold the halves of eight pairs, each takes four of the pairs, so that every value is normed
+// once: dimensions d1 .. d1 + 3 and d2 .. d2 + 3.
+struct Sixteenth {
+    int sub, half, d1, d2;               // half: vectors of eight in half of the rotated part
+    bool turned, swap, low;
+    __device__ __forceinline__ Sixteenth(const RopePlan& r, int lane) : sub(lane & 15), half(r.rot / 16)
+    {
+        turned = 8 * sub < r.rot;
+        swap = turned && !r.interleaved;
+        low = sub < half;
+        d1 = !swap || low ? 8 * sub : 8 * (sub - half) + 4;
+        d2 = !swap ? d1 + 4 : d1 + r.rot / 2;
+    }
+};
+struct SixteenthWeights {
+    f16x4 w1, w2;
+};
+__device__ __forceinline__ SixteenthWeights sixteenth_weights(const HeadNorm& n, int h, const Sixteenth& s)
+{
+    SixteenthWeights w;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w.w1[i] = w.w2[i] = (_Float16)1.0f;
+    if (n.w) {
+        w.w1 = *(const f16x4*)(n.w + h * n.stride + s.d1);
+        w.w2 = *(const f16x4*)(n.w + h * n.stride + s.d2);
+    }
+    return w;
+}
+
+// The lane's dimensions 8 * sub ..; cs without gaps.
+__device__ __forceinline__ u32x4 head_sixteenth(u32x4 raw, const SixteenthWeights& w, const Sixteenth& s, const HeadNorm& n, const RopePlan& r, const CosSin* cs, int lane)
 {
     if (!n.on) return r.rot ? rope_sixteenth(raw, r, cs, lane) : raw;
-    const int sub = lane & 15, half = r.rot / 16;            // vectors of eight in half of the rotated part
-    const bool turned = 8 * sub < r.rot, low = sub < half;
-    const int partner = r.interleaved || !turned ? sub : low ? sub + half : sub - half;
-    u32x4 other = raw;
+    const bool turned = s.turned, swap = s.swap, low = s.low;
+    const int partner = swap ? (lane & ~15) | (low ? s.sub + s.half : s.sub - s.half) : lane;
+    u32x2 first = {raw[0], raw[1]}, second = {raw[2], raw[3]};
     if (r.rot && !r.interleaved) {                           // (uniform)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) other[i] = (uint32_t)__shfl((int)raw[i], (lane & ~15) | partner);
+        const u32x2 out = low ? second : first;
+        const u32x2 in = {(uint32_t)__shfl((int)out[0], partner), (uint32_t)__shfl((int)out[1], partner)};
+        if (swap && low) second = in;
+        if (swap && !low) first = in;
     }
-    const f16x8 a = __builtin_bit_cast(f16x8, raw), b = __builtin_bit_cast(f16x8, other), wa = head_weights(n, h, 8 * sub), wb = head_weights(n, h, 8 * partner);
+    const f16x4 a = __builtin_bit_cast(f16x4, first), b = __builtin_bit_cast(f16x4, second);
     double x[8], mean, factor;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] = (double)(float)a[i];
-    head_norm<16, true>(x, true, true, n, mean, factor);
+    for (int i = 0; i < 4; ++i) x[i] = (double)(float)a[i], x[4 + i] = (double)(float)b[i];
+    if (n.centred) head_norm<16, true>(x, true, true, n, mean, factor);
+    else head_norm<16, false>(x, true, true, n, mean, factor);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] = (x[i] - mean) * (factor * (n.offset + (double)(float)wa[i]));
-    f16x8 y;
-    if (turned && r.interleaved) {
+    for (int i = 0; i < 8; ++i) x[i] = (x[i] - mean) * (factor * (n.offset + (double)(float)(i < 4 ? w.w1[i & 3] : w.w2[i & 3])));
+    if (turned) {
+        const CosSin* const mine = cs + (r.interleaved ? 4 * s.sub : s.d1);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const CosSin c = cs[4 * sub + i];
-            y[2 * i] = rope_round(x[2 * i] * c.c - x[2 * i + 1] * c.s);
-            y[2 * i + 1] = rope_round(x[2 * i + 1] * c.c + x[2 * i] * c.s);
+            const CosSin c = mine[i];
+            if (r.interleaved) {
+                const double u = x[2 * i], v = x[2 * i + 1];
+                x[2 * i] = u * c.c - v * c.s;
+                x[2 * i + 1] = v * c.c + u * c.s;
+            } else {
+                const double u = x[i], v = x[4 + i];
+                x[i] = u * c.c - v * c.s;
+                x[4 + i] = v * c.c + u * c.s;
+            }
         }
-    } else if (turned) {
-        const CosSin* const mine = cs + 8 * (low ? sub : sub - half);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const double z = ((double)(float)b[i] - mean) * (factor * (n.offset + (double)(float)wb[i]));
-            y[i] = rope_round(x[i] * mine[i].c + (low ? -z : z) * mine[i].s);
-        }
-    } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) y[i] = rope_round(x[i]);
     }
-    return __builtin_bit_cast(u32x4, y);
+    f16x4 y1, y2;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) y1[i] = rope_round(x[i]), y2[i] = rope_round(x[4 + i]);
+    first = __builtin_bit_cast(u32x2, y1), second = __builtin_bit_cast(u32x2, y2);
+    if (r.rot && !r.interleaved) {
+        const u32x2 out = low ? second : first;
+        const u32x2 in = {(uint32_t)__shfl((int)out[0], partner), (uint32_t)__shfl((int)out[1], partner)};
+        if (swap && low) second = in;
+        if (swap && !low) first = in;
+    }
+    return u32x4{first[0], first[1], second[0], second[1]};
 }
 
 }  // namespace tmw4
