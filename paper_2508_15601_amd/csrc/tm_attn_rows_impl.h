@@ -34,8 +34,8 @@ struct PagedWhere {
     int b, hk;
 };
 
-// WINDOW (paged): a row attends over the first tokens and those of its window; stages that no row of the CTA sees are left out (`hidden`), and job.first_stage and job.stages count what
-// is left.  Runs of a stage that none sees are not read either.
+// WINDOW (paged): a row attends over the first tokens and those of its window; runs that no row of the CTA sees are left out (`hidden`), a stage is two of those that are left, and
+// job.first_stage and job.stages count such stages.
 template <int BITS, int RW, bool PAGED, bool WINDOW = false>
 __device__ __forceinline__ void attn_rows(const RowsJob& job, const uint8_t* kcodes, const uint8_t* vcodes, const uint32_t* words, const PagedWhere& where, int len_all,
                                           float scale_log2e, unsigned char* smem)
@@ -56,8 +56,8 @@ __device__ __forceinline__ void attn_rows(const RowsJob& job, const uint8_t* kco
     const int nst = job.stages;
     const int tok0 = PAGED && !WINDOW ? job.first_stage * ST : 0;      // first token of the piece
     const int sinks = WINDOW ? where.seqs.sinks : 0, tile_first = WINDOW ? (int)min(max(pos0 + tok_first, 0L), (long)job.cap) : 0;
-    const Hidden hidden(where.seqs, tile_first, ST);
-    auto token_of = [&](int st) { return WINDOW ? hidden.real(job.first_stage + st) * ST : tok0 + st * ST; };      // first of a stage
+    const Hidden hidden(where.seqs, tile_first, kRun);
+    auto run_of = [&](int st, int n) { return WINDOW ? hidden.real(2 * (job.first_stage + st) + n) : (tok0 >> 5) + 2 * st + n; };      // of the sequence
 
     // this wave's rows, and this lane's
     const int w0 = row0 + rg * 32;
@@ -103,9 +103,8 @@ __device__ __forceinline__ void attn_rows(const RowsJob& job, const uint8_t* kco
         if constexpr (PAGED) {
 #pragma unroll
             for (int n = 0; n < 2; ++n) {
-                const int run = (token_of(st) >> 5) + n;
+                const int run = run_of(st, n);
                 if (run * kRun >= len_all) continue;
-                if (WINDOW && run * kRun >= sinks && (run + 1) * kRun <= tile_first - where.seqs.window + 1) continue;
                 const int page = run >> where.pool.run_log;
                 if (page >= ids_at + 64) {
                     ids_at = page;
@@ -304,7 +303,7 @@ __device__ __forceinline__ void attn_rows(const RowsJob& job, const uint8_t* kco
 #pragma unroll
         for (int e = 1; e < 16; ++e) mx = fmaxf(mx, x[e]);
     };
-    auto first_token = [&](int st, int sub) { return token_of(st) + (KS > 1 ? ksg : sub) * 32; };
+    auto first_token = [&](int st, int sub) { return WINDOW ? run_of(st, KS > 1 ? ksg : sub) * kRun : tok0 + st * ST + (KS > 1 ? ksg : sub) * 32; };
     auto at_edge = [&](int t0) { return t0 + 32 > wmin || (WINDOW && t0 < most_lo && t0 + 32 > sinks); };           // not every row sees all 32
     auto is_there = [&](int st, int sub) { return !PAGED || (present >> (2 * (st & 3) + (KS > 1 ? ksg : sub)) & 1u); };
 

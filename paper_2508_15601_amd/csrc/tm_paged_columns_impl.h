@@ -173,7 +173,7 @@ struct Columns {
 // the other read it twice: 12 x 5 drafted tokens after 6000, 25 columns, 8-bit codes: 45 us, like this 36.  The codes are then not loaded as data that nobody else wants, which
 // cost the second wave a quarter of its hits: 32 x 5 after 8000 120 us, so 104.)
 // block, blocks: the CTA and how many there are; WAVES: of a CTA.
-// WINDOW: quads that none of a sequence's new tokens sees are left out, and what is left is numbered through; a block that its tile does not see is not read.  A block that holds
+// WINDOW: blocks that none of a sequence's new tokens sees are left out, and what is left is numbered through; a block that its tile does not see is not read.  A block that holds
 // first tokens and tokens of windows is taken in two steps, so that the tokens a column sees are a range in each.
 template <int BITS, bool PACK, int PARTS, int TILES, bool ALONE, int WAVES, bool WINDOW = false>
 __device__ __forceinline__ void paged_columns(const PagedPool& pool, const PagedSeqs& seqs, const uint16_t* __restrict__ Q, long q_stride, uint16_t* __restrict__ O, int q_heads,
@@ -205,8 +205,8 @@ __device__ __forceinline__ void paged_columns(const PagedPool& pool, const Paged
     // ---- this CTA's piece of the work
     auto tiles_of = [&](const PagedSeq& s) { return s.count * G <= most_rows ? (s.count * G + COLS - 1) / COLS : 0; };
     auto quads_of = [&](const PagedSeq& s) {
-        const int quads = (max(s.last(seqs.cap), 0) + kStep * TOK - 1) / (kStep * TOK);
-        return WINDOW ? quads - Hidden(seqs, s.first(), kStep * TOK).count : quads;
+        const int end = max(s.last(seqs.cap), 0);
+        return WINDOW ? ((end + TOK - 1) / TOK - Hidden(seqs, s.first(), TOK).count + kStep - 1) / kStep : (end + kStep * TOK - 1) / (kStep * TOK);
     };
     const uint32_t ctas = ALONE ? WAVES * blocks : blocks, me = ALONE ? WAVES * block + any_wave : block;      // CTAs, or waves, that share the work
     // Up to 64 sequences a lane holds one, loaded once: a launch of few short contexts is a chain of memory round trips, and this one is its first.
@@ -282,12 +282,11 @@ __device__ __forceinline__ void paged_columns(const PagedPool& pool, const Paged
         const int len_all = (int)min(max((long)s.pos + last_tok + 1, 0L), (long)seqs.cap);
         Form form;
         form.request_query(Q + (size_t)(s.row + col.tok) * q_stride + ((size_t)hk * G + col.head) * kHeadDim, lane);
-        const Hidden hidden(seqs, WINDOW ? s.first() : 0, kStep * TOK);
-        const int hidden_from = hidden.from * kStep, hidden_blocks = hidden.count * kStep;
-        auto real = [&](int k) { return WINDOW && k >= hidden_from ? k + hidden_blocks : k; };
+        const Hidden hidden(seqs, WINDOW ? s.first() : 0, TOK);
+        auto real = [&](int k) { return WINDOW ? hidden.real(k) : k; };
         const int tile_lo = WINDOW ? (int)min(max((long)s.pos + r0 / G, 0L), (long)seqs.cap) - seqs.window + 1 : 0;      // of the tile's first row; the lane's:
         const int lo = WINDOW ? len - seqs.window : 0;
-        const int blk1 = min((int)qb * kStep, (len_all + TOK - 1) / TOK - (WINDOW ? hidden_blocks : 0));
+        const int blk1 = min((int)qb * kStep, (len_all + TOK - 1) / TOK - (WINDOW ? hidden.count : 0));
         int blk = (int)qa * kStep + wave;
 
         constexpr uint32_t kPart = 4096 / PARTS, kPartTokens = TOK / PARTS;

@@ -40,7 +40,7 @@ __device__ __forceinline__ RowsShape rows_shape(const PagedSeq& s, const PagedSe
     const uint32_t tiles = (uint32_t)((s.count * G + ROWS - 1) / ROWS), stages = (uint32_t)((max(s.last(seqs.cap), 0) + ST - 1) / ST);
     const float causal = fmaxf((float)stages - 0.5f / ST * (float)s.count, 0.f);     // (half the new tokens less)
     if constexpr (WINDOW) {
-        const uint32_t seen = (uint32_t)((seqs.window + ROWS / G + 1) / ST + 2 + (seqs.sinks + ST - 1) / ST);
+        const uint32_t seen = (uint32_t)(((seqs.window + ROWS / G + 1) / kRun + 2 + (seqs.sinks + kRun - 1) / kRun + 1) / 2);
         return RowsShape{tiles, min(stages, seen), (float)tiles * fminf(causal, (float)seen)};
     }
     return RowsShape{tiles, stages, (float)tiles * causal};
@@ -168,7 +168,7 @@ __device__ __forceinline__ bool rows_tile(RowsTile& t, const PagedSeqs& seqs, in
     if (tok_first >= t.s.count || (long)t.s.pos + tok_first >= seqs.cap) return false;
     t.len = (int)min(max((long)t.s.pos + min(t.s.count, (t.row0 + ROWS - 1) / G + 1), 0L), (long)seqs.cap);
     t.stages = (t.len + ST - 1) / ST;
-    if constexpr (WINDOW) t.stages -= Hidden(seqs, (int)min(max((long)t.s.pos + tok_first, 0L), (long)seqs.cap), ST).count;
+    if constexpr (WINDOW) t.stages = ((t.len + kRun - 1) / kRun - Hidden(seqs, (int)min(max((long)t.s.pos + tok_first, 0L), (long)seqs.cap), kRun).count + 1) / 2;
     t.pieces = (int)pieces_of(t.stages, P);
     return t.len > 0 && t.piece < t.pieces;
 }
