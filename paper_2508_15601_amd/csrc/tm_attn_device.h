@@ -116,7 +116,7 @@ __device__ __forceinline__ void move_reference(float mx, SoftmaxState& st, f32x4
 // value it meets.  len: tokens the lane's query column attends over (the same in every lane at a decoding step; at prefill
 // every column has its own causal limit).
 // STEP: a wave takes every STEP-th block.
-// WINDOW: the lane's column attends over the tokens `lo` .. len - 1 only.
+// WINDOW: the lane's column attends over the tokens `lo` .. len - 1 and the first `first` of all only.
 // HOLES (paged cache): bit i of `present` tells whether run i of the block lies on a page of the pool; without it the run has no tokens.
 //
 // PACK: at most eight query heads share the KV head.  The query operand then carries every head twice
@@ -127,20 +127,21 @@ __device__ __forceinline__ void move_reference(float mx, SoftmaxState& st, f32x4
 template <int BITS, bool PACK, int N0, int NH, bool HOLES = false, int STEP = 4, bool WINDOW = false>
 __device__ __forceinline__ void process_runs(const BlockRegs& r, const uint32_t* sz_slot, const f16x8 (&qf)[4],
                                               float scale_log2e, float qsum, const f32x4& neg_qbias, const Magic& mg, int blk, int len,
-                                              int lane, SoftmaxState& st, f32x4 (&acc)[8], uint32_t present = ~0u, int lo = 0)
+                                              int lane, SoftmaxState& st, f32x4 (&acc)[8], uint32_t present = ~0u, int lo = 0, int first = 0)
 {
     constexpr int NS = PACK ? 1 : 2;                         // score tiles a lane keeps of a run
     const int h = lane >> 4, jl = PACK ? (lane >> 3) & 1 : 0;      // jl: the 16-token tile this lane keeps
     const int rem_all = len - blk * (256 / BITS) - 32 * N0 - 4 * h - 16 * jl;  // slot (n, j, rr) is a live token iff 32*n + 16*j + rr < rem
-    const int lo_rem = WINDOW ? len - rem_all - lo : 0;                        // WINDOW: iff 32*n + 16*j + rr + lo_rem is in 0 .. rem - 1
+    const int lo_rem = WINDOW ? len - rem_all - lo : 0;                        // WINDOW: iff 32*n + 16*j + rr + lo_rem is in 0 .. rem - 1, or 32*n + 16*j + rr < first_rem
     auto rem_of = [&](int n) { return !HOLES || (present >> (N0 + n) & 1u) ? WINDOW ? max(len - lo, 0) : rem_all : WINDOW ? 0 : -1; };
-    auto is_live = [&](int slot, int rem) { return WINDOW ? (uint32_t)(slot + lo_rem) < (uint32_t)rem : slot < rem; };
+    auto first_of = [&](int n) { return WINDOW && (!HOLES || (present >> (N0 + n) & 1u)) ? min(first, len) - (len - rem_all) : -1; };
+    auto is_live = [&](int slot, int rem, int first_rem) { return WINDOW ? (uint32_t)(slot + lo_rem) < (uint32_t)rem || slot < first_rem : slot < rem; };
     float t[NH][NS][4];                                      // scores before the key's scale
     f16x2 kp[NH][NS][4];                                     // (scale, zero-point) of the slot's key
     uint32_t vw[NH][NS][4];                                  // and of its value; 0 for a dead token
 #pragma unroll
     for (int n = 0; n < NH; ++n) {
-        const int rem = rem_of(n);
+        const int rem = rem_of(n), first_rem = first_of(n);
         // S^T for the two 16-token tiles: rows = tokens, columns = query heads.  The accumulator starts at minus the bias
         // term: sum_d (bias_d + q_d) Q_d - sum_d bias_d Q_d = sum_d q_d Q_d
         f32x4 d[2];
@@ -167,7 +168,7 @@ __device__ __forceinline__ void process_runs(const BlockRegs& r, const uint32_t*
 #pragma unroll
             for (int rr = 0; rr < 4; ++rr) {
                 // a dead token contributes nothing, whatever its pair holds: scale 0 and zero-point 0 for its values
-                const bool live = is_live(32 * n + 16 * j + rr, rem);
+                const bool live = is_live(32 * n + 16 * j + rr, rem, first_rem);
                 kp[n][j][rr] = as_f16x2(rr < 2 ? p0[2 * rr] : p1[2 * (rr - 2)]);
                 vw[n][j][rr] = live ? (rr < 2 ? p0[2 * rr + 1] : p1[2 * (rr - 2) + 1]) : 0u;
                 // sum_d q_d Q_d  -  z sum_d Q_d  =  sum_d (q_d - z) Q_d, times scale * log2(e).  (The pair enters a multiply-add,
@@ -184,13 +185,13 @@ __device__ __forceinline__ void process_runs(const BlockRegs& r, const uint32_t*
         mx = kNegBig;
 #pragma unroll
         for (int n = 0; n < NH; ++n) {
-            const int rem = rem_of(n);
+            const int rem = rem_of(n), first_rem = first_of(n);
 #pragma unroll
             for (int j = 0; j < NS; ++j)
 #pragma unroll
                 for (int rr = 0; rr < 4; ++rr) {
                     const float v = __builtin_fmaf((float)kp[n][j][rr].x, t[n][j][rr], -ref);
-                    x[n][j][rr] = is_live(32 * n + 16 * j + rr, rem) ? v : kNegBig;
+                    x[n][j][rr] = is_live(32 * n + 16 * j + rr, rem, first_rem) ? v : kNegBig;
                     mx = fmaxf(mx, x[n][j][rr]);
                 }
         }
@@ -290,14 +291,14 @@ __device__ __forceinline__ void process_runs(const BlockRegs& r, const uint32_t*
 template <int BITS, bool PACK, bool HOLES = false, int STEP = 4, bool WINDOW = false>
 __device__ __forceinline__ void process_block(const BlockRegs& r, const uint32_t* sz_slot, const f16x8 (&qf)[4],
                                               float scale_log2e, float qsum, const f32x4& neg_qbias, const Magic& mg, int blk, int len, int len_all,
-                                              int lane, SoftmaxState& st, f32x4 (&acc)[8], uint32_t present = ~0u, int lo = 0)
+                                              int lane, SoftmaxState& st, f32x4 (&acc)[8], uint32_t present = ~0u, int lo = 0, int first = 0)
 {
     if constexpr (BITS == 8 || PACK) {
-        process_runs<BITS, PACK, 0, BITS == 8 ? 1 : 2, HOLES, STEP, WINDOW>(r, sz_slot, qf, scale_log2e, qsum, neg_qbias, mg, blk, len, lane, st, acc, present, lo);
+        process_runs<BITS, PACK, 0, BITS == 8 ? 1 : 2, HOLES, STEP, WINDOW>(r, sz_slot, qf, scale_log2e, qsum, neg_qbias, mg, blk, len, lane, st, acc, present, lo, first);
     } else {
-        process_runs<BITS, PACK, 0, 1, HOLES, STEP, WINDOW>(r, sz_slot, qf, scale_log2e, qsum, neg_qbias, mg, blk, len, lane, st, acc, present, lo);
+        process_runs<BITS, PACK, 0, 1, HOLES, STEP, WINDOW>(r, sz_slot, qf, scale_log2e, qsum, neg_qbias, mg, blk, len, lane, st, acc, present, lo, first);
         if (blk * 64 + 32 < len_all)                         // (wave-uniform) the second run may lie wholly behind the context
-            process_runs<BITS, PACK, 1, 1, HOLES, STEP, WINDOW>(r, sz_slot, qf, scale_log2e, qsum, neg_qbias, mg, blk, len, lane, st, acc, present, lo);
+            process_runs<BITS, PACK, 1, 1, HOLES, STEP, WINDOW>(r, sz_slot, qf, scale_log2e, qsum, neg_qbias, mg, blk, len, lane, st, acc, present, lo, first);
     }
 }
 

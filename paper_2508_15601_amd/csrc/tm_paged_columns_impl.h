@@ -98,12 +98,12 @@ struct Columns {
         for (int i = 0; i < 8; ++i) acc[i] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
     template <int PARTS, int STEP, bool WINDOW>
-    __device__ __forceinline__ void block(const BlockRegs& r, const uint32_t* words, const Magic& mg, int blk, int len, int len_all, int lane, uint32_t present, int lo)
+    __device__ __forceinline__ void block(const BlockRegs& r, const uint32_t* words, const Magic& mg, int blk, int len, int len_all, int lane, uint32_t present, int lo, int first)
     {
         if constexpr (PARTS == 1)
-            process_block<BITS, PACK, false, STEP, WINDOW>(r, words, qf, scale_log2e, qsum, neg_qbias, mg, blk, present ? len : 0, len_all, lane, st, acc, ~0u, lo);
+            process_block<BITS, PACK, false, STEP, WINDOW>(r, words, qf, scale_log2e, qsum, neg_qbias, mg, blk, present ? len : 0, len_all, lane, st, acc, ~0u, present ? lo : 0, first);
         else
-            process_block<BITS, PACK, true, STEP, WINDOW>(r, words, qf, scale_log2e, qsum, neg_qbias, mg, blk, len, len_all, lane, st, acc, present, lo);
+            process_block<BITS, PACK, true, STEP, WINDOW>(r, words, qf, scale_log2e, qsum, neg_qbias, mg, blk, len, len_all, lane, st, acc, present, lo, first);
     }
     // The four waves that share the columns meet in LDS: wave `wave` gets the unnormalised values o[i] of dimensions 16 * (2 * wave + i) + 4 * (lane / 16) ... of its lane's column, the
     // reference M and the denominator L.  (One barrier; another has to follow before the next segment's.)
@@ -173,8 +173,7 @@ struct Columns {
 // the other read it twice: 12 x 5 drafted tokens after 6000, 25 columns, 8-bit codes: 45 us, like this 36.  The codes are then not loaded as data that nobody else wants, which
 // cost the second wave a quarter of its hits: 32 x 5 after 8000 120 us, so 104.)
 // block, blocks: the CTA and how many there are; WAVES: of a CTA.
-// WINDOW: blocks that none of a sequence's new tokens sees are left out, and what is left is numbered through; a block that its tile does not see is not read.  A block that holds
-// first tokens and tokens of windows is taken in two steps, so that the tokens a column sees are a range in each.
+// WINDOW: blocks that none of a sequence's new tokens sees are left out, and what is left is numbered through; a block that its tile does not see is not read.
 template <int BITS, bool PACK, int PARTS, int TILES, bool ALONE, int WAVES, bool WINDOW = false>
 __device__ __forceinline__ void paged_columns(const PagedPool& pool, const PagedSeqs& seqs, const uint16_t* __restrict__ Q, long q_stride, uint16_t* __restrict__ O, int q_heads,
                                               float scale_log2e, int most_rows, float* __restrict__ partial, uint32_t* __restrict__ counters, uint32_t block, uint32_t blocks)
@@ -342,16 +341,7 @@ __device__ __forceinline__ void paged_columns(const PagedPool& pool, const Paged
             const int fill = (use + 2) % 3;
             there[fill] = load(g[fill], ring(fill), blk + 2 * kStep, next);
             next = pages_of(blk + 3 * kStep);
-            if constexpr (WINDOW) {
-                const int k = real(blk);
-                // first tokens, then the window's; both parts may be there (uniform)
-                for (int part = k * TOK < seqs.sinks ? 0 : 1; part < ((k + 1) * TOK > seqs.sinks ? 2 : 1); ++part) {
-                    const int from = part ? max(lo, seqs.sinks) : 0, to = part ? len : min(len, seqs.sinks);
-                    form.template block<PARTS, kStep, true>(g[use], ring(use), mg, k, max(to, from), len_all, lane, there[use], from);
-                }
-            } else {
-                form.template block<PARTS, kStep, false>(g[use], ring(use), mg, blk, len, len_all, lane, there[use], 0);
-            }
+            form.template block<PARTS, kStep, WINDOW>(g[use], ring(use), mg, real(blk), len, len_all, lane, there[use], lo, WINDOW ? seqs.sinks : 0);
             blk += kStep;
             return blk < blk1;
         };

@@ -34,6 +34,11 @@ hipError_t paged_rows_setup()
 // 118; 128 at 1000 and 512 at 2000 86, 93, 104 and 78, 82, 92; 200 at 2000 and a prompt of 256, where the rule takes 11 / 16, 147, 133, 137 and 90, 80, 90.  Short contexts beside tiles of 128 rows
 // it does not tell apart, and takes half: 60 at 500 and 400 at 500 23, 30 and 24, 29, but 300 at 300 and a prompt of 64 46, 41, 48 and 37, 31, 43.  Behind the row tiles the columns' long
 // pieces stick out: 2 to 8 % more than with half in the first three; on all compute units first 10 to 14 %.
+// In a window both parts' work is known, about: a sequence's context is what it sees.  Where row tiles do not fill the chip by themselves the columns take the compute units that their share
+// of the work asks for: a compute unit that has nothing but columns reads 50 GB/s of 8-bit codes, 38 of 4-bit ones, and a stage takes 2.3 us (1.5 with 128 rows).  Half of them, and the share
+// (us; 8-bit unless said): 24 decoding and chunks of 1024 and 512, window 2048, 4-bit: 116 and 97 with 16 to 64; 8 decoding and 300, 16 / 2 heads: 41 and 33 with 16 to 64; 96 decoding and 200: 107, and
+// 100 with 176; 64 decoding and 512, window 4096: 136 with 128, 157 with 96 and 170 with 176.  Where the tiles fill the chip half is as good as any: 40 decoding and 1500 and 750: 87 with 96 to
+// 176, 96 with 32.
 // 128 or 256 rows a CTA: a stage of 128 costs 0.66 of one of 256 (the four prompts above: 1154 against 867 us).  So 256, unless the chip does not fill with either and pieces cannot
 // make up for it, a context being short (two prompts of 307 and 161 tokens, 2 / 1 heads: 19 against 20 us; 400 and 150, 16 / 1: 34 against 39).  Over 57 random calls (one chunk after
 // up to 40000 tokens, up to six prompts, up to 30 decoding sequences with chunks; 1 to 8 KV heads, 1 to 16 query heads each) the rule's choice takes 1.02 of the better one's time,
@@ -80,6 +85,15 @@ PagedForm paged_form(const PagedPool& pool, const PagedSeqs& seqs, int q_heads, 
         }
     }
     if (f.together) f.column_ctas = std::min(rows / (32 * f.row_waves) * pool.heads >= num_cu / 4 ? num_cu / 2 : num_cu * 11 / 16, kPagedMostWaves / 8);
+    if (f.together && windowed) {
+        const long count = std::max(most / G, 1L), chunks = std::min(std::max((seqs.tokens - seqs.batch + count - 1) / count, 1L), (long)seqs.batch), decoding = seqs.batch - chunks;
+        const double tiles = (double)(seqs.tokens - decoding) * G / (32 * f.row_waves) * pool.heads;
+        if (tiles < num_cu) {
+            const double columns = (double)decoding * std::min((long)len, (long)seqs.window + seqs.sinks) * pool.heads * (32 * pool.bits + 8) / (pool.bits == 8 ? 50e3 : 38e3);
+            const double tall = tiles * (stages + 5.0) * (f.row_waves == 8 ? 2.3 : 1.5);
+            f.column_ctas = std::min(std::max((int)(num_cu * columns / (columns + tall)), num_cu / 16), std::min(num_cu * 11 / 16, kPagedMostWaves / 8));
+        }
+    }
     return f;
 }
 
