@@ -12,22 +12,24 @@ namespace tmw4 {
 
 namespace {
 
-constexpr int kPlanThreads = 1024;
+constexpr int kPlanThreads = 1024;       // most rows that a CTA works out at a time
+constexpr int kOwnTokens = 8;            // of a row that its own thread places
 
-// Inclusive sum over the CTA, at most 2^32 - 1 each; `total` is the CTA's.
+// Inclusive sum over the CTA, at most 2^32 - 1 each; `total` is the CTA's.  `waves` may be used again behind another barrier.
+template <int THREADS>
 __device__ __forceinline__ uint32_t block_sums(uint32_t v, uint32_t* waves, uint32_t& total)
 {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     auto add = [](uint32_t a, uint32_t b) { return __builtin_elementwise_add_sat(a, b); };
     v = wave_scan(v, add);
-    __syncthreads();                                         // (what was there has been read)
     if (lane == 63) waves[wave] = v;
     __syncthreads();
     uint32_t before = 0;
     total = 0;
-    for (int w = 0; w < (int)blockDim.x / 64; ++w) {
+#pragma unroll
+    for (int w = 0; w < THREADS / 64; ++w) {
         const uint32_t n = waves[w];
-        if (w < wave) before = add(before, n);
+        before = add(before, w < wave ? n : 0u);
         total = add(total, n);
     }
     return add(before, v);
@@ -39,11 +41,13 @@ struct AssignedRow {
     bool served;
 };
 
+// sums: room for two sums over the CTA.
+template <int THREADS>
 struct AssignPlan {
     uint32_t tokens, pages;              // of the rows so far: given or not
-    uint32_t taken;                      // pages given
+    uint32_t given;                      // pages given to the thread's rows and all before them, if those were given any
     int available;
-    __device__ __forceinline__ AssignedRow next(const AssignJob& j, int b, uint32_t* waves)
+    __device__ __forceinline__ AssignedRow next(const AssignJob& j, int b, uint32_t (*sums)[THREADS / 64])
     {
         const int cap = j.cap, page = 1 << j.page_log;
         int len = 0;
@@ -53,7 +57,7 @@ struct AssignPlan {
             count = (uint32_t)max(j.counts[b], 0);
         }
         AssignedRow r;
-        const uint32_t end = __builtin_elementwise_add_sat(block_sums(count, waves, all), tokens);
+        const uint32_t end = __builtin_elementwise_add_sat(block_sums<THREADS>(count, sums[0], all), tokens);
         r.end = (int)min(end, (uint32_t)j.tokens);
         r.row = (int)min(end == ~0u ? ~0u : end - count, (uint32_t)j.tokens);
         tokens = __builtin_elementwise_add_sat(tokens, all);
@@ -61,15 +65,11 @@ struct AssignPlan {
         r.stop = (int)min((uint32_t)len + (uint32_t)(r.end - r.row), (uint32_t)cap);
         const int have = (len + page - 1) >> j.page_log;
         const uint32_t need = (uint32_t)max(((r.stop + page - 1) >> j.page_log) - have, 0);
-        const uint32_t until = block_sums(need, waves, all) + pages;         // (at most tokens / 32 + batch)
+        const uint32_t until = block_sums<THREADS>(need, sums[1], all) + pages;         // (at most tokens / 32 + batch)
         pages += all;
         r.served = need == 0 || until <= (uint32_t)available;
         r.first = available - 1 - (int)(until - need) + have;
-        const uint32_t given = wave_greatest(r.served && need ? until : 0u);
-        __syncthreads();
-        if ((threadIdx.x & 63) == 0) waves[threadIdx.x >> 6] = given;
-        __syncthreads();
-        for (int w = 0; w < (int)blockDim.x / 64; ++w) taken = max(taken, waves[w]);
+        if (r.served && need) given = until;
         return r;
     }
 };
@@ -99,21 +99,30 @@ __device__ __forceinline__ void place_token(const AssignJob& j, int b, int t, in
     if (j.slots) j.slots[t] = (uint32_t)id < (uint32_t)j.pool_pages ? (int64_t)id << j.page_log | (at & (page - 1)) : -1;
 }
 
-// Up to kPlanThreads rows: every CTA works out the rows for itself and places its share of the tokens.  The lengths and the list's count may be updated in place, so they are
-// written by the CTA that is last to have read them.
-__global__ __launch_bounds__(kPlanThreads) void assign_kernel(AssignJob j, uint32_t* arrived)
+// Up to THREADS rows: every CTA works out the rows for itself and places its share of the tokens: the first one, a thread a row, those of rows with up to kOwnTokens of them, and the others
+// by search.  The lengths and the list's count may be updated in place, so they are written by the CTA that is last to have read them.
+template <int THREADS>
+__global__ __launch_bounds__(THREADS) void assign_kernel(AssignJob j, uint32_t* arrived)
 {
-    __shared__ uint32_t waves[kPlanThreads / 64], s_last;
-    __shared__ int s_end[kPlanThreads], s_row[kPlanThreads], s_len[kPlanThreads], s_first[kPlanThreads];
+    __shared__ uint32_t sums[2][THREADS / 64], s_last, s_taken;
+    __shared__ int s_end[THREADS], s_row[THREADS], s_len[THREADS], s_first[THREADS];
     const int b = threadIdx.x;
-    AssignPlan plan{0u, 0u, 0u, available_pages(j)};
-    const AssignedRow r = plan.next(j, b, waves);
+    if (b == 0) s_taken = 0;
+    AssignPlan<THREADS> plan{0u, 0u, 0u, available_pages(j)};
+    const AssignedRow r = plan.next(j, b, sums);
+    const bool mine = r.end - r.row <= kOwnTokens;           // to place by its own thread
+    const uint32_t given = wave_greatest(plan.given);
+    if ((b & 63) == 0 && given) atomicMax(&s_taken, given);
     s_end[b] = b < j.batch ? r.end : j.tokens;
     s_row[b] = r.row;
     s_len[b] = r.len;
     s_first[b] = r.served ? r.first : INT_MIN;
-    if (blockIdx.x == 0 && b < j.batch) write_row(j, b, r);
-    __syncthreads();
+    if (blockIdx.x == 0 && b < j.batch) {
+        write_row(j, b, r);
+        if (mine)
+            for (int t = r.row; t < r.end; ++t) place_token(j, b, t, r.row, r.len, r.first, r.served);
+    }
+    const bool search = __syncthreads_or(!mine);
     if (gridDim.x > 1) {
         if (b == 0) s_last = atomicAdd(arrived, 1u) == gridDim.x - 1;
         __syncthreads();
@@ -121,35 +130,40 @@ __global__ __launch_bounds__(kPlanThreads) void assign_kernel(AssignJob j, uint3
     if (gridDim.x == 1 || s_last) {                          // (uniform)
         if (b < j.batch) j.lens_out[b] = r.served ? r.stop : r.len;
         if (b == 0) {
-            *j.left = plan.available - (int)plan.taken;
+            *j.left = plan.available - (int)s_taken;
             if (gridDim.x > 1) __hip_atomic_store(arrived, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
         }
     }
+    if (!search) return;
     const int all = s_end[j.batch - 1];
-    for (int t = (int)blockIdx.x * kPlanThreads + b; t < all; t += (int)gridDim.x * kPlanThreads) {
+    for (int t = (int)blockIdx.x * THREADS + b; t < all; t += (int)gridDim.x * THREADS) {
         int lo = 0;                                          // rows that end at t or before
 #pragma unroll
-        for (int step = kPlanThreads / 2; step; step >>= 1)
+        for (int step = THREADS / 2; step; step >>= 1)
             if (lo + step <= j.batch && s_end[lo + step - 1] <= t) lo += step;
         lo = min(lo, j.batch - 1);
-        place_token(j, lo, t, s_row[lo], s_len[lo], s_first[lo], s_first[lo] != INT_MIN);
+        if (s_end[lo] - s_row[lo] > kOwnTokens) place_token(j, lo, t, s_row[lo], s_len[lo], s_first[lo], s_first[lo] != INT_MIN);
     }
 }
 
 // More rows: one CTA works them out, kPlanThreads at a time, the tokens follow in a launch of their own.
 __global__ __launch_bounds__(kPlanThreads) void assign_rows_kernel(AssignJob j, int32_t* __restrict__ first)
 {
-    __shared__ uint32_t waves[kPlanThreads / 64];
-    AssignPlan plan{0u, 0u, 0u, available_pages(j)};
+    __shared__ uint32_t sums[2][kPlanThreads / 64], s_taken;
+    AssignPlan<kPlanThreads> plan{0u, 0u, 0u, available_pages(j)};
+    if (threadIdx.x == 0) s_taken = 0;
     for (int b0 = 0; b0 < j.batch; b0 += kPlanThreads) {
         const int b = b0 + (int)threadIdx.x;
-        const AssignedRow r = plan.next(j, b, waves);
-        if (b >= j.batch) continue;                          // (nobody meets these threads again)
+        if (b0) __syncthreads();                             // (the sums have been read)
+        const AssignedRow r = plan.next(j, b, sums);
+        if (b >= j.batch) continue;
         write_row(j, b, r);
         j.lens_out[b] = r.served ? r.stop : r.len;
         first[b] = r.served ? r.first : INT_MIN;
     }
-    if (threadIdx.x == 0) *j.left = plan.available - (int)plan.taken;
+    atomicMax(&s_taken, plan.given);
+    __syncthreads();
+    if (threadIdx.x == 0) *j.left = plan.available - (int)s_taken;
 }
 
 __global__ __launch_bounds__(256) void assign_tokens_kernel(AssignJob j, const int32_t* __restrict__ first)
@@ -192,7 +206,7 @@ __global__ __launch_bounds__(256) void release_count_kernel(ReleaseJob j, int32_
 // The first row's first page comes to lie last, so that it is taken first.
 __global__ __launch_bounds__(256) void release_kernel(ReleaseJob j, const int32_t* __restrict__ counts)
 {
-    __shared__ uint32_t waves[4];
+    __shared__ uint32_t waves[2][4];
     const int b = (int)blockIdx.x, tid = threadIdx.x, lane = tid & 63;
     uint32_t before = 0, all = 0, sum;
     for (int i = tid; i < j.batch; i += 256) {
@@ -200,9 +214,9 @@ __global__ __launch_bounds__(256) void release_kernel(ReleaseJob j, const int32_
         all += n;
         before += i < b ? n : 0u;
     }
-    block_sums(before, waves, sum);
+    block_sums<256>(before, waves[0], sum);
     before = sum;
-    block_sums(all, waves, sum);
+    block_sums<256>(all, waves[1], sum);
     all = sum;
     const long top = (long)counts[j.batch] + all;            // pages of the list then
     if (b == 0 && tid == 0) *j.left = (int)min(top, (long)j.capacity);
@@ -210,12 +224,13 @@ __global__ __launch_bounds__(256) void release_kernel(ReleaseJob j, const int32_
     int e0, e1;
     released_entries(j, b, e0, e1);
     for (int base = e0; base < e1; base += 256) {
+        __syncthreads();                                     // (the sums have been read)
         const int e = base + tid;
         int32_t* const entry = j.table + (size_t)b * j.max_pages + e;
         const int id = e < e1 ? *entry : -1;
         const bool live = (uint32_t)id < (uint32_t)j.pool_pages;
         const uint64_t mask = __builtin_amdgcn_ballot_w64(live);
-        const uint32_t until = block_sums(lane == 63 ? (uint32_t)__builtin_popcountll(mask) : 0u, waves, sum);     // of the waves up to this one in the last lane, before it in the others
+        const uint32_t until = block_sums<256>(lane == 63 ? (uint32_t)__builtin_popcountll(mask) : 0u, waves[0], sum);     // of the waves up to this one in the last lane, before it in the others
         const uint32_t rank = (lane == 63 ? until - (uint32_t)__builtin_popcountll(mask) : until) + (uint32_t)__builtin_popcountll(mask & ((uint64_t(1) << lane) - 1));
         if (live) {
             const long at = top - 1 - (long)before - rank;
@@ -232,8 +247,11 @@ hipError_t launch_assign(const AssignJob& j, int num_cu, void* workspace, hipStr
 {
     int32_t* const first = (int32_t*)((char*)workspace + kPagedCounterBytes);
     if (j.batch <= kPlanThreads) {
-        const long blocks = std::min(((long)j.tokens + kPlanThreads - 1) / kPlanThreads, (long)num_cu);
-        hipLaunchKernelGGL(assign_kernel, dim3((unsigned)std::max(blocks, 1L)), dim3(kPlanThreads), 0, stream, j, (uint32_t*)((char*)workspace + kPagedArrivedAt));
+        const unsigned threads = j.batch <= 256 ? 256 : kPlanThreads;
+        // tokens that are not more than the rows' own threads place need one CTA
+        const long blocks = (long)j.tokens <= kOwnTokens * 64 ? 1 : std::min(((long)j.tokens + threads - 1) / threads, (long)num_cu);
+        const auto kernel = threads == 256 ? assign_kernel<256> : assign_kernel<kPlanThreads>;
+        hipLaunchKernelGGL(kernel, dim3((unsigned)std::max(blocks, 1L)), dim3(threads), 0, stream, j, (uint32_t*)((char*)workspace + kPagedArrivedAt));
         return hipGetLastError();
     }
     hipLaunchKernelGGL(assign_rows_kernel, dim3(1), dim3(kPlanThreads), 0, stream, j, first);
