@@ -12,27 +12,29 @@ namespace tmw4 {
 
 namespace {
 
-constexpr int kPlanThreads = 1024;       // most rows that a CTA works out at a time
+constexpr int kPlanThreads = 1024;       // of the CTA that works out many rows,
+constexpr int kPlanRows = 4;             // and rows of each
 constexpr int kOwnTokens = 8;            // of a row that its own thread places
 
-// Inclusive sum over the CTA, at most 2^32 - 1 each; `total` is the CTA's.  `waves` may be used again behind another barrier.
+__device__ __forceinline__ uint32_t add_sat(uint32_t a, uint32_t b) { return __builtin_elementwise_add_sat(a, b); }
+
+// Sum over the threads before this one, at most 2^32 - 1; `total` is the CTA's.  `waves` may be used again behind another barrier.
 template <int THREADS>
-__device__ __forceinline__ uint32_t block_sums(uint32_t v, uint32_t* waves, uint32_t& total)
+__device__ __forceinline__ uint32_t sums_before(uint32_t v, uint32_t* waves, uint32_t& total)
 {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    auto add = [](uint32_t a, uint32_t b) { return __builtin_elementwise_add_sat(a, b); };
-    v = wave_scan(v, add);
+    v = wave_scan(v, add_sat);
     if (lane == 63) waves[wave] = v;
     __syncthreads();
-    uint32_t before = 0;
+    uint32_t before = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x138, 0xf, 0xf, false);           // of the lane before
     total = 0;
 #pragma unroll
     for (int w = 0; w < THREADS / 64; ++w) {
         const uint32_t n = waves[w];
-        before = add(before, w < wave ? n : 0u);
-        total = add(total, n);
+        before = add_sat(before, w < wave ? n : 0u);
+        total = add_sat(total, n);
     }
-    return add(before, v);
+    return before;
 }
 
 // A row: its place in the packed arrays, and number `first - page` of the list is its page `page`.
@@ -41,36 +43,47 @@ struct AssignedRow {
     bool served;
 };
 
-// sums: room for two sums over the CTA.
-template <int THREADS>
+// A thread has the ROWS rows from b on.
+template <int THREADS, int ROWS>
 struct AssignPlan {
     uint32_t tokens, pages;              // of the rows so far: given or not
     uint32_t given;                      // pages given to the thread's rows and all before them, if those were given any
     int available;
-    __device__ __forceinline__ AssignedRow next(const AssignJob& j, int b, uint32_t (*sums)[THREADS / 64])
+    __device__ __forceinline__ void next(const AssignJob& j, int b, uint32_t (*sums)[THREADS / 64], AssignedRow (&r)[ROWS])
     {
         const int cap = j.cap, page = 1 << j.page_log;
-        int len = 0;
-        uint32_t count = 0, all;
-        if (b < j.batch) {
-            len = min(max(j.lens[b], 0), cap);
-            count = (uint32_t)max(j.counts[b], 0);
+        uint32_t count[ROWS], need[ROWS], own = 0, all;
+#pragma unroll
+        for (int i = 0; i < ROWS; ++i) {
+            count[i] = 0;
+            r[i].len = 0;
+            if (b + i < j.batch) {
+                r[i].len = min(max(j.lens[b + i], 0), cap);
+                count[i] = (uint32_t)max(j.counts[b + i], 0);
+            }
+            own = add_sat(own, count[i]);
         }
-        AssignedRow r;
-        const uint32_t end = __builtin_elementwise_add_sat(block_sums<THREADS>(count, sums[0], all), tokens);
-        r.end = (int)min(end, (uint32_t)j.tokens);
-        r.row = (int)min(end == ~0u ? ~0u : end - count, (uint32_t)j.tokens);
-        tokens = __builtin_elementwise_add_sat(tokens, all);
-        r.len = len;
-        r.stop = (int)min((uint32_t)len + (uint32_t)(r.end - r.row), (uint32_t)cap);
-        const int have = (len + page - 1) >> j.page_log;
-        const uint32_t need = (uint32_t)max(((r.stop + page - 1) >> j.page_log) - have, 0);
-        const uint32_t until = block_sums<THREADS>(need, sums[1], all) + pages;         // (at most tokens / 32 + batch)
+        uint32_t at = add_sat(sums_before<THREADS>(own, sums[0], all), tokens);
+        tokens = add_sat(tokens, all);
+        own = 0;
+#pragma unroll
+        for (int i = 0; i < ROWS; ++i) {
+            r[i].row = (int)min(at, (uint32_t)j.tokens);
+            at = add_sat(at, count[i]);
+            r[i].end = (int)min(at, (uint32_t)j.tokens);
+            r[i].stop = (int)min((uint32_t)r[i].len + (uint32_t)(r[i].end - r[i].row), (uint32_t)cap);
+            need[i] = (uint32_t)max(((r[i].stop + page - 1) >> j.page_log) - ((r[i].len + page - 1) >> j.page_log), 0);
+            own += need[i];                                  // (all rows' together: at most tokens / 32 + batch)
+        }
+        uint32_t until = sums_before<THREADS>(own, sums[1], all) + pages;
         pages += all;
-        r.served = need == 0 || until <= (uint32_t)available;
-        r.first = available - 1 - (int)(until - need) + have;
-        if (r.served && need) given = until;
-        return r;
+#pragma unroll
+        for (int i = 0; i < ROWS; ++i) {
+            r[i].first = available - 1 - (int)until + ((r[i].len + page - 1) >> j.page_log);
+            until += need[i];
+            r[i].served = need[i] == 0 || until <= (uint32_t)available;
+            if (r[i].served && need[i]) given = until;
+        }
     }
 };
 
@@ -99,67 +112,78 @@ __device__ __forceinline__ void place_token(const AssignJob& j, int b, int t, in
     if (j.slots) j.slots[t] = (uint32_t)id < (uint32_t)j.pool_pages ? (int64_t)id << j.page_log | (at & (page - 1)) : -1;
 }
 
-// Up to THREADS rows: every CTA works out the rows for itself and places its share of the tokens: the first one, a thread a row, those of rows with up to kOwnTokens of them, and the others
-// by search.  The lengths and the list's count may be updated in place, so they are written by the CTA that is last to have read them.
-template <int THREADS>
+// Up to THREADS * ROWS rows: every CTA works out the rows for itself and places its share of the tokens: the first one, a thread its rows, those of rows with up to kOwnTokens of them, and
+// the others by search.  The lengths and the list's count may be updated in place, so they are written by the CTA that is last to have read them.
+template <int THREADS, int ROWS>
 __global__ __launch_bounds__(THREADS) void assign_kernel(AssignJob j, uint32_t* arrived)
 {
     __shared__ uint32_t sums[2][THREADS / 64], s_last, s_taken;
-    __shared__ int s_end[THREADS], s_row[THREADS], s_len[THREADS], s_first[THREADS];
-    const int b = threadIdx.x;
-    if (b == 0) s_taken = 0;
-    AssignPlan<THREADS> plan{0u, 0u, 0u, available_pages(j)};
-    const AssignedRow r = plan.next(j, b, sums);
-    const bool mine = r.end - r.row <= kOwnTokens;           // to place by its own thread
+    __shared__ int s_end[THREADS * ROWS], s_len[THREADS * ROWS], s_first[THREADS * ROWS];
+    const int tid = threadIdx.x, b = tid * ROWS;
+    if (tid == 0) s_taken = 0;
+    AssignPlan<THREADS, ROWS> plan{0u, 0u, 0u, available_pages(j)};
+    AssignedRow r[ROWS];
+    plan.next(j, b, sums, r);
+    bool mine = true;                                        // to place by their own thread
     const uint32_t given = wave_greatest(plan.given);
-    if ((b & 63) == 0 && given) atomicMax(&s_taken, given);
-    s_end[b] = b < j.batch ? r.end : j.tokens;
-    s_row[b] = r.row;
-    s_len[b] = r.len;
-    s_first[b] = r.served ? r.first : INT_MIN;
-    if (blockIdx.x == 0 && b < j.batch) {
-        write_row(j, b, r);
-        if (mine)
-            for (int t = r.row; t < r.end; ++t) place_token(j, b, t, r.row, r.len, r.first, r.served);
+    if ((tid & 63) == 0 && given) atomicMax(&s_taken, given);
+#pragma unroll
+    for (int i = 0; i < ROWS; ++i) {
+        mine = mine && r[i].end - r[i].row <= kOwnTokens;
+        s_end[b + i] = r[i].end;
+        s_len[b + i] = r[i].len;
+        s_first[b + i] = r[i].served ? r[i].first : INT_MIN;
+        if (blockIdx.x == 0 && b + i < j.batch) {
+            write_row(j, b + i, r[i]);
+            if (r[i].end - r[i].row <= kOwnTokens)
+                for (int t = r[i].row; t < r[i].end; ++t) place_token(j, b + i, t, r[i].row, r[i].len, r[i].first, r[i].served);
+        }
     }
     const bool search = __syncthreads_or(!mine);
     if (gridDim.x > 1) {
-        if (b == 0) s_last = atomicAdd(arrived, 1u) == gridDim.x - 1;
+        if (tid == 0) s_last = atomicAdd(arrived, 1u) == gridDim.x - 1;
         __syncthreads();
     }
     if (gridDim.x == 1 || s_last) {                          // (uniform)
-        if (b < j.batch) j.lens_out[b] = r.served ? r.stop : r.len;
-        if (b == 0) {
+#pragma unroll
+        for (int i = 0; i < ROWS; ++i)
+            if (b + i < j.batch) j.lens_out[b + i] = r[i].served ? r[i].stop : r[i].len;
+        if (tid == 0) {
             *j.left = plan.available - (int)s_taken;
             if (gridDim.x > 1) __hip_atomic_store(arrived, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
         }
     }
     if (!search) return;
     const int all = s_end[j.batch - 1];
-    for (int t = (int)blockIdx.x * THREADS + b; t < all; t += (int)gridDim.x * THREADS) {
+    for (int t = (int)blockIdx.x * THREADS + tid; t < all; t += (int)gridDim.x * THREADS) {
         int lo = 0;                                          // rows that end at t or before
 #pragma unroll
-        for (int step = THREADS / 2; step; step >>= 1)
+        for (int step = THREADS * ROWS / 2; step; step >>= 1)
             if (lo + step <= j.batch && s_end[lo + step - 1] <= t) lo += step;
         lo = min(lo, j.batch - 1);
-        if (s_end[lo] - s_row[lo] > kOwnTokens) place_token(j, lo, t, s_row[lo], s_len[lo], s_first[lo], s_first[lo] != INT_MIN);
+        const int row = lo ? s_end[lo - 1] : 0;
+        if (s_end[lo] - row > kOwnTokens) place_token(j, lo, t, row, s_len[lo], s_first[lo], s_first[lo] != INT_MIN);
     }
 }
 
-// More rows: one CTA works them out, kPlanThreads at a time, the tokens follow in a launch of their own.
+// More rows: one CTA works them out, some thousand at a time, the tokens follow in a launch of their own.
 __global__ __launch_bounds__(kPlanThreads) void assign_rows_kernel(AssignJob j, int32_t* __restrict__ first)
 {
     __shared__ uint32_t sums[2][kPlanThreads / 64], s_taken;
-    AssignPlan<kPlanThreads> plan{0u, 0u, 0u, available_pages(j)};
+    AssignPlan<kPlanThreads, kPlanRows> plan{0u, 0u, 0u, available_pages(j)};
     if (threadIdx.x == 0) s_taken = 0;
-    for (int b0 = 0; b0 < j.batch; b0 += kPlanThreads) {
-        const int b = b0 + (int)threadIdx.x;
+    for (int b0 = 0; b0 < j.batch; b0 += kPlanThreads * kPlanRows) {
+        const int b = b0 + (int)threadIdx.x * kPlanRows;
         if (b0) __syncthreads();                             // (the sums have been read)
-        const AssignedRow r = plan.next(j, b, sums);
-        if (b >= j.batch) continue;
-        write_row(j, b, r);
-        j.lens_out[b] = r.served ? r.stop : r.len;
-        first[b] = r.served ? r.first : INT_MIN;
+        AssignedRow r[kPlanRows];
+        plan.next(j, b, sums, r);
+#pragma unroll
+        for (int i = 0; i < kPlanRows; ++i) {
+            if (b + i >= j.batch) continue;
+            write_row(j, b + i, r[i]);
+            j.lens_out[b + i] = r[i].served ? r[i].stop : r[i].len;
+            first[b + i] = r[i].served ? r[i].first : INT_MIN;
+        }
     }
     atomicMax(&s_taken, plan.given);
     __syncthreads();
@@ -207,16 +231,16 @@ __global__ __launch_bounds__(256) void release_count_kernel(ReleaseJob j, int32_
 __global__ __launch_bounds__(256) void release_kernel(ReleaseJob j, const int32_t* __restrict__ counts)
 {
     __shared__ uint32_t waves[2][4];
-    const int b = (int)blockIdx.x, tid = threadIdx.x, lane = tid & 63;
+    const int b = (int)blockIdx.x, tid = threadIdx.x;
     uint32_t before = 0, all = 0, sum;
     for (int i = tid; i < j.batch; i += 256) {
         const uint32_t n = (uint32_t)counts[i];
         all += n;
         before += i < b ? n : 0u;
     }
-    block_sums<256>(before, waves[0], sum);
+    sums_before<256>(before, waves[0], sum);
     before = sum;
-    block_sums<256>(all, waves[1], sum);
+    sums_before<256>(all, waves[1], sum);
     all = sum;
     const long top = (long)counts[j.batch] + all;            // pages of the list then
     if (b == 0 && tid == 0) *j.left = (int)min(top, (long)j.capacity);
@@ -229,9 +253,7 @@ __global__ __launch_bounds__(256) void release_kernel(ReleaseJob j, const int32_
         int32_t* const entry = j.table + (size_t)b * j.max_pages + e;
         const int id = e < e1 ? *entry : -1;
         const bool live = (uint32_t)id < (uint32_t)j.pool_pages;
-        const uint64_t mask = __builtin_amdgcn_ballot_w64(live);
-        const uint32_t until = block_sums<256>(lane == 63 ? (uint32_t)__builtin_popcountll(mask) : 0u, waves[0], sum);     // of the waves up to this one in the last lane, before it in the others
-        const uint32_t rank = (lane == 63 ? until - (uint32_t)__builtin_popcountll(mask) : until) + (uint32_t)__builtin_popcountll(mask & ((uint64_t(1) << lane) - 1));
+        const uint32_t rank = sums_before<256>(live ? 1u : 0u, waves[0], sum);
         if (live) {
             const long at = top - 1 - (long)before - rank;
             if (at >= 0 && at < j.capacity) j.pages[at] = id;
@@ -246,11 +268,11 @@ __global__ __launch_bounds__(256) void release_kernel(ReleaseJob j, const int32_
 hipError_t launch_assign(const AssignJob& j, int num_cu, void* workspace, hipStream_t stream)
 {
     int32_t* const first = (int32_t*)((char*)workspace + kPagedCounterBytes);
-    if (j.batch <= kPlanThreads) {
+    if (j.batch <= kPlanThreads * kPlanRows) {
         const unsigned threads = j.batch <= 256 ? 256 : kPlanThreads;
         // tokens that are not more than the rows' own threads place need one CTA
         const long blocks = (long)j.tokens <= kOwnTokens * 64 ? 1 : std::min(((long)j.tokens + threads - 1) / threads, (long)num_cu);
-        const auto kernel = threads == 256 ? assign_kernel<256> : assign_kernel<kPlanThreads>;
+        const auto kernel = j.batch <= 256 ? assign_kernel<256, 1> : j.batch <= kPlanThreads ? assign_kernel<kPlanThreads, 1> : assign_kernel<kPlanThreads, kPlanRows>;
         hipLaunchKernelGGL(kernel, dim3((unsigned)std::max(blocks, 1L)), dim3(threads), 0, stream, j, (uint32_t*)((char*)workspace + kPagedArrivedAt));
         return hipGetLastError();
     }

@@ -104,7 +104,7 @@ def test_assign(tm, lens, counts, page, max_pages, spare):
     Rows(tm, lens, page, max_pages, spare).check(counts, tokens=5000 if total > 100000 else None)
 
 
-@pytest.mark.parametrize("batch", [1, 63, 64, 65, 1000, 1024, 1025, 2048, 5000])
+@pytest.mark.parametrize("batch", [1, 63, 64, 65, 256, 257, 1000, 1024, 1025, 2048, 4096, 4097, 9001])
 @pytest.mark.parametrize("kind", ["decode", "mixed", "scarce"])
 def test_assign_many_rows(tm, batch, kind):
     print(f"assign batch={batch} {kind}", file=sys.stderr, flush=True)
@@ -116,7 +116,7 @@ def test_assign_many_rows(tm, batch, kind):
 
 
 @pytest.mark.parametrize("tokens", [0, 1, 30, 64, 100])
-@pytest.mark.parametrize("batch", [3, 1500])
+@pytest.mark.parametrize("batch", [3, 1500, 5000])
 def test_packed_arrays_that_are_too_small(tm, tokens, batch):
     Rows(tm, [20] * batch, 32, 4, 2 * batch).check([33] * batch, tokens=tokens)
 
@@ -185,7 +185,7 @@ def test_what_goes_back_comes_again(tm, batch, wide):
     assert torch.equal(r.T, table) and torch.equal(slots, first)
 
 
-@pytest.mark.parametrize("batch", [40, 1100])
+@pytest.mark.parametrize("batch", [40, 1100, 5000])
 def test_captured_steps_go_on(tm, batch):
     """A captured step that updates lengths and list in place, replayed: every replay goes on where the last one ended.  Eager work between the replays."""
     import torch
