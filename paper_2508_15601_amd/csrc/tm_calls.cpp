@@ -138,6 +138,8 @@ void call(F&& f)
     throw Failed{};
 }
 
+thread_local int t_device = -1;                          // the current device, asked for once a call
+
 // Shared frame of the entry points: argument count, exceptions, and the object handed back (the output tensor or None).
 template <class F>
 PyObject* entry(Py_ssize_t have, Py_ssize_t want, PyObject* result, F&& f)
@@ -146,6 +148,7 @@ PyObject* entry(Py_ssize_t have, Py_ssize_t want, PyObject* result, F&& f)
         PyErr_Format(PyExc_TypeError, "expected %zd arguments, got %zd", want, have);
         return nullptr;
     }
+    t_device = -1;
     try {
         f();
     } catch (const Failed&) {
@@ -327,8 +330,9 @@ constexpr const char* kPagedFreed = "paged cache already freed";
 
 void on_current_device(const at::Tensor& t, const char* what)
 {
-    if (t.get_device() != c10::hip::current_device()) {
-        PyErr_Format(PyExc_ValueError, "%s is on device %d, the current device is %d", what, (int)t.get_device(), (int)c10::hip::current_device());
+    if (t_device < 0) t_device = (int)c10::hip::current_device();
+    if (t.get_device() != t_device) {
+        PyErr_Format(PyExc_ValueError, "%s is on device %d, the current device is %d", what, (int)t.get_device(), t_device);
         throw Failed{};
     }
 }

@@ -202,6 +202,19 @@ __device__ __forceinline__ SixteenthWeights sixteenth_weights(const HeadNorm& n,
     return w;
 }
 
+// What a lane keeps of the norm of a head's sixteenth; nothing where heads are not normed.
+template <class Heads>
+struct SixteenthNorm {
+    __device__ __forceinline__ SixteenthNorm(const RopePlan&, int) {}
+};
+template <>
+struct SixteenthNorm<AppendHeads> {
+    Sixteenth at;
+    SixteenthWeights w;
+    __device__ __forceinline__ SixteenthNorm(const RopePlan& r, int lane) : at(r, lane), w{} {}
+    __device__ __forceinline__ void request(const HeadNorm& n, int h) { w = sixteenth_weights(n, h, at); }
+};
+
 // The lane's dimensions 8 * sub ..; cs without gaps.
 __device__ __forceinline__ u32x4 head_sixteenth(u32x4 raw, const SixteenthWeights& w, const Sixteenth& s, const HeadNorm& n, const RopePlan& r, const CosSin* cs, int lane)
 {

@@ -41,9 +41,8 @@ __device__ __forceinline__ void append_run(const PagedPool& pool, const PagedSeq
         }
     };
     request(h0);
-    const Sixteenth sixteenth(rope, lane);
-    SixteenthWeights weights{};
-    if constexpr (kHeads) weights = sixteenth_weights(heads.k, h0, sixteenth);
+    SixteenthNorm<Heads> norm(rope, lane);
+    if constexpr (kHeads) norm.request(heads.k, h0);
     if (rope.rot) {
         const int pairs = rope.rot / 2, at_once = 64 / pairs, tok = lane / pairs, p = lane - tok * pairs;      // tokens of a wave at a time
         if (tok < at_once) {
@@ -68,7 +67,7 @@ __device__ __forceinline__ void append_run(const PagedPool& pool, const PagedSeq
             const int which = it >> 1, u = slot[it & 1];
             const bool live = u >= u0 && u < u1;
             if constexpr (kHeads) {
-                if (which == 0) raw[it] = head_sixteenth(raw[it], weights, sixteenth, heads.k, rope, cs + (live ? u : u0) * (kHeadDim / 2), lane);
+                if (which == 0) raw[it] = head_sixteenth(raw[it], norm.w, norm.at, heads.k, rope, cs + (live ? u : u0) * (kHeadDim / 2), lane);
             } else {
                 if (which == 0 && rope.rot) raw[it] = rope_sixteenth(raw[it], rope, cs + (live ? u : u0) * (kHeadDim / 2), lane);
             }
@@ -105,7 +104,7 @@ __device__ __forceinline__ void append_run(const PagedPool& pool, const PagedSeq
         __syncthreads();
         if (h + 1 < h1) request(h + 1);
         if constexpr (kHeads) {
-            if (h + 1 < h1 && heads.k.stride) weights = sixteenth_weights(heads.k, h + 1, sixteenth);
+            if (h + 1 < h1 && heads.k.stride) norm.request(heads.k, h + 1);
         }
         if constexpr (BITS == 8) {
             const u32x4 kc = *reinterpret_cast<const u32x4*>(lds + tid * 16);
@@ -224,9 +223,8 @@ __global__ __launch_bounds__(256) void paged_append_tokens_kernel(PagedPool pool
     if (b >= seqs.batch) return;
     const PagedSeq s = paged_seq(seqs, b);
     const int which = vec < pool.heads ? 0 : vec < 2 * pool.heads ? 1 : 2, h = vec - which * pool.heads;   // keys, values, queries
-    const Sixteenth sixteenth(rope, lane);
-    SixteenthWeights weights{};
-    if constexpr (kHeads) weights = sixteenth_weights(which == 2 ? heads.q : heads.k, which == 2 ? max(min(h, q_heads - 1), 0) : h, sixteenth);
+    SixteenthNorm<Heads> norm(rope, lane);
+    if constexpr (kHeads) norm.request(which == 2 ? heads.q : heads.k, which == 2 ? max(min(h, q_heads - 1), 0) : h);
     for (int i = (int)(token - (uint32_t)b * step); i < s.count; i += step) {
         const int pos = (int)((uint32_t)s.pos + (uint32_t)i);
         const long row = (long)s.row + i;
@@ -244,7 +242,7 @@ __global__ __launch_bounds__(256) void paged_append_tokens_kernel(PagedPool pool
             __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
             __builtin_amdgcn_wave_barrier();
             if constexpr (kHeads) {
-                if (which != 1) raw = head_sixteenth(raw, weights, sixteenth, which == 2 ? heads.q : heads.k, rope, cs[wave], lane);
+                if (which != 1) raw = head_sixteenth(raw, norm.w, norm.at, which == 2 ? heads.q : heads.k, rope, cs[wave], lane);
             } else {
                 const u32x4 turned = rope_sixteenth(raw, rope, cs[wave], lane);
                 if (which != 1) raw = turned;
