@@ -94,24 +94,27 @@ __device__ __forceinline__ void attn_rows(const RowsJob& job, const uint8_t* kco
     };
     constexpr int kChunks = BITS == 8 ? 256 : 128;                                  // of 16 bytes a run
     const int mine = (BITS == 8 ? wave >> 2 : wave >> 1) & 1;
-    // Entries of the table for 64 pages at a time, a lane each; loading the entry of a run when its turn comes made all waves stand still twice a stage.  They still do once: in the
-    // generated code every stage waits for all of its wave's loads in front of the two reads of `ids`, the codes and pairs that it has just requested among them, since one path
-    // to there has loaded `ids` and the compiler keeps one account for all.
-    int ids = -1, ids_at = -64;                            // of pages ids_at .. ids_at + 63 of the sequence
-    auto runs_of = [&](int st) {
+    // The table's entries are scalar loads, requested a stage before they are looked at: as vector loads they would stand in line with the codes and pairs, and a wait for them would be
+    // one for those.
+    struct StageEntries {
+        int id[2];
+    };
+    const int last_run = max(len_all - 1, 0) / kRun;
+    auto entries_of = [&](int st) {
+        StageEntries e{{-1, -1}};
+        if constexpr (PAGED) {
+#pragma unroll
+            for (int n = 0; n < 2; ++n) e.id[n] = paged_entry(where.pool, where.seqs, where.b, min(run_of(st, n), last_run));
+        }
+        return e;
+    };
+    auto runs_of = [&](int st, const StageEntries& e) {
         StageRuns r{{-1, -1}};
         if constexpr (PAGED) {
 #pragma unroll
             for (int n = 0; n < 2; ++n) {
                 const int run = run_of(st, n);
-                if (run * kRun >= len_all) continue;
-                const int page = run >> where.pool.run_log;
-                if (page >= ids_at + 64) {
-                    ids_at = page;
-                    ids = page + lane < where.seqs.max_pages ? where.seqs.table[(size_t)where.b * where.seqs.max_pages + page + lane] : -1;
-                }
-                const int id = __builtin_amdgcn_readlane(ids, page - ids_at);
-                if ((uint32_t)id < (uint32_t)where.pool.pages) r.at[n] = (int)paged_run(where.pool, id, where.hk, run);
+                if (run <= last_run && (uint32_t)e.id[n] < (uint32_t)where.pool.pages) r.at[n] = (int)paged_run(where.pool, e.id[n], where.hk, run);
             }
         }
         return r;
@@ -234,7 +237,8 @@ __device__ __forceinline__ void attn_rows(const RowsJob& job, const uint8_t* kco
         asm volatile("" ::: "memory");
     };
 
-    StageRuns run0 = runs_of(0), run1 = runs_of(1);        // of the stages whose codes and pairs are requested next
+    StageEntries next = entries_of(2), after = entries_of(3);
+    StageRuns run0 = runs_of(0, entries_of(0)), run1 = runs_of(1, entries_of(1));      // of the stages whose codes and pairs are requested next
     note(0, run0);
     note(1, run1);
     load_codes(0, run0);
@@ -242,13 +246,14 @@ __device__ __forceinline__ void attn_rows(const RowsJob& job, const uint8_t* kco
     store_pairs(0);
     load_pairs(1, run1);
     store_pairs(1);
-    run0 = runs_of(2);
+    run0 = runs_of(2, next);
     note(2, run0);
     load_pairs(2, run0);
     barrier();
     convert_stage(0);
     load_codes(1, run1);
-    run1 = runs_of(3);
+    run1 = runs_of(3, after);
+    next = entries_of(4);
 
 #pragma unroll
     for (int t = 0; t < 8; ++t)
@@ -324,7 +329,8 @@ __device__ __forceinline__ void attn_rows(const RowsJob& job, const uint8_t* kco
         if constexpr (PAGED) {
             run0 = run1;
             note(st + 3, run0);                            // (stage st - 1 has been scored)
-            run1 = runs_of(st + 4);
+            run1 = runs_of(st + 4, next);
+            next = entries_of(st + 5);
         }
 #pragma unroll
         for (int sub = 0; sub < NB; ++sub) {
