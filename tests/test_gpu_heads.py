@@ -256,6 +256,35 @@ def test_text_positions_stand_on_every_axis(tm):
     assert torch.equal(out[0][1:-2], out[1][1:-2]) and all(torch.equal(p, q) for p, q in zip(a.contents(), b.contents()))
 
 
+@pytest.mark.parametrize("counts, max_count", [([1, 1], 1), ([3, 70], 0)])
+def test_positions_of_their_own_on_one_axis(tm, counts, max_count):
+    """What a key is turned by need not be where it is stored (a context that was cut, say)."""
+    import torch
+    a, b = (Pool(tm, 8, 32, 2, counts, [50, 7], seed=6, max_count=max_count) for _ in range(2))
+    x = torch.randn(a.tokens, 8, 128, device="cuda").half()
+    at = torch.randint(0, 1 << 30, (a.tokens,), device="cuda", dtype=torch.int32)
+    rope = tm.tm_rope_create(96)
+    turned, out = torch.empty_like(x), torch.empty_like(x)
+    tm.tm_rope_apply(x, at, rope, turned)
+    tm.tm_paged_append(a.cache, a.batch, turned[:, :2], x[:, 2:4])
+    tm.tm_paged_append(b.cache, b.batch, x[:, :2], x[:, 2:4], rope=rope, Q=x, Q_out=out, positions=at)
+    assert torch.equal(out[1:-2], turned[1:-2]) and all(torch.equal(p, q) for p, q in zip(a.contents(), b.contents()))
+
+
+def test_rows_further_apart_than_32_bits_count(tm):
+    import torch
+    far = (1 << 30) + 8
+    space = torch.empty(2 * far + 4096, dtype=torch.float16, device="cuda")
+    X = space.as_strided((3, 2, 128), (far, 128, 1))
+    X.copy_(torch.randn(3, 2, 128, device="cuda"))
+    pos = torch.tensor([5, 6, 7], dtype=torch.int32, device="cuda")
+    rope, norm = tm.tm_rope_create(128), tm.HeadNorm(torch.randn(128, device="cuda").half())
+    want = torch.empty(3, 2, 128, dtype=torch.float16, device="cuda")
+    tm.tm_heads_apply(rope=rope, positions=pos, Q=X.contiguous(), Q_out=want, q_norm=norm)
+    tm.tm_heads_apply(rope=rope, positions=pos, Q=X, Q_out=X, q_norm=norm)
+    assert torch.equal(X, want)
+
+
 def test_heads_in_a_graph_and_on_another_stream(tm):
     import torch
     s = Heads(tm, 50, 8, 2, 128, 128, "half", 3)
