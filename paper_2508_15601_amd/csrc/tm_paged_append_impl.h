@@ -186,8 +186,8 @@ __device__ __forceinline__ void rotate_row(const PagedSeqs& seqs, PagedRows q, u
 
 // Blocks 0 .. kv_blocks - 1: runs of keys and values, heads of a run next to each other; the blocks behind them: queries, a wave `per_wave` heads of a row.
 template <int BITS, class Heads>
-__global__ __launch_bounds__(256) void paged_append_kernel(PagedPool pool, PagedSeqs seqs, PagedRows k, PagedRows v, RopePlan rope, Heads heads, unsigned kv_blocks, int kv_heads,
-                                                           PagedRows q, uint16_t* q_out, long q_out_stride, int q_heads, int per_wave)
+__global__ __launch_bounds__(256) void paged_append_kernel(PagedPool pool, PagedSeqs seqs, PagedRows k, PagedRows v, RopePlan rope, unsigned kv_blocks, int kv_heads,
+                                                           PagedRows q, uint16_t* q_out, long q_out_stride, int q_heads, int per_wave, Heads heads)
 {
     __shared__ __align__(16) unsigned char lds[kAppendLds];
     __shared__ CosSin cs[kRun * kHeadDim / 2];
@@ -211,8 +211,8 @@ __global__ __launch_bounds__(256) void paged_append_kernel(PagedPool pool, Paged
 template <int BITS>
 constexpr int kFewTokens = BITS == 8 ? 8 : 1;
 template <int BITS, class Heads>
-__global__ __launch_bounds__(256) void paged_append_tokens_kernel(PagedPool pool, PagedSeqs seqs, PagedRows k, PagedRows v, RopePlan rope, Heads heads, PagedRows q, uint16_t* q_out,
-                                                                  long q_out_stride, int q_heads, int per_token, int step)
+__global__ __launch_bounds__(256) void paged_append_tokens_kernel(PagedPool pool, PagedSeqs seqs, PagedRows k, PagedRows v, RopePlan rope, PagedRows q, uint16_t* q_out,
+                                                                  long q_out_stride, int q_heads, int per_token, int step, Heads heads)
 {
     constexpr bool kHeads = std::is_same<Heads, AppendHeads>::value;
     __shared__ CosSin cs[4][kHeadDim / 2];
@@ -301,7 +301,7 @@ hipError_t launch_append(const PagedPool& pool, const PagedSeqs& seqs, PagedRows
     if (max_count >= 1 && max_count <= (pool.bits == 8 ? kFewTokens<8> : kFewTokens<4>) && (long)seqs.batch * max_count * per_token <= 4 * most_ctas(256)) {
         const long blocks = ((long)seqs.batch * max_count * per_token + 3) / 4;
         const auto kernel = pool.bits == 8 ? paged_append_tokens_kernel<8, Heads> : paged_append_tokens_kernel<4, Heads>;
-        hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(256), 0, stream, pool, seqs, k, v, plan, of_heads, q, q_out, q_out_stride, heads, per_token, max_count);
+        hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(256), 0, stream, pool, seqs, k, v, plan, q, q_out, q_out_stride, heads, per_token, max_count, of_heads);
         return hipGetLastError();
     }
     // KV heads a CTA: they share a run's sines and cosines, but take their turns, so that only pays where a compute unit has more CTAs than it holds at a time.  By runs x heads (us; one, two
@@ -316,7 +316,7 @@ hipError_t launch_append(const PagedPool& pool, const PagedSeqs& seqs, PagedRows
     const long jobs = q.p ? (long)seqs.tokens * ((q_heads + per_wave - 1) / per_wave) : 0, blocks = kv + (jobs + 3) / 4;
     if (blocks <= 0 || blocks > most_ctas(256)) return hipErrorInvalidConfiguration;
     const auto kernel = pool.bits == 8 ? paged_append_kernel<8, Heads> : paged_append_kernel<4, Heads>;
-    hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(256), 0, stream, pool, seqs, k, v, plan, of_heads, (unsigned)kv, kv_heads, q, q_out, q_out_stride, q_heads, per_wave);
+    hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(256), 0, stream, pool, seqs, k, v, plan, (unsigned)kv, kv_heads, q, q_out, q_out_stride, q_heads, per_wave, of_heads);
     return hipGetLastError();
 }
 

@@ -23,8 +23,8 @@ struct RopePlan {
     const RopeTurn* turns;               // [rot / 2] F of every pair (device)
     double amp;                          // factor of the rotated values
     int rot;                             // dimensions that are rotated, a multiple of 16
-    int interleaved;                     // pairs are (2i, 2i + 1); otherwise (i, i + rot / 2)
-    int axes;                            // positions of a token
+    int16_t interleaved;                 // pairs are (2i, 2i + 1); otherwise (i, i + rot / 2)
+    int16_t axes;                        // positions of a token
 };
 
 struct CosSin {

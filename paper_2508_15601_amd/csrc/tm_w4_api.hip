@@ -2089,7 +2089,7 @@ int tm_rope_axes(const tm_rope* rope)
     return rope->axes;
 }
 
-static RopePlan rope_plan(const tm_rope* r) { return r ? RopePlan{r->turns, r->amp, r->rot, r->interleaved, r->axes} : RopePlan{nullptr, 1.0, 0, 0, 1}; }
+static RopePlan rope_plan(const tm_rope* r) { return r ? RopePlan{r->turns, r->amp, r->rot, (int16_t)r->interleaved, (int16_t)r->axes} : RopePlan{nullptr, 1.0, 0, 0, 1}; }
 
 // A packed array of [rows][values]: alignment and stride.
 static int check_rows(const char* what, const void* p, int64_t stride, int64_t values)
