@@ -8,9 +8,10 @@
 //     the pieces are every CTA works out by itself from the sequences' lengths (piece_stages), which the host does not know.  A second kernel puts a row's pieces together in
 //     their order, so results do not depend on which is done first.
 //
-// Measured (32 / 8 heads): prompts of 6000, 5000, 4000 and 3000 tokens, 8-bit: 860 us (0.82 PFLOP/s), 4-bit 853; 512 tokens after 30000, 4-bit: 297 us (0.85 PFLOP/s), 1024 without
-// pieces; 100 after 8000, 8-bit: 42 us, 259 without pieces; one prompt of 4000: 163.  (Calls in a row; after an idle time, until the clock is up, a sixth more.)  What bounds it is the issue of
-// vector and matrix instructions (tm_attn_prefill.hip) and a wait for memory in every stage (tm_attn_rows_impl.h); a piece of 256 rows leaves 133 KB in memory.
+// Measured (32 / 8 heads): prompts of 6000, 5000, 4000 and 3000 tokens, 8-bit: 840 us (0.84 PFLOP/s), 4-bit 845; 512 tokens after 30000, 4-bit: 285 us (0.89 PFLOP/s), 1024 without
+// pieces; 100 after 8000, 8-bit: 41 us, 259 without pieces; one prompt of 4000: 162.  (Calls in a row; after an idle time, until the clock is up, a sixth more.)  What bounds it is the issue of
+// vector and matrix instructions (tm_attn_prefill.hip); page numbers as vector loads, which made every stage wait for all of its wave's loads, took 295 and 870 us in place of 285 and 855 of the
+// same run; a piece of 256 rows leaves 133 KB in memory.
 #include "tm_paged_rows_impl.h"
 
 namespace tmw4 {

@@ -2,6 +2,10 @@
 //
 // Rows' tokens and pages are two prefix sums over the rows: where a row's tokens lie in the packed arrays, and which pages of the list are its.  Everything else is a thread's own: a
 // token's page is an entry that the row had, or a page of the list, and the token that begins a page writes the entry.
+//
+// Measured: 256 rows of one new token 4.2 us a call (2.7 in a graph), 1000 rows with 45000 tokens 5.1, 64 rows with 66000 6.8, 2048 rows of one token 7.9.  A launch, and a chain of trips to memory:
+// lengths, table or list, results, with two sums over the CTA between; the host's part of the call is longer than the kernel's up to some thousand tokens.  Rows of more than kOwnTokens new tokens are
+// searched for by each token, 0.5 us.
 #include "tm_paged_host.h"
 
 #include <limits.h>
