@@ -180,7 +180,7 @@ typedef struct tm_paged_step {
 /*
  * Gives the rows' new tokens pages, in the order of the rows: table, offsets and positions are then those of a tm_paged_batch.  A row whose pages, with those of all rows before it,
  * are more than the list has gets none: its new entries become -1, its tokens have no slots, its length stays; rows that need no page are served all the same.  Tokens at positions from
- * max_pages * page_tokens on have no slots and do not count into lens_out.  Arrays that are written must not overlap others but as said.  Uses the cache's workspace.
+ * max_pages * page_tokens on have no slots and do not count into lens_out.  Arrays that are written must not overlap others but as said (refused).  Uses the cache's workspace.
  */
 TM_API int tm_paged_assign(tm_paged_cache* cache, const tm_page_list* list, const tm_paged_step* step, tm_stream stream);
 

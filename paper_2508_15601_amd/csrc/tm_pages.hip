@@ -158,8 +158,9 @@ __global__ __launch_bounds__(THREADS) void assign_kernel(AssignJob j, uint32_t* 
         }
     }
     if (!search) return;
-    const int all = s_end[j.batch - 1];
-    for (int t = (int)blockIdx.x * THREADS + tid; t < all; t += (int)gridDim.x * THREADS) {
+    const uint32_t all = (uint32_t)s_end[j.batch - 1];
+    for (uint32_t at = blockIdx.x * THREADS + tid; at < all; at += gridDim.x * THREADS) {     // (below 2^31, and a step is at most 2^18)
+        const int t = (int)at;
         int lo = 0;                                          // rows that end at t or before
 #pragma unroll
         for (int step = THREADS * ROWS / 2; step; step >>= 1)
@@ -196,8 +197,9 @@ __global__ __launch_bounds__(kPlanThreads) void assign_rows_kernel(AssignJob j, 
 
 __global__ __launch_bounds__(256) void assign_tokens_kernel(AssignJob j, const int32_t* __restrict__ first)
 {
-    const int t = (int)(blockIdx.x * 256 + threadIdx.x);
-    if (t >= j.offsets[j.batch]) return;
+    const uint32_t at = blockIdx.x * 256 + threadIdx.x;
+    if (at >= (uint32_t)j.offsets[j.batch]) return;
+    const int t = (int)at;
     int lo = 0;                                              // rows that end at t or before
     for (int step = 1 << 15; step; step >>= 1)
         if (lo + step <= j.batch && j.offsets[lo + step] <= t) lo += step;

@@ -2309,6 +2309,26 @@ int tm_paged_read(const tm_paged_cache* cache, const tm_paged_batch* batch, uint
     return TM_OK;
 }
 
+// An array of a call; `same` may be the array of this one's number, exactly.
+struct Extent {
+    const char* name;
+    const void* p;
+    size_t bytes;
+    bool written;
+    int same;
+};
+static int check_apart(const Extent* e, int n)
+{
+    for (int i = 0; i < n; ++i)
+        for (int k = 0; k < n; ++k) {
+            const uintptr_t a = (uintptr_t)e[i].p, b = (uintptr_t)e[k].p;
+            if (i == k || !e[i].written || !a || !b || a >= b + e[k].bytes || b >= a + e[i].bytes) continue;
+            if (a == b && (e[i].same == k || e[k].same == i)) continue;
+            return fail(TM_EINVAL, "%s is written and must not overlap %s", e[i].name, e[k].name);
+        }
+    return TM_OK;
+}
+
 // The pages of a list and the rows of a table.
 static int check_pages(const tm_paged_cache* cache, const tm_page_list* list, const int32_t* table, int batch, int max_pages)
 {
@@ -2332,8 +2352,20 @@ int tm_paged_assign(tm_paged_cache* cache, const tm_page_list* list, const tm_pa
     if (((uintptr_t)s.lens | (uintptr_t)s.counts | (uintptr_t)s.lens_out | (uintptr_t)s.offsets | (uintptr_t)s.positions | (uintptr_t)s.lacking) & 3 || (uintptr_t)s.slots & 7)
         return fail(TM_EINVAL, "misaligned lens, counts, lens_out, offsets, positions, lacking or slots");
     if (s.tokens < 0) return fail(TM_EINVAL, "tokens = %d", s.tokens);
-    if (s.positions == s.lens || s.positions == s.lens_out || s.positions == s.counts || s.lens_out == s.counts)
-        return fail(TM_EINVAL, "positions and counts must be arrays of their own");
+    const size_t row = sizeof(int32_t) * (size_t)s.batch;
+    const Extent arrays[] = {{"lens", s.lens, row, false, -1},
+                             {"counts", s.counts, row, false, -1},
+                             {"the list's pages", list->pages, sizeof(int32_t) * (size_t)list->capacity, false, -1},
+                             {"the list's count", list->count, sizeof(int32_t), false, -1},
+                             {"lens_out", s.lens_out, row, true, 0},
+                             {"left", list->left, sizeof(int32_t), true, 3},
+                             {"table", s.table, row * (size_t)s.max_pages, true, -1},
+                             {"offsets", s.offsets, row + sizeof(int32_t), true, -1},
+                             {"positions", s.positions, row, true, -1},
+                             {"slots", s.slots, sizeof(int64_t) * (size_t)s.tokens, true, -1},
+                             {"lacking", s.lacking, row, true, -1}};
+    rc = check_apart(arrays, 11);
+    if (rc != TM_OK) return rc;
     int dev;
     rc = check_paged_device(cache, &dev);
     if (rc != TM_OK) return rc;
@@ -2350,6 +2382,15 @@ int tm_paged_release(tm_paged_cache* cache, const tm_page_list* list, int32_t* t
     int rc = check_pages(cache, list, table, batch, max_pages);
     if (rc != TM_OK) return rc;
     if (((uintptr_t)from | (uintptr_t)to) & 3) return fail(TM_EINVAL, "misaligned from or to");
+    const size_t row = sizeof(int32_t) * (size_t)batch;
+    const Extent arrays[] = {{"from", from, row, false, -1},
+                             {"to", to, row, false, -1},
+                             {"the list's count", list->count, sizeof(int32_t), false, -1},
+                             {"the list's pages", list->pages, sizeof(int32_t) * (size_t)list->capacity, true, -1},
+                             {"left", list->left, sizeof(int32_t), true, 2},
+                             {"table", table, row * (size_t)max_pages, true, -1}};
+    rc = check_apart(arrays, 6);
+    if (rc != TM_OK) return rc;
     int dev;
     rc = check_paged_device(cache, &dev);
     if (rc != TM_OK) return rc;

@@ -151,6 +151,32 @@ def test_axes_of_tm_rope_apply(tm, axes, rot, dim, layout):
     assert torch.equal(a, b)
 
 
+@pytest.mark.parametrize("rot, layout", [(0, "half"), (64, "half"), (128, "interleaved")])
+@pytest.mark.parametrize("centred", [False, True])
+@pytest.mark.parametrize("tokens", [3, 3000])
+def test_one_side_normed(tm, tokens, rot, layout, centred):
+    """The other one is turned as tm_rope_apply turns it, bit for bit, and what is not turned is copied bit for bit.  Where the
+    turn's sum is NaN both must be NaN: IEEE 754 leaves the sign of a NaN that arithmetic returns undefined (a x - b y and
+    a x + (-b) y may give different ones), so it is compared only in the columns that no arithmetic touches."""
+    import torch
+    s = Heads(tm, tokens, 12, 4, 128, rot, layout, 1, "shared", 0.0, centred)
+    s.both[0, 12:, 64:] = torch.tensor([-0.0, float("nan"), float("inf"), -65504.0] * 16, device="cuda").half()
+    for side, other in ("QK", "KQ"):
+        keep, s.norm[other] = s.norm[other], None
+        out = {"Q": torch.empty(tokens, 12, 128, dtype=torch.float16, device="cuda"), "K": torch.empty(tokens, 4, 128, dtype=torch.float16, device="cuda")}
+        s.apply(out["Q"], out["K"])
+        plain = s.X[other].contiguous()
+        if rot:
+            tm.tm_rope_apply(s.X[other], s.positions, s.rope, plain)
+        same = out[other].view(torch.int16) == plain.view(torch.int16)
+        same[..., :rot] |= out[other][..., :rot].isnan() & plain[..., :rot].isnan()
+        assert same.all()
+        if side == "Q":
+            want, size = s.want(side, np.arange(min(tokens, 3)))
+            assert _near(_host(out[side])[:3], want, size).all()
+        s.norm[other] = keep
+
+
 def test_heads_of_zeros_infinities_and_nan(tm):
     """A head of zeros is zeros, one with an infinity or a NaN is NaN as the formula has it, and no head touches another."""
     import torch

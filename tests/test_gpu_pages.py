@@ -212,14 +212,22 @@ def test_refusals(tm):
     import torch
     r = Rows(tm, [1, 2], 32, 4, 4)
     ints = lambda *n: torch.zeros(n, dtype=torch.int32, device="cuda")  # noqa: E731
-    b = r.batch()
+    b, both = r.batch(), ints(4, 2)
     for call, error, text in [
             (lambda: tm.tm_paged_assign(r.cache, r.list, b, ints(2), ints(2)), ValueError, "slots or tokens"),
             (lambda: tm.tm_paged_assign(r.cache, r.list, b, ints(3), ints(2), tokens=4), ValueError, "lens"),
             (lambda: tm.tm_paged_assign(r.cache, r.list, b, ints(2), ints(1), tokens=4), ValueError, "counts"),
             (lambda: tm.tm_paged_assign(r.cache, r.list, b, ints(2), ints(2), slots=ints(4)), TypeError, "int64"),
             (lambda: tm.tm_paged_assign(r.cache, r.list, b, ints(2), ints(2), slots=torch.zeros(3, dtype=torch.int64, device="cuda"), tokens=4), ValueError, "slots"),
-            (lambda: tm.tm_paged_assign(r.cache, r.list, b, b.positions, ints(2), tokens=4), tm.TmError, "arrays of their own"),
+            (lambda: tm.tm_paged_assign(r.cache, r.list, b, b.positions, ints(2), tokens=4), tm.TmError, "overlap"),
+            (lambda: tm.tm_paged_assign(r.cache, r.list, b, ints(2), b.positions, tokens=4), tm.TmError, "overlap"),
+            (lambda: tm.tm_paged_assign(r.cache, r.list, b, both[0], both[0], tokens=4), tm.TmError, "lens_out .* counts"),
+            (lambda: tm.tm_paged_assign(r.cache, r.list, b, both[:2].reshape(-1)[:2], ints(2), lens_out=both.reshape(-1)[1:3], tokens=4), tm.TmError, "lens_out .* lens"),
+            (lambda: tm.tm_paged_assign(r.cache, r.list, b, ints(2), ints(2), left=b.offsets[:1], tokens=4), tm.TmError, "left .* offsets"),
+            (lambda: tm.tm_paged_assign(r.cache, tm.PageList(r.list.pages, r.list.pages[:1]), b, ints(2), ints(2), tokens=4), tm.TmError, "left .* pages"),
+            (lambda: tm.tm_paged_assign(r.cache, r.list, b, ints(2), ints(2), short=r.T.reshape(-1)[3:5], tokens=4), tm.TmError, "table .* lacking"),
+            (lambda: tm.tm_paged_release(r.cache, r.list, r.T, first=r.T.reshape(-1)[2:4]), tm.TmError, "table .* from"),
+            (lambda: tm.tm_paged_release(r.cache, tm.PageList(r.T.reshape(-1), r.list.count), r.T), tm.TmError, "pages .* table"),
             (lambda: tm.tm_paged_assign(r.cache, tm.PageList(ints(4), ints(2)), b, ints(2), ints(2), tokens=4), ValueError, "count"),
             (lambda: tm.tm_paged_assign(r.cache, r.list, b, ints(2).cpu(), ints(2), tokens=4), TypeError, "device"),
             (lambda: tm.tm_paged_release(r.cache, r.list, ints(8)), ValueError, "table"),
