@@ -184,6 +184,36 @@ def test_a_window_over_everything_is_full_attention(tm, bits, counts, positions,
     s.check()
 
 
+@pytest.mark.parametrize("bits", [8, 4])
+@pytest.mark.parametrize("counts, positions, q_heads, max_count", [([1, 1], [900, 300], 8, 1), ([5, 2], [900, 30], 32, 0), ([100, 3], [900, 30], 8, 100)])
+def test_offsets_past_32_bits(tm, bits, counts, positions, q_heads, max_count):
+    """Pages whose codes lie beyond 2^32 bytes, stored with norms and positions of their own: as on the pool's first pages, bit for bit, and nothing between them is written."""
+    import torch
+    page, heads, cols = 256, 8, 4
+    pages = 17000 if bits == 8 else 34000                                  # 4.4 GB of key codes
+    k, v, pairs = tm.tm_paged_pool(pages, heads, page, bits)
+    cache = tm.tm_paged_create(k, v, pairs)
+    total = sum(counts)
+    offsets = _dev(np.array([0, counts[0], total], np.int32))
+    g = torch.Generator(device="cuda").manual_seed(bits + total)
+    K, V, Q = (torch.randn(n, h, 128, generator=g, device="cuda").half() for n, h in ((1000, heads), (1000, heads), (total, q_heads)))
+    rope, norm = tm.tm_rope_create(128, axis=[i % 2 for i in range(64)]), tm.HeadNorm(K[0, 0].clone())
+    at = torch.randint(0, 5000, (1000, 2), generator=g, device="cuda", dtype=torch.int32)
+    out = []
+    for ids in (np.arange(2 * cols), np.arange(pages - 2 * cols, pages)):
+        table = _dev(ids.reshape(2, cols).astype(np.int32))
+        for b in range(2):                                                 # what the new tokens see of their sequences
+            n = positions[b] + counts[b]
+            tm.tm_paged_append(cache, tm.PagedBatch(table[b:b + 1].contiguous(), _dev(np.array([0, n], np.int32)), _dev(np.zeros(1, np.int32))), K[:n], V[:n], rope=rope, k_norm=norm,
+                               positions=at[:n])
+        O = torch.empty_like(Q)
+        batch = tm.PagedBatch(table, offsets, _dev(np.array(positions, np.int32)), max_count=max_count)
+        out.append((tm.tm_paged_attn(Q, cache, batch, O, SCALE, window=200, sinks=5), [x[torch.as_tensor(ids, device="cuda")] for x in (k, v, pairs)]))
+    assert torch.equal(out[0][0], out[1][0]) and out[0][0].isfinite().all() and out[0][0].any()
+    assert all(torch.equal(x, y) for x, y in zip(out[0][1], out[1][1]))
+    assert not pairs[2 * cols:-2 * cols].any() and not k[2 * cols:-2 * cols].any()
+
+
 def test_in_a_graph(tm):
     """Captured, and replayed with tables, positions and queries that changed in between; two graphs over one workspace in turn."""
     import torch
