@@ -12,6 +12,22 @@ namespace tmw4 {
 
 namespace {
 
+constexpr int kBehind = 1 << 26;         // values: behind any token's heads
+__device__ __forceinline__ f16x8 load8(__amdgpu_buffer_rsrc_t at, int value)
+{
+#if defined(__HIP_DEVICE_COMPILE__)
+    return __builtin_bit_cast(f16x8, __builtin_amdgcn_raw_buffer_load_b128(at, value * 2, 0, 0));
+#else
+    return f16x8{};
+#endif
+}
+__device__ __forceinline__ void store8(__amdgpu_buffer_rsrc_t at, f16x8 v, int value)
+{
+#if defined(__HIP_DEVICE_COMPILE__)
+    __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, v), at, value * 2, 0, 0);
+#endif
+}
+
 // A wave takes `rounds` times 64 / LANES heads of one token, queries first; LANES lanes hold a head, sixteen dimensions each.  Weights that all
 // heads of a side share stay in registers.  X and Y of a side may be the same.
 template <int LANES, int MODE, bool INTERLEAVED>
@@ -30,11 +46,11 @@ __global__ __launch_bounds__(256) void heads_kernel(HeadRows q, HeadRows k, cons
     auto request = [&](int round) {
         const bool keys = round >= q_rounds;
         const HeadRows& s = keys ? k : q;
-        const int h = min((round - (keys ? q_rounds : 0)) * AT_ONCE + slot, s.heads - 1);      // (a head that exists)
-        const uint16_t* const x = s.x + token * s.x_stride + (long)h * dim;
-        a = *(const f16x8*)(x + part.d0);
-        b = *(const f16x8*)(x + part.d1);
-        if (MODE != kNoNorm && (s.norm.stride || round == first || round == q_rounds)) wa = head_weights(s.norm, h, part.d0), wb = head_weights(s.norm, h, part.d1);
+        const int h = (round - (keys ? q_rounds : 0)) * AT_ONCE + slot, there = min(h, s.heads - 1);
+        if (MODE != kNoNorm && (s.norm.stride || round == first || round == q_rounds)) wa = head_weights(s.norm, there, part.d0), wb = head_weights(s.norm, there, part.d1);
+        const __amdgpu_buffer_rsrc_t x = make_rsrc(s.x + token * s.x_stride, (uint32_t)s.heads * (uint32_t)dim * 2u);
+        a = load8(x, h * dim + part.d0);
+        b = load8(x, h * dim + part.d1);
     };
     request(first);
     if (r.rot) {
@@ -42,6 +58,10 @@ __global__ __launch_bounds__(256) void heads_kernel(HeadRows q, HeadRows k, cons
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         __builtin_amdgcn_wave_barrier();
     }
+    // The first heads are there (they were requested before the positions): with nothing in flight here, a round's wait for its heads leaves the stores behind them in flight.
+#if defined(__HIP_DEVICE_COMPILE__)
+    __builtin_amdgcn_s_waitcnt(0x0f70);                      // vmcnt(0)
+#endif
     for (int round = first; round < last; ++round) {
         f16x8 y0 = a, y1 = b;
         const f16x8 w0 = wa, w1 = wb;
@@ -50,10 +70,10 @@ __global__ __launch_bounds__(256) void heads_kernel(HeadRows q, HeadRows k, cons
         const HeadRows& s = keys ? k : q;
         const int h = (round - (keys ? q_rounds : 0)) * AT_ONCE + slot;
         head_turn<LANES, MODE, INTERLEAVED>(y0, y1, w0, w1, part, s.norm, cs[wave] + turn_at(8 * u));
-        if (h >= s.heads || !part.any) continue;
-        uint16_t* const y = s.y + token * s.y_stride + (long)h * dim;
-        *(f16x8*)(y + part.d0) = y0;
-        if (part.whole) *(f16x8*)(y + part.d1) = y1;
+        // no branch: heads that there are not lie behind the buffer's end, and what lies there is not stored
+        const __amdgpu_buffer_rsrc_t y = make_rsrc(s.y + token * s.y_stride, (uint32_t)s.heads * (uint32_t)dim * 2u);
+        store8(y, y0, part.any ? h * dim + part.d0 : kBehind);
+        store8(y, y1, part.whole ? h * dim + part.d1 : kBehind);
     }
 }
 

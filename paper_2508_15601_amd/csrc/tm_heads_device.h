@@ -121,9 +121,10 @@ __device__ __forceinline__ void head_turn(f16x8& a, f16x8& b, const f16x8& wa, c
     double x[16];
 #pragma unroll
     for (int i = 0; i < 8; ++i) x[i] = (double)(float)a[i], x[8 + i] = (double)(float)b[i];
-    if (MODE != kNoNorm && n.on) {
+    if constexpr (MODE != kNoNorm) {                         // a side without a norm is multiplied by ones, which changes nothing: a branch around this costs a copy of x
         double mean, factor;
         head_norm<LANES, MODE == kAnyNorm>(x, p.any, p.whole, n, mean, factor);
+        factor = n.on ? factor : 1.0;
 #pragma unroll
         for (int i = 0; i < 16; ++i) x[i] = (MODE == kAnyNorm ? x[i] - mean : x[i]) * (factor * (n.offset + (double)(float)(i < 8 ? wa[i & 7] : wb[i & 7])));
     }
