@@ -81,6 +81,10 @@ __device__ __forceinline__ void head_norm(const double (&x)[N], bool any, bool w
                           n.eps);
 }
 
+// (offset + w) * factor; least: offset * factor, finite as the factor is.  (Where offset and w cancel, 2^-53 of `least` is left: a normed value is at most the root of a head's
+// dimensions, so nothing that fp16 has.)
+__device__ __forceinline__ double weight_of(_Float16 w, double factor, double least) { return __builtin_fma((double)(float)w, factor, least); }
+
 __device__ __forceinline__ f16x8 head_weights(const HeadNorm& n, int head, int d)
 {
     f16x8 w;
@@ -125,20 +129,25 @@ __device__ __forceinline__ void head_turn(f16x8& a, f16x8& b, const f16x8& wa, c
         double mean, factor;
         head_norm<LANES, MODE == kAnyNorm>(x, p.any, p.whole, n, mean, factor);
         factor = n.on ? factor : 1.0;
+        const double least = n.offset * factor;
 #pragma unroll
-        for (int i = 0; i < 16; ++i) x[i] = (MODE == kAnyNorm ? x[i] - mean : x[i]) * (factor * (n.offset + (double)(float)(i < 8 ? wa[i & 7] : wb[i & 7])));
+        for (int i = 0; i < 16; ++i) x[i] = (MODE == kAnyNorm ? x[i] - mean : x[i]) * weight_of(i < 8 ? wa[i & 7] : wb[i & 7], factor, least);
     }
-    if (p.turned) {
+    _Float16 y[16];
+    if (p.turned) {                                          // (rounded on either side: eight registers meet behind it, not thirty-two)
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             const CosSin t = cs[i];
             const double u = x[STEP * i], v = x[STEP * i + OTHER];
-            x[STEP * i] = u * t.c - v * t.s;
-            x[STEP * i + OTHER] = v * t.c + u * t.s;
+            y[STEP * i] = rope_round(u * t.c - v * t.s);
+            y[STEP * i + OTHER] = rope_round(v * t.c + u * t.s);
         }
-    }
 #pragma unroll
-    for (int i = 0; i < 8; ++i) a[i] = rope_round(x[i]), b[i] = rope_round(x[8 + i]);
+        for (int i = 0; i < 8; ++i) a[i] = y[i], b[i] = y[8 + i];
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) a[i] = rope_round(x[i]), b[i] = rope_round(x[8 + i]);
+    }
 }
 
 // Heads h0 .. h1 - 1 of 128 dimensions of one token, by one wave; x and y may be the same; cs as turn_at() has it.
@@ -235,8 +244,9 @@ __device__ __forceinline__ u32x4 head_sixteenth(u32x4 raw, const SixteenthWeight
     for (int i = 0; i < 4; ++i) x[i] = (double)(float)a[i], x[4 + i] = (double)(float)b[i];
     if (n.centred) head_norm<16, true>(x, true, true, n, mean, factor);
     else head_norm<16, false>(x, true, true, n, mean, factor);
+    const double least = n.offset * factor;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] = (x[i] - mean) * (factor * (n.offset + (double)(float)(i < 4 ? w.w1[i & 3] : w.w2[i & 3])));
+    for (int i = 0; i < 8; ++i) x[i] = (x[i] - mean) * weight_of(i < 4 ? w.w1[i & 3] : w.w2[i & 3], factor, least);
     if (turned) {
         const CosSin* const mine = cs + (r.interleaved ? 4 * s.sub : s.d1);
 #pragma unroll
