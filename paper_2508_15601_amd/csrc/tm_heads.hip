@@ -12,22 +12,6 @@ namespace tmw4 {
 
 namespace {
 
-constexpr int kBehind = 1 << 26;         // values: behind any token's heads
-__device__ __forceinline__ f16x8 load8(__amdgpu_buffer_rsrc_t at, int value)
-{
-#if defined(__HIP_DEVICE_COMPILE__)
-    return __builtin_bit_cast(f16x8, __builtin_amdgcn_raw_buffer_load_b128(at, value * 2, 0, 0));
-#else
-    return f16x8{};
-#endif
-}
-__device__ __forceinline__ void store8(__amdgpu_buffer_rsrc_t at, f16x8 v, int value)
-{
-#if defined(__HIP_DEVICE_COMPILE__)
-    __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, v), at, value * 2, 0, 0);
-#endif
-}
-
 // A wave takes `rounds` times 64 / LANES heads of one token, queries first; LANES lanes hold a head, sixteen dimensions each.  Weights that all
 // heads of a side share stay in registers.  X and Y of a side may be the same.
 template <int LANES, int MODE, bool INTERLEAVED>
@@ -43,6 +27,7 @@ __global__ __launch_bounds__(256) void heads_kernel(HeadRows q, HeadRows k, cons
     const int first = (int)(job % parts) * rounds, last = min(first + rounds, all);
     const HeadPart part(u, dim, r);
     f16x8 a, b, wa, wb;
+    Sixteen weights;
     auto request = [&](int round) {
         const bool keys = round >= q_rounds;
         const HeadRows& s = keys ? k : q;
@@ -58,18 +43,23 @@ __global__ __launch_bounds__(256) void heads_kernel(HeadRows q, HeadRows k, cons
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         __builtin_amdgcn_wave_barrier();
     }
-    // The first heads are there (they were requested before the positions): with nothing in flight here, a round's wait for its heads leaves the stores behind them in flight.
-#if defined(__HIP_DEVICE_COMPILE__)
-    __builtin_amdgcn_s_waitcnt(0x0f70);                      // vmcnt(0)
-#endif
+    wait_for_loads();                                        // (they were requested before the positions)
     for (int round = first; round < last; ++round) {
-        f16x8 y0 = a, y1 = b;
-        const f16x8 w0 = wa, w1 = wb;
-        if (round + 1 < last) request(round + 1);
         const bool keys = round >= q_rounds;
         const HeadRows& s = keys ? k : q;
+        f16x8 y0, y1;
+        Sixteen from;
+        if constexpr (MODE == kNoNorm) {
+            y0 = a, y1 = b;
+            if (round + 1 < last) request(round + 1);
+            from.of(y0, y1);
+        } else {
+            from.of(a, b);
+            if (s.norm.stride || round == first || round == q_rounds) weights.of(wa, wb);
+            if (round + 1 < last) request(round + 1);
+        }
         const int h = (round - (keys ? q_rounds : 0)) * AT_ONCE + slot;
-        head_turn<LANES, MODE, INTERLEAVED>(y0, y1, w0, w1, part, s.norm, cs[wave] + turn_at(8 * u));
+        head_turn<LANES, MODE, INTERLEAVED>(y0, y1, from, weights, part, s.norm, cs[wave] + turn_at(8 * u));
         // no branch: heads that there are not lie behind the buffer's end, and what lies there is not stored
         const __amdgpu_buffer_rsrc_t y = make_rsrc(s.y + token * s.y_stride, (uint32_t)s.heads * (uint32_t)dim * 2u);
         store8(y, y0, part.any ? h * dim + part.d0 : kBehind);

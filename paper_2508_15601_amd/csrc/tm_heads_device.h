@@ -116,22 +116,33 @@ constexpr int kNoNorm = 0, kPlainNorm = 1, kAnyNorm = 2;
 __device__ __forceinline__ int turn_at(int pair) { return pair + pair / 8; }
 constexpr int turns_of(int pairs) { return pairs + pairs / 8; }
 
-// a, b: the part's vectors, wa, wb: their weights; cs: cosines and sines of the part's pairs.  Every lane of a head takes part.
+// A lane's sixteen values in fp32.  They are what the next heads' vectors leave of these: loaded into registers of their own, the conversion being the copy.
+struct Sixteen {
+    float v[16];
+    __device__ __forceinline__ void of(const f16x8& a, const f16x8& b)
+    {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = (float)a[i], v[8 + i] = (float)b[i];
+    }
+};
+
+// from: the part's vectors, w: their weights, a, b: where the results go (kNoNorm: the vectors themselves, which stay where they are not turned); cs: cosines and sines of the part's
+// pairs.  Every lane of a head takes part.
 template <int LANES, int MODE, bool INTERLEAVED>
-__device__ __forceinline__ void head_turn(f16x8& a, f16x8& b, const f16x8& wa, const f16x8& wb, const HeadPart& p, const HeadNorm& n, const CosSin* cs)
+__device__ __forceinline__ void head_turn(f16x8& a, f16x8& b, const Sixteen& from, const Sixteen& w, const HeadPart& p, const HeadNorm& n, const CosSin* cs)
 {
     constexpr int STEP = INTERLEAVED ? 2 : 1, OTHER = INTERLEAVED ? 1 : 8;           // of a pair's values
-    if ((MODE == kNoNorm || !n.on) && !p.turned) return;
+    if (MODE == kNoNorm && !p.turned) return;
     double x[16];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] = (double)(float)a[i], x[8 + i] = (double)(float)b[i];
+    for (int i = 0; i < 16; ++i) x[i] = (double)from.v[i];
     if constexpr (MODE != kNoNorm) {                         // a side without a norm is multiplied by ones, which changes nothing: a branch around this costs a copy of x
         double mean, factor;
         head_norm<LANES, MODE == kAnyNorm>(x, p.any, p.whole, n, mean, factor);
         factor = n.on ? factor : 1.0;
         const double least = n.offset * factor;
 #pragma unroll
-        for (int i = 0; i < 16; ++i) x[i] = (MODE == kAnyNorm ? x[i] - mean : x[i]) * weight_of(i < 8 ? wa[i & 7] : wb[i & 7], factor, least);
+        for (int i = 0; i < 16; ++i) x[i] = (MODE == kAnyNorm ? x[i] - mean : x[i]) * __builtin_fma((double)w.v[i], factor, least);
     }
     _Float16 y[16];
     if (p.turned) {                                          // (rounded on either side: eight registers meet behind it, not thirty-two)
@@ -150,29 +161,57 @@ __device__ __forceinline__ void head_turn(f16x8& a, f16x8& b, const f16x8& wa, c
     }
 }
 
-// Heads h0 .. h1 - 1 of 128 dimensions of one token, by one wave; x and y may be the same; cs as turn_at() has it.
+// Heads of a token as a buffer: what lies behind them is read as zeros and not stored, so that no branch stands around a load or a store.  With nothing in flight before a loop over
+// heads (wait_for_loads), its wait for the next ones, which are requested first, leaves the stores behind them in flight; across a branch the compiler would wait for those too.
+constexpr int kBehind = 1 << 26;         // values: behind any token's heads
+__device__ __forceinline__ f16x8 load8(__amdgpu_buffer_rsrc_t at, int value)
+{
+#if defined(__HIP_DEVICE_COMPILE__)
+    return __builtin_bit_cast(f16x8, __builtin_amdgcn_raw_buffer_load_b128(at, value * 2, 0, 0));
+#else
+    return f16x8{};
+#endif
+}
+__device__ __forceinline__ void store8(__amdgpu_buffer_rsrc_t at, f16x8 v, int value)
+{
+#if defined(__HIP_DEVICE_COMPILE__)
+    __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, v), at, value * 2, 0, 0);
+#endif
+}
+
+__device__ __forceinline__ void wait_for_loads()
+{
+#if defined(__HIP_DEVICE_COMPILE__)
+    __builtin_amdgcn_s_waitcnt(0x0f70);                      // vmcnt(0)
+#endif
+}
+
+// Heads h0 .. h1 - 1 of 128 dimensions of one token, by one wave; x and y (of all of it) may be the same; cs as turn_at() has it.
 template <int MODE, bool INTERLEAVED>
 __device__ __forceinline__ void turn_heads(const uint16_t* x, uint16_t* y, int h0, int h1, const HeadNorm& n, const RopePlan& r, const CosSin* cs, int lane)
 {
     const HeadPart part(lane & 7, 128, r);
     f16x8 a, b, wa, wb;
+    const __amdgpu_buffer_rsrc_t from_row = make_rsrc(x, (uint32_t)h1 * 256u), to_row = make_rsrc(y, (uint32_t)h1 * 256u);
     auto request = [&](int at) {
-        const int h = min(at + (lane >> 3), h1 - 1);
-        const uint16_t* const from = x + (size_t)h * 128;
-        a = *(const f16x8*)(from + part.d0);
-        b = *(const f16x8*)(from + part.d1);
-        if (n.stride || at == h0) wa = head_weights(n, h, part.d0), wb = head_weights(n, h, part.d1);
+        const int h = at + (lane >> 3), there = min(h, h1 - 1);
+        if (n.stride || at == h0) wa = head_weights(n, there, part.d0), wb = head_weights(n, there, part.d1);
+        a = load8(from_row, h * 128 + part.d0);
+        b = load8(from_row, h * 128 + part.d1);
     };
     request(h0);
+    wait_for_loads();
+    Sixteen weights;
     for (int at = h0; at < h1; at += 8) {
-        f16x8 y0 = a, y1 = b;
-        const f16x8 w0 = wa, w1 = wb;
+        f16x8 y0, y1;
+        Sixteen from;
+        from.of(a, b);
+        if (n.stride || at == h0) weights.of(wa, wb);
         if (at + 8 < h1) request(at + 8);
-        head_turn<8, MODE, INTERLEAVED>(y0, y1, w0, w1, part, n, cs + turn_at(8 * (lane & 7)));
+        head_turn<8, MODE, INTERLEAVED>(y0, y1, from, weights, part, n, cs + turn_at(8 * (lane & 7)));
         const int h = at + (lane >> 3);
-        if (h >= h1) continue;
-        *(f16x8*)(y + (size_t)h * 128 + part.d0) = y0;
-        *(f16x8*)(y + (size_t)h * 128 + part.d1) = y1;
+        store8(to_row, y0, h * 128 + part.d0);
+        store8(to_row, y1, h * 128 + part.d1);
     }
 }
 __device__ __forceinline__ void turn_heads(const uint16_t* x, uint16_t* y, int h0, int h1, const HeadNorm& n, const RopePlan& r, const CosSin* cs, int lane)
