@@ -25,7 +25,7 @@ __global__ __launch_bounds__(256) void heads_kernel(HeadRows q, HeadRows k, cons
     const long token = job / parts;
     if (token >= tokens) return;
     const int first = (int)(job % parts) * rounds, last = min(first + rounds, all);
-    const HeadPart part(u, dim, r);
+    const HeadPart<LANES, INTERLEAVED> part(u, dim, r);
     f16x8 a, b, wa, wb;
     Sixteen weights;
     auto request = [&](int round) {
@@ -59,7 +59,7 @@ __global__ __launch_bounds__(256) void heads_kernel(HeadRows q, HeadRows k, cons
             if (round + 1 < last) request(round + 1);
         }
         const int h = (round - (keys ? q_rounds : 0)) * AT_ONCE + slot;
-        head_turn<LANES, MODE, INTERLEAVED>(y0, y1, from, weights, part, s.norm, cs[wave] + turn_at(8 * u));
+        head_turn<LANES, MODE, INTERLEAVED>(y0, y1, from, weights, part, s.norm, cs[wave]);
         // no branch: heads that there are not lie behind the buffer's end, and what lies there is not stored
         const __amdgpu_buffer_rsrc_t y = make_rsrc(s.y + token * s.y_stride, (uint32_t)s.heads * (uint32_t)dim * 2u);
         store8(y, y0, part.any ? h * dim + part.d0 : kBehind);
@@ -88,7 +88,7 @@ hipError_t launch_heads(const HeadRows& q, const HeadRows& k, const int32_t* pos
     const int rounds = (int)((all + least_parts - 1) / least_parts);
     const long parts = (all + rounds - 1) / rounds, most = 4 * most_ctas(256) / parts;       // tokens of a launch
     const auto of = lanes == 1 ? pick<1> : lanes == 2 ? pick<2> : lanes == 4 ? pick<4> : lanes == 8 ? pick<8> : pick<16>;
-    const auto kernel = of(!q.norm.on && !k.norm.on ? kNoNorm : !q.norm.centred && !k.norm.centred ? kPlainNorm : kAnyNorm, r.interleaved);
+    const auto kernel = of(!q.norm.on && !k.norm.on ? kNoNorm : !q.norm.centred && !k.norm.centred ? kPlainNorm : kAnyNorm, r.interleaved || r.rot == 0);
     for (long t = 0; t < tokens; t += most) {
         const int n = (int)std::min(most, tokens - t);
         auto from = [&](HeadRows s) {

@@ -94,25 +94,35 @@ __device__ __forceinline__ f16x8 head_weights(const HeadNorm& n, int head, int d
     return w;
 }
 
-// Sixteen dimensions of a head, which a lane holds in two vectors: the eight pairs of one stretch of the rotated part, or a stretch that is not turned, which may
-// end after eight.
+// Sixteen dimensions of a head, which a lane holds in two vectors.  INTERLEAVED: one of each half of the lanes' dimensions, so that lanes lie next to each other and all have their share of
+// what is turned; otherwise the eight pairs of one stretch of the rotated part, or a stretch that is not turned, which may end after eight.
+template <int LANES, bool INTERLEAVED>
 struct HeadPart {
     int d0, d1;
-    bool turned, any, whole;             // whole: the second vector is there too
+    bool turned, turned1, any, whole;    // the vectors are turned, and are there
     __device__ __forceinline__ HeadPart(int u, int dim, const RopePlan& r)
     {
-        any = 16 * u < dim;
-        whole = 16 * u + 8 < dim;
-        turned = 16 * u < r.rot;
-        d0 = !any ? 0 : turned && !r.interleaved ? 8 * u : 16 * u;
-        d1 = !any ? 0 : turned && !r.interleaved ? 8 * u + r.rot / 2 : whole ? 16 * u + 8 : d0;
+        if constexpr (INTERLEAVED) {
+            any = 8 * u < dim;
+            whole = 8 * (u + LANES) < dim;
+            turned = 8 * u < r.rot;
+            turned1 = 8 * (u + LANES) < r.rot;
+            d0 = any ? 8 * u : 0;
+            d1 = whole ? 8 * (u + LANES) : d0;
+        } else {
+            any = 16 * u < dim;
+            whole = 16 * u + 8 < dim;
+            turned = turned1 = 16 * u < r.rot;
+            d0 = !any ? 0 : turned ? 8 * u : 16 * u;
+            d1 = !any ? 0 : turned ? 8 * u + r.rot / 2 : whole ? 16 * u + 8 : d0;
+        }
     }
 };
 
 // Norms of the heads of a launch: none, those without a mean, any.
 constexpr int kNoNorm = 0, kPlainNorm = 1, kAnyNorm = 2;
 
-// Cosines and sines in LDS: eight pairs, which a lane reads, begin 144 bytes behind the eight before them, so that the lanes of a head meet no banks of each other's.
+// Cosines and sines in LDS: eight pairs, which a lane reads (or two lanes), begin 144 bytes behind the eight before them, so that the lanes of a head meet no banks of each other's.
 __device__ __forceinline__ int turn_at(int pair) { return pair + pair / 8; }
 constexpr int turns_of(int pairs) { return pairs + pairs / 8; }
 
@@ -126,13 +136,12 @@ struct Sixteen {
     }
 };
 
-// from: the part's vectors, w: their weights, a, b: where the results go (kNoNorm: the vectors themselves, which stay where they are not turned); cs: cosines and sines of the part's
-// pairs.  Every lane of a head takes part.
+// from: the part's vectors, w: their weights, a, b: where the results go (kNoNorm: the vectors themselves, which stay where they are not turned); cs: cosines and sines of the
+// token.  Every lane of a head takes part.
 template <int LANES, int MODE, bool INTERLEAVED>
-__device__ __forceinline__ void head_turn(f16x8& a, f16x8& b, const Sixteen& from, const Sixteen& w, const HeadPart& p, const HeadNorm& n, const CosSin* cs)
+__device__ __forceinline__ void head_turn(f16x8& a, f16x8& b, const Sixteen& from, const Sixteen& w, const HeadPart<LANES, INTERLEAVED>& p, const HeadNorm& n, const CosSin* cs)
 {
-    constexpr int STEP = INTERLEAVED ? 2 : 1, OTHER = INTERLEAVED ? 1 : 8;           // of a pair's values
-    if (MODE == kNoNorm && !p.turned) return;
+    if (MODE == kNoNorm && !p.turned) return;                // (nor is the second vector then)
     double x[16];
 #pragma unroll
     for (int i = 0; i < 16; ++i) x[i] = (double)from.v[i];
@@ -144,17 +153,27 @@ __device__ __forceinline__ void head_turn(f16x8& a, f16x8& b, const Sixteen& fro
 #pragma unroll
         for (int i = 0; i < 16; ++i) x[i] = (MODE == kAnyNorm ? x[i] - mean : x[i]) * __builtin_fma((double)w.v[i], factor, least);
     }
-    _Float16 y[16];
-    if (p.turned) {                                          // (rounded on either side: eight registers meet behind it, not thirty-two)
+    // (rounded on either side of a branch: eight registers meet behind it, not thirty-two)
+    if constexpr (INTERLEAVED) {
+        auto vector = [&](f16x8& out, const double* v, bool turned, int d) {
+            if (turned) {
+                const CosSin* const t = cs + turn_at(d / 2);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const CosSin t = cs[i];
-            const double u = x[STEP * i], v = x[STEP * i + OTHER];
-            y[STEP * i] = rope_round(u * t.c - v * t.s);
-            y[STEP * i + OTHER] = rope_round(v * t.c + u * t.s);
-        }
+                for (int i = 0; i < 4; ++i) {
+                    out[2 * i] = rope_round(v[2 * i] * t[i].c - v[2 * i + 1] * t[i].s);
+                    out[2 * i + 1] = rope_round(v[2 * i + 1] * t[i].c + v[2 * i] * t[i].s);
+                }
+            } else if (MODE != kNoNorm) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) a[i] = y[i], b[i] = y[8 + i];
+                for (int i = 0; i < 8; ++i) out[i] = rope_round(v[i]);
+            }
+        };
+        vector(a, x, p.turned, p.d0);
+        vector(b, x + 8, p.turned1, p.d1);
+    } else if (p.turned) {
+        const CosSin* const t = cs + turn_at(p.d0);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) a[i] = rope_round(x[i] * t[i].c - x[8 + i] * t[i].s), b[i] = rope_round(x[8 + i] * t[i].c + x[i] * t[i].s);
     } else {
 #pragma unroll
         for (int i = 0; i < 8; ++i) a[i] = rope_round(x[i]), b[i] = rope_round(x[8 + i]);
@@ -190,7 +209,7 @@ __device__ __forceinline__ void wait_for_loads()
 template <int MODE, bool INTERLEAVED>
 __device__ __forceinline__ void turn_heads(const uint16_t* x, uint16_t* y, int h0, int h1, const HeadNorm& n, const RopePlan& r, const CosSin* cs, int lane)
 {
-    const HeadPart part(lane & 7, 128, r);
+    const HeadPart<8, INTERLEAVED> part(lane & 7, 128, r);
     f16x8 a, b, wa, wb;
     const __amdgpu_buffer_rsrc_t from_row = make_rsrc(x, (uint32_t)h1 * 256u), to_row = make_rsrc(y, (uint32_t)h1 * 256u);
     auto request = [&](int at) {
@@ -208,7 +227,7 @@ __device__ __forceinline__ void turn_heads(const uint16_t* x, uint16_t* y, int h
         from.of(a, b);
         if (n.stride || at == h0) weights.of(wa, wb);
         if (at + 8 < h1) request(at + 8);
-        head_turn<8, MODE, INTERLEAVED>(y0, y1, from, weights, part, n, cs + turn_at(8 * (lane & 7)));
+        head_turn<8, MODE, INTERLEAVED>(y0, y1, from, weights, part, n, cs);
         const int h = at + (lane >> 3);
         store8(to_row, y0, h * 128 + part.d0);
         store8(to_row, y1, h * 128 + part.d1);
