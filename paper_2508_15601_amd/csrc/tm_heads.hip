@@ -1,8 +1,9 @@
 // Norms of queries and keys head by head with their rotation in the same pass (tm_heads_apply).
 //
-// Bound by memory where tokens are many: 8192 tokens of 32 / 8 heads of 128, nothing in the caches: 35.2 us, 168 MB at 4.8 TB/s (a large copy reaches 5.2; without norms 33.8 us); 64-bit arithmetic
-// and a wave's chain of load, sums over lanes, root and store bound the middle (1024 tokens 7.3 us, 21 MB), a launch the small (16 tokens 3.5 us).  Weights multiplied into the sines and
-// cosines once a token, which saves a third of the arithmetic, took registers and with them waves: 38 us.  Keeping the cosines in registers 35.1, but 8.6 for 1024.
+// Bound by memory where tokens are many: 8192 tokens of 32 / 8 heads of 128, nothing in the caches: 34.5 us, 168 MB at 4.9 TB/s (a large copy reaches 5.2; without norms 33.6 us); the arithmetic, 240 vector
+// instructions for a lane's sixteen values, each of which takes its four cycles in 64 bits as in 32, and a wave's chain of load, sums over lanes, root and store bound the middle (1024 tokens 7.1 us, 21 MB), a
+// launch the small (16 tokens 3.5 us).  Waiting for the stores of a round before the next one cost 3 % (3000 tokens: 13.6 us, so 13.0; 12.2 with what else was saved since).  Weights multiplied into the sines
+// and cosines once a token, which saves a third of the arithmetic, took registers and with them waves: 38 us.  Keeping the cosines in registers 35.1, but 8.6 for 1024.  Five waves a SIMD forced: 35.6.
 #include "tm_heads_device.h"
 #include "tm_paged_host.h"
 
@@ -81,9 +82,9 @@ hipError_t launch_heads(const HeadRows& q, const HeadRows& k, const int32_t* pos
 {
     const int lanes = dim <= 16 ? 1 : dim <= 32 ? 2 : dim <= 64 ? 4 : dim <= 128 ? 8 : 16, at_once = 64 / lanes;
     const int all = (q.heads + at_once - 1) / at_once + (k.heads + at_once - 1) / at_once;
-    // Rounds a wave takes, which work out the token's angles once but follow one another.  Measured with 1, 2, 3 and 5 (us; heads of 128): 32 / 8 heads, 5 rounds a token: 512 tokens 4.8, 5.6, 5.7,
-    // 7.5; 1024 7.3, 7.7, 7.8, 8.4; 1500 10.2, 10.3, 9.5, 10.8; 2048 12.2, 12.0, 10.9, 11.4; 3000 16.3, 15.4, 14.2, 13.6; 8192 43.1, 36.8, 35.2, 35.4.  64 / 4 heads, 9 rounds: 1024 11.1, 10.4, 10.0,
-    // 10.6, 2048 18.9, 16.9, 15.6, 15.3, and 17.0 with all nine.
+    // Rounds a wave takes, which work out the token's angles once but follow one another.  Measured with 1, 2, 3 and 5 (us; heads of 128): 32 / 8 heads, 5 rounds a token: 512 tokens 4.8, 5.3, 5.3,
+    // 6.7; 1024 7.1, 7.2, 7.2, 7.7; 1500 9.9, 9.6, 8.8, 9.6; 2048 11.8, 11.1, 10.2, 10.1; 3000 15.4, 14.6, 13.3, 12.2; 8192 41.8, 36.3, 34.2, 34.6.  64 / 4 heads, 9 rounds: 1024 10.7, 9.6, 9.1,
+    // 9.6, 2048 18.2, 15.9, 14.4, 13.8, and 15.4 with all nine.
     const long total = (long)tokens * all, least_parts = total < 6144 ? all : total < 12288 ? (all + 2) / 3 : (all + 4) / 5;
     const int rounds = (int)((all + least_parts - 1) / least_parts);
     const long parts = (all + rounds - 1) / rounds, most = 4 * most_ctas(256) / parts;       // tokens of a launch

@@ -5,8 +5,8 @@
 // surplus CTAs end at once.
 //
 // Measured: 10 prompts of 451 to 901 tokens, 28 / 4 heads, 4-bit, keys and queries turned, nothing in the caches: 29 us (114 MB, 3.9 TB/s, most of it the queries, a wave a token);
-// 4 x 2000, 32 / 8 heads, 8-bit 42 us (4.3 TB/s): memory and, for the keys, 64-bit arithmetic.  With norms (AppendHeads) 45.9 us; 6 prompts of 801 to 1601 tokens, 28 / 4 heads, 4-bit, three axes: 34.5 us
-// (30 without norms); 64 sequences of one token 4.5 us (4.2).  Norms put a sum over sixteen lanes and a root into every vector's chain.
+// 4 x 2000, 32 / 8 heads, 8-bit 42 us (4.3 TB/s): memory and, for the keys, 64-bit arithmetic.  With norms (AppendHeads) 42.8 us; 6 prompts of 801 to 1601 tokens, 28 / 4 heads, 4-bit, three axes: 31.0 us
+// (28.6 without norms); 64 sequences of one token 4.5 us (4.2).  Norms put a sum over sixteen lanes and a root into every vector's chain.
 #pragma once
 
 namespace tmw4 {
