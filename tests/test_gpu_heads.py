@@ -133,6 +133,26 @@ def test_heads(tm, tokens, q_heads, k_heads, dim, rot, layout, axes, norm, offse
 
 
 @pytest.mark.parametrize("layout", ["half", "interleaved"])
+@pytest.mark.parametrize("norm, centred", [("none", False), ("shared", False), ("own", True)])
+def test_every_dimension(tm, layout, norm, centred):
+    """Heads of 8 to 256 dimensions, of which none, sixteen, about half or all that can be are turned, more of them than lanes go into; what lies next to them stays."""
+    import torch
+    for dim in range(8, 257, 8):
+        for rot in sorted({0, 16, dim // 32 * 16, dim // 16 * 16}):
+            if rot > dim or (rot == 0 and norm == "none"):
+                continue
+            q_heads, k_heads = 1 + dim // 8 % 5, 3 + dim // 8 % 7
+            s = Heads(tm, 2, q_heads, k_heads, dim, rot, layout, 1, norm, 0.5, centred)
+            wide = torch.full((2, q_heads + k_heads + 3, dim), 7.0, dtype=torch.float16, device="cuda")
+            Q, K = wide[:, 1:1 + q_heads], wide[:, 2 + q_heads:2 + q_heads + k_heads]
+            s.apply(Q, K)
+            for side, got in (("Q", Q), ("K", K)):
+                want, size = s.want(side, np.arange(2))
+                assert _near(_host(got), want, size).all(), (dim, rot, side)
+            assert (wide[:, 0] == 7).all() and (wide[:, 1 + q_heads] == 7).all() and (wide[:, -1] == 7).all(), (dim, rot)
+
+
+@pytest.mark.parametrize("layout", ["half", "interleaved"])
 @pytest.mark.parametrize("axes, rot, dim", [(2, 128, 128), (3, 96, 128), (4, 32, 64), (8, 256, 256)])
 def test_axes_of_tm_rope_apply(tm, axes, rot, dim, layout):
     import torch
