@@ -57,7 +57,8 @@ PagedForm paged_form(const PagedPool& pool, const PagedSeqs& seqs, int q_heads, 
     const int reach = windowed ? (int)std::min((long)len, (long)seqs.window + seqs.sinks + most / G) : len;
     f.columns = most > 64 ? G <= 8 ? 8 : 16 : most <= 8 ? 8 : most <= 16 ? 16 : 32;
     f.column_rows = most <= 64 ? 64 : seqs.batch > 1 ? 16 : 0;
-    const long segments = (long)seqs.batch * pool.heads * (most <= 64 ? (most + f.columns - 1) / f.columns : 1);
+    // (a sequence of the call has a token: 10 of 8000 in a table of 256 rows, 8-bit, 39 us with a segment counted for every row, 34 like this)
+    const long segments = std::min((long)seqs.batch, (long)seqs.tokens) * pool.heads * (most <= 64 ? (most + f.columns - 1) / f.columns : 1);
     const double most_units = ((double)seqs.tokens * G / 8 + seqs.batch) * pool.heads * (seqs.cap / 32 + 3);      // blocks and starts, were every context as long as the table
     f.alone = (pool.bits == 4 ? segments > num_cu : f.columns < 32 && segments >= 4L * num_cu) && most_units < 2147483648.0;      // (counted in 32 bits)
     if (f.alone && f.columns == 32) f.columns = 16;
@@ -87,8 +88,12 @@ PagedForm paged_form(const PagedPool& pool, const PagedSeqs& seqs, int q_heads, 
     }
     if (f.together) f.column_ctas = std::min(rows / (32 * f.row_waves) * pool.heads >= num_cu / 4 ? num_cu / 2 : num_cu * 11 / 16, kPagedMostWaves / 8);
     if (f.together && windowed) {
-        const long count = std::max(most / G, 1L), chunks = std::min(std::max((seqs.tokens - seqs.batch + count - 1) / count, 1L), (long)seqs.batch), decoding = seqs.batch - chunks;
-        const double tiles = (double)(seqs.tokens - decoding) * G / (32 * f.row_waves) * pool.heads;
+        // Rows of the table that have no new tokens are not told apart from decoding ones, but by this: beside the longest new tokens no more sequences decode than tokens are left.  (Taking
+        // fewer for decoding than do would cost more than it saves: 64 decoding ones, 8-bit, left to 16 compute units are 700 us of reading.)  64 decoding and 512 in a table of 256 rows, 8-bit: 171 us
+        // with all other rows taken for decoding ones, like this 147 (133 in a table of 65); 8 decoding and 300, 16 / 2 heads, 49 and 45 (33); the rest is the plan's loop over the rows.
+        const long count = std::max(most / G, 1L), chunks = std::min(std::max((seqs.tokens - seqs.batch + count - 1) / count, 1L), (long)seqs.batch);
+        const long decoding = std::max(std::min(seqs.batch - chunks, seqs.tokens - count), 0L);
+        const double tiles = (double)(seqs.tokens - decoding) * G / (32 * f.row_waves) * pool.heads;         // (more than 0: tokens beyond `decoding` are at least `count`)
         if (tiles < num_cu) {
             const double columns = (double)decoding * std::min((long)len, (long)seqs.window + seqs.sinks) * pool.heads * (32 * pool.bits + 8) / (pool.bits == 8 ? 50e3 : 38e3);
             const double tall = tiles * (stages + 5.0) * (f.row_waves == 8 ? 2.3 : 1.5);
