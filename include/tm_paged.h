@@ -249,7 +249,7 @@ TM_API int tm_paged_attn_window(const uint16_t* Q, int64_t q_stride, const tm_pa
 
 /*
  * Query hook: how tm_paged_attn divides such a call (host out-pointers, any may be NULL).  Sequences with up to *column_rows (token, query head of a KV head) rows, *columns of
- * them at a time (8, 16 or 32; 0 = no such launch), the others in CTAs of *rows rows (128 or 256; 0 = no such launch), their contexts in up to *pieces. (A call with a window goes by what its tokens see, and may be divided otherwise.)
+ * them at a time (8, 16 or 32; 0 = no such launch), the others in CTAs of *rows rows (128 or 256; 0 = no such launch), their contexts in up to *pieces.
  */
 TM_API int tm_get_paged_plan(const tm_paged_cache* cache, const tm_paged_batch* batch, int q_heads, int* columns, int* column_rows, int* rows, int* pieces);
 /*
@@ -257,6 +257,10 @@ TM_API int tm_get_paged_plan(const tm_paged_cache* cache, const tm_paged_batch* 
  * one launch, the rows' pieces are put together in another.
  */
 TM_API int tm_get_paged_form(const tm_paged_cache* cache, const tm_paged_batch* batch, int q_heads, int* launches, int* column_ctas, int* alone);
+/* The same of tm_paged_attn_window, which goes by what the tokens see. */
+TM_API int tm_get_paged_window_plan(const tm_paged_cache* cache, const tm_paged_batch* batch, int q_heads, int window, int sinks, int* columns, int* column_rows, int* rows,
+                                    int* pieces);
+TM_API int tm_get_paged_window_form(const tm_paged_cache* cache, const tm_paged_batch* batch, int q_heads, int window, int sinks, int* launches, int* column_ctas, int* alone);
 
 #ifdef __cplusplus
 }

@@ -809,11 +809,11 @@ def tm_paged_attn(Q, cache: PagedCache, batch: PagedBatch, O, scale: float, stre
     return (_calls or _native()).paged_attn(Q, cache, batch, O, scale, stream, window, sinks)
 
 
-def tm_get_paged_plan(cache: PagedCache, batch: PagedBatch, tokens: int, q_heads: int):
+def tm_get_paged_plan(cache: PagedCache, batch: PagedBatch, tokens: int, q_heads: int, window: int = None, sinks: int = 0):
     """(columns, column_rows, rows, pieces) of such a tm_paged_attn call, see include/tm_paged.h."""
-    return (_calls or _native()).paged_plan(cache, batch, tokens, q_heads)
+    return (_calls or _native()).paged_plan(cache, batch, tokens, q_heads, window, sinks)
 
 
-def tm_get_paged_form(cache: PagedCache, batch: PagedBatch, tokens: int, q_heads: int):
+def tm_get_paged_form(cache: PagedCache, batch: PagedBatch, tokens: int, q_heads: int, window: int = None, sinks: int = 0):
     """(launches, column_ctas, alone) of such a tm_paged_attn call, see include/tm_paged.h."""
-    return (_calls or _native()).paged_form(cache, batch, tokens, q_heads)
+    return (_calls or _native()).paged_form(cache, batch, tokens, q_heads, window, sinks)

@@ -661,6 +661,25 @@ PyObject* paged_read(PyObject*, PyObject* const* a, Py_ssize_t n)    // cache, b
     });
 }
 
+// window (None: none) and sinks of a call.
+struct Window {
+    int window = 0x7fffffff, sinks;
+    Window(PyObject* of, PyObject* first) : sinks(whole(first, "sinks"))
+    {
+        if (of != Py_None) window = whole(of, "window");
+        else if (sinks) raise(PyExc_ValueError, "sinks without a window");
+    }
+    static int whole(PyObject* v, const char* what)
+    {
+        const long long x = as_int(v);
+        if (x < -0x7fffffffLL || x > 0x7fffffffLL) {
+            PyErr_Format(PyExc_ValueError, "%s = %lld out of range", what, x);
+            throw Failed{};
+        }
+        return (int)x;
+    }
+};
+
 PyObject* paged_attn(PyObject*, PyObject* const* a, Py_ssize_t n)    // Q, cache, batch, O, scale, stream, window (None: none), sinks
 {
     return entry(n, 8, n > 3 ? a[3] : Py_None, [&] {
@@ -674,42 +693,35 @@ PyObject* paged_attn(PyObject*, PyObject* const* a, Py_ssize_t n)    // Q, cache
         const int q_heads = Sequences::whole(Q.size(1), "q_heads");
         const float scale = (float)as_double(a[4]);
         const tm_stream st = stream_of(a[5]);
-        auto whole = [](PyObject* v, const char* what) {
-            const long long x = as_int(v);
-            if (x < -0x7fffffffLL || x > 0x7fffffffLL) {
-                PyErr_Format(PyExc_ValueError, "%s = %lld out of range", what, x);
-                throw Failed{};
-            }
-            return (int)x;
-        };
-        const int window = a[6] == Py_None ? 0x7fffffff : whole(a[6], "window"), sinks = whole(a[7], "sinks");
-        if (a[6] == Py_None && sinks) raise(PyExc_ValueError, "sinks without a window");
-        call([&] { return tm_paged_attn_window(q.p, q.stride, h, &seqs.b, o, q_heads, scale, window, sinks, st); });
+        const Window w(a[6], a[7]);
+        call([&] { return tm_paged_attn_window(q.p, q.stride, h, &seqs.b, o, q_heads, scale, w.window, w.sinks, st); });
     });
 }
 
-PyObject* paged_plan(PyObject*, PyObject* const* a, Py_ssize_t n)    // cache, batch, tokens, q_heads -> (columns, column_rows, rows, pieces)
+PyObject* paged_plan(PyObject*, PyObject* const* a, Py_ssize_t n)    // cache, batch, tokens, q_heads, window, sinks -> (columns, column_rows, rows, pieces)
 {
     int v[4] = {0, 0, 0, 0};
-    PyObject* none = entry(n, 4, Py_None, [&] {
+    PyObject* none = entry(n, 6, Py_None, [&] {
         const Sequences seqs(a[1], as_int(a[2]));
         const auto* h = (const tm_paged_cache*)handle_of(a[0], kPagedFreed);
         const int q_heads = Sequences::whole(as_int(a[3]), "q_heads");
-        call([&] { return tm_get_paged_plan(h, &seqs.b, q_heads, &v[0], &v[1], &v[2], &v[3]); });
+        const Window w(a[4], a[5]);
+        call([&] { return tm_get_paged_window_plan(h, &seqs.b, q_heads, w.window, w.sinks, &v[0], &v[1], &v[2], &v[3]); });
     });
     if (!none) return nullptr;
     Py_DECREF(none);
     return Py_BuildValue("(iiii)", v[0], v[1], v[2], v[3]);
 }
 
-PyObject* paged_form(PyObject*, PyObject* const* a, Py_ssize_t n)    // cache, batch, tokens, q_heads -> (launches, column_ctas, alone)
+PyObject* paged_form(PyObject*, PyObject* const* a, Py_ssize_t n)    // cache, batch, tokens, q_heads, window, sinks -> (launches, column_ctas, alone)
 {
     int v[3] = {0, 0, 0};
-    PyObject* none = entry(n, 4, Py_None, [&] {
+    PyObject* none = entry(n, 6, Py_None, [&] {
         const Sequences seqs(a[1], as_int(a[2]));
         const auto* h = (const tm_paged_cache*)handle_of(a[0], kPagedFreed);
         const int q_heads = Sequences::whole(as_int(a[3]), "q_heads");
-        call([&] { return tm_get_paged_form(h, &seqs.b, q_heads, &v[0], &v[1], &v[2]); });
+        const Window w(a[4], a[5]);
+        call([&] { return tm_get_paged_window_form(h, &seqs.b, q_heads, w.window, w.sinks, &v[0], &v[1], &v[2]); });
     });
     if (!none) return nullptr;
     Py_DECREF(none);

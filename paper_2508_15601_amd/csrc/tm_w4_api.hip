@@ -2415,6 +2415,13 @@ static int check_paged_attn(const tm_paged_cache* cache, const tm_paged_batch* b
     return TM_OK;
 }
 
+static int set_window(int window, int sinks, PagedSeqs* seqs)
+{
+    if (window < 1 || sinks < 0) return fail(TM_EINVAL, "need window >= 1 and sinks >= 0 (got %d, %d)", window, sinks);
+    if ((int64_t)window + sinks < seqs->cap) seqs->window = window, seqs->sinks = sinks;      // otherwise every token sees all before it
+    return TM_OK;
+}
+
 int tm_paged_attn(const uint16_t* Q, int64_t q_stride, const tm_paged_cache* cache, const tm_paged_batch* batch, uint16_t* O, int q_heads, float scale, tm_stream stream)
 {
     return tm_paged_attn_window(Q, q_stride, cache, batch, O, q_heads, scale, INT_MAX, 0, stream);
@@ -2426,8 +2433,8 @@ int tm_paged_attn_window(const uint16_t* Q, int64_t q_stride, const tm_paged_cac
     PagedSeqs seqs;
     int rc = check_paged_attn(cache, batch, q_heads, &seqs);
     if (rc != TM_OK) return rc;
-    if (window < 1 || sinks < 0) return fail(TM_EINVAL, "need window >= 1 and sinks >= 0 (got %d, %d)", window, sinks);
-    if ((int64_t)window + sinks < seqs.cap) seqs.window = window, seqs.sinks = sinks;      // otherwise every token sees all before it
+    rc = set_window(window, sinks, &seqs);
+    if (rc != TM_OK) return rc;
     if (!(scale > 0.0f) || !(scale < 1.0e6f)) return fail(TM_EINVAL, "scale out of range");
     if (seqs.tokens == 0) return TM_OK;
     rc = check_rows("Q", Q, q_stride, (int64_t)q_heads * 128);
@@ -2441,12 +2448,21 @@ int tm_paged_attn_window(const uint16_t* Q, int64_t q_stride, const tm_paged_cac
     return TM_OK;
 }
 
-int tm_get_paged_plan(const tm_paged_cache* cache, const tm_paged_batch* batch, int q_heads, int* columns, int* column_rows, int* rows, int* pieces)
+static int form_of(const tm_paged_cache* cache, const tm_paged_batch* batch, int q_heads, int window, int sinks, PagedForm* form)
 {
     PagedSeqs seqs;
-    const int rc = check_paged_attn(cache, batch, q_heads, &seqs);
+    int rc = check_paged_attn(cache, batch, q_heads, &seqs);
+    if (rc == TM_OK) rc = set_window(window, sinks, &seqs);
     if (rc != TM_OK) return rc;
-    const PagedForm f = paged_form(cache->pool, seqs, q_heads, batch->max_count, batch->max_len, g_dev[cache->device].num_cu);
+    *form = paged_form(cache->pool, seqs, q_heads, batch->max_count, batch->max_len, g_dev[cache->device].num_cu);
+    return TM_OK;
+}
+
+int tm_get_paged_window_plan(const tm_paged_cache* cache, const tm_paged_batch* batch, int q_heads, int window, int sinks, int* columns, int* column_rows, int* rows, int* pieces)
+{
+    PagedForm f;
+    const int rc = form_of(cache, batch, q_heads, window, sinks, &f);
+    if (rc != TM_OK) return rc;
     if (columns) *columns = f.column_rows ? f.columns : 0;
     if (column_rows) *column_rows = f.column_rows;
     if (rows) *rows = 32 * f.row_waves;
@@ -2454,16 +2470,25 @@ int tm_get_paged_plan(const tm_paged_cache* cache, const tm_paged_batch* batch, 
     return TM_OK;
 }
 
-int tm_get_paged_form(const tm_paged_cache* cache, const tm_paged_batch* batch, int q_heads, int* launches, int* column_ctas, int* alone)
+int tm_get_paged_window_form(const tm_paged_cache* cache, const tm_paged_batch* batch, int q_heads, int window, int sinks, int* launches, int* column_ctas, int* alone)
 {
-    PagedSeqs seqs;
-    const int rc = check_paged_attn(cache, batch, q_heads, &seqs);
+    PagedForm f;
+    const int rc = form_of(cache, batch, q_heads, window, sinks, &f);
     if (rc != TM_OK) return rc;
-    const PagedForm f = paged_form(cache->pool, seqs, q_heads, batch->max_count, batch->max_len, g_dev[cache->device].num_cu);
     if (launches) *launches = (f.row_waves ? f.target ? 2 : 1 : 0) + (f.column_rows && !f.together ? 1 : 0);
     if (column_ctas) *column_ctas = f.column_rows ? f.column_ctas : 0;
     if (alone) *alone = f.column_rows && (f.alone || f.together);
     return TM_OK;
+}
+
+int tm_get_paged_plan(const tm_paged_cache* cache, const tm_paged_batch* batch, int q_heads, int* columns, int* column_rows, int* rows, int* pieces)
+{
+    return tm_get_paged_window_plan(cache, batch, q_heads, INT_MAX, 0, columns, column_rows, rows, pieces);
+}
+
+int tm_get_paged_form(const tm_paged_cache* cache, const tm_paged_batch* batch, int q_heads, int* launches, int* column_ctas, int* alone)
+{
+    return tm_get_paged_window_form(cache, batch, q_heads, INT_MAX, 0, launches, column_ctas, alone);
 }
 
 }  // extern "C"

@@ -94,3 +94,18 @@ def test_share_of_columns_is_within_the_chip(form):
     assert len(forms) == len(calls)
     mixed = [f for f in forms if f["together"]]
     assert len(mixed) > 500 and all(CUS // 16 <= f["column_ctas"] <= CUS * 11 // 16 for f in mixed)
+
+
+def test_a_window_is_told_from_the_full_call(form):
+    """512 tokens after 30000: a window of 4096 is cut otherwise than the whole context; one that reaches as far as the table is no window."""
+    full, wide, window = form([_call(1, 512, 512, 30000, window=w, sinks=0) for w in (1 << 30, 30528, 4096)])
+    assert full == wide and full["row_waves"] == 8 and full["target"] == CUS
+    assert form([_call(8, 16000, 2000, 0, window=256, sinks=0)])[0]["target"] == 0 and window["row_waves"] == 8
+
+
+def test_hooks_refuse_before_they_look_at_a_device():
+    import ctypes
+    import paper_2508_15601_amd as tm
+    lib = tm.load_library()
+    for hook, outs in ((lib.tm_get_paged_window_plan, 4), (lib.tm_get_paged_window_form, 3)):
+        assert hook(None, ctypes.c_void_p(4096), 8, 100, 4, *[None] * outs) == -1 and "cache" in tm.tm_last_error()
