@@ -188,7 +188,7 @@ TM_API int tm_paged_assign(tm_paged_cache* cache, const tm_page_list* list, cons
  * Gives pages back: those of row b whose tokens all lie in [from[b], to[b]) (int32 [batch], device; from NULL: 0, to NULL or from max_pages * page_tokens on: to the end of the row).  Whole
  * rows of sequences that ended, what lies behind a length (drafts that were refused), what lies before a window.  Their entries become -1; entries that name no page of the pool are
  * passed over.  They come onto the list so that the first row's first page is taken first; what the list has no room for is lost.  A page that several rows share must not be given
- * back through more than one.  Uses the cache's workspace.
+ * back through more than one.  All of a range's entries are read, those of pages given back before among them, so in a window `from` may as well move along.  Uses the cache's workspace.
  */
 TM_API int tm_paged_release(tm_paged_cache* cache, const tm_page_list* list, int32_t* table, int batch, int max_pages, const int32_t* from, const int32_t* to, tm_stream stream);
 

@@ -207,7 +207,7 @@ __global__ __launch_bounds__(256) void assign_tokens_kernel(AssignJob j, const i
     place_token(j, lo, t, j.offsets[lo], j.positions[lo], first[lo], first[lo] != INT_MIN);
 }
 
-// ---- back.  Two launches, a CTA a row in each: 6.5 us up to 1000 rows of 300 entries that are gone through, 6.8 for 4000 of 100 (11.8 while rows that give nothing summed the counts too).
+// ---- back.  Two launches, up to 4096 rows a CTA a row in each: 6.5 us up to 1000 rows of 300 entries that are gone through, 6.8 for 4000 of 100 (11.8 while rows that give nothing summed the counts too).
 // Entries of row b whose pages' tokens all lie in the row's range.
 __device__ __forceinline__ void released_entries(const ReleaseJob& j, int b, int& e0, int& e1)
 {
@@ -271,6 +271,82 @@ __global__ __launch_bounds__(256) void release_kernel(ReleaseJob j, const int32_
     }
 }
 
+// More than kGroupsFrom rows: a CTA takes kGroupRows of them, a wave a row at a time, and leaves their sum, so that the CTAs of the second launch sum groups and not rows.  Rows of ten entries that give a
+// page each / none, in brackets a CTA a row: 8000 7.4 / 6.7 us (28.5 / 9.9), 20000 10.1 / 7.3 (118 / 19), 65000 27 / 12 (1000 / 54); 8000 of 500 27 / 10 (37 / 10).  With fewer rows a CTA a row
+// goes through a long row sooner: 1000 of 1000 7.4 us (35 by groups), 4000 of 500 16.5 (23), while 4000 of ten take 12.3 (6.8).
+constexpr int kGroupRows = 16, kGroupsFrom = 4096;
+static_assert(kGroupRows % 4 == 0 && kGroupRows <= 64, "rows of four waves, and of the lanes of one");
+
+// counts and groups follow each other: rows, what the list has, groups.
+struct GroupedCounts {
+    int32_t* counts;
+    uint32_t* groups;
+    int number;
+    __host__ __device__ GroupedCounts(int32_t* at, int batch) : counts(at), groups((uint32_t*)at + batch + 1), number((batch + kGroupRows - 1) / kGroupRows) {}
+};
+
+__global__ __launch_bounds__(256) void release_count_groups_kernel(ReleaseJob j, int32_t* at)
+{
+    __shared__ uint32_t waves[4];
+    const GroupedCounts c(at, j.batch);
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), first = (int)blockIdx.x * kGroupRows;
+    uint32_t total = 0;
+    for (int b = first + wave; b < min(first + kGroupRows, j.batch); b += 4) {
+        int e0, e1;
+        uint32_t n = 0;
+        released_entries(j, b, e0, e1);
+        for (int e = e0 + lane; e < e1; e += 64) n += (uint32_t)j.table[(size_t)b * j.max_pages + e] < (uint32_t)j.pool_pages;
+        n = wave_total(n);
+        if (lane == 0) c.counts[b] = (int)n;
+        total += n;
+    }
+    if (lane == 0) waves[wave] = total;
+    __syncthreads();
+    if (tid == 0) c.groups[blockIdx.x] = waves[0] + waves[1] + waves[2] + waves[3];
+    if (blockIdx.x == 0 && tid == 0) c.counts[j.batch] = min(max(*j.count, 0), j.capacity);
+}
+
+__global__ __launch_bounds__(256) void release_groups_kernel(ReleaseJob j, int32_t* at)
+{
+    __shared__ uint32_t waves[2][4];
+    const GroupedCounts c(at, j.batch);
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), group = (int)blockIdx.x, first = group * kGroupRows;
+    if (group && c.groups[group] == 0) return;
+    uint32_t before = 0, all = 0, sum;
+    for (int i = tid; i < c.number; i += 256) {
+        const uint32_t n = c.groups[i];
+        all += n;
+        before += i < group ? n : 0u;
+    }
+    sums_before<256>(before, waves[0], sum);
+    before = sum;
+    sums_before<256>(all, waves[1], sum);
+    const long top = (long)c.counts[j.batch] + sum;          // pages of the list then
+    if (group == 0 && tid == 0) *j.left = (int)min(top, (long)j.capacity);
+    const uint32_t n = lane < kGroupRows && first + lane < j.batch ? (uint32_t)c.counts[first + lane] : 0u, incl = wave_sums(n);      // a lane a row
+    for (int r = wave; r < kGroupRows; r += 4) {
+        const uint32_t mine = (uint32_t)__builtin_amdgcn_readlane((int)n, r);
+        if (mine == 0) continue;
+        const int b = first + r;
+        uint32_t rank = before + (uint32_t)__builtin_amdgcn_readlane((int)incl, r) - mine;
+        int e0, e1;
+        released_entries(j, b, e0, e1);
+        for (int base = e0; base < e1; base += 64) {
+            const int e = base + lane;
+            int32_t* const entry = j.table + (size_t)b * j.max_pages + e;
+            const int id = e < e1 ? *entry : -1;
+            const bool live = (uint32_t)id < (uint32_t)j.pool_pages;
+            const uint64_t there = __builtin_amdgcn_ballot_w64(live);
+            if (live) {
+                const long place = top - 1 - (long)rank - __builtin_popcountll(there & ((1ull << lane) - 1));
+                if (place >= 0 && place < j.capacity) j.pages[place] = id;
+                *entry = -1;
+            }
+            rank += (uint32_t)__builtin_popcountll(there);
+        }
+    }
+}
+
 }  // namespace
 
 hipError_t launch_assign(const AssignJob& j, int num_cu, void* workspace, hipStream_t stream)
@@ -293,7 +369,16 @@ hipError_t launch_assign(const AssignJob& j, int num_cu, void* workspace, hipStr
 
 hipError_t launch_release(const ReleaseJob& j, void* workspace, hipStream_t stream)
 {
+    static_assert(sizeof(int32_t) * (65535 + 1 + 65535 / kGroupRows + 1) <= kPagedColumnBytes, "counts of rows and groups");
     int32_t* const counts = (int32_t*)((char*)workspace + kPagedCounterBytes);
+    if (j.batch > kGroupsFrom) {
+        const dim3 groups((unsigned)((j.batch + kGroupRows - 1) / kGroupRows));
+        hipLaunchKernelGGL(release_count_groups_kernel, groups, dim3(256), 0, stream, j, counts);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+        hipLaunchKernelGGL(release_groups_kernel, groups, dim3(256), 0, stream, j, counts);
+        return hipGetLastError();
+    }
     hipLaunchKernelGGL(release_count_kernel, dim3((unsigned)j.batch), dim3(256), 0, stream, j, counts);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
