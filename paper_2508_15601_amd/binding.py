@@ -643,22 +643,28 @@ class Rope:
 
 
 def tm_rope_create(rot_dim: int = 128, layout: int = TM_ROPE_HALF, base: float = 10000.0, scaling: int = TM_ROPE_PLAIN, factor: float = 1.0,
-                   original_len: float = 0.0, low: float = 0.0, high: float = 0.0, amplitude: float = 0.0, frequencies=None, axis=None) -> Rope:
+                   original_len: float = 0.0, low: float = 0.0, high: float = 0.0, amplitude: float = 0.0, frequencies=None, axis=None, axes: int = None) -> Rope:
     """Rotary positions over the first rot_dim dimensions of a head (see include/tm_paged.h); `frequencies`: rot_dim / 2 numbers,
     radians per position, instead of those that base and scaling give; `axis`: rot_dim / 2 whole numbers, the axis whose position turns
-    a pair, where positions have several (positions are then [tokens][max(axis) + 1])."""
+    a pair, where positions have several: they are then [tokens][axes], with axes = max(axis) + 1 unless given."""
     p = TmRopeParams(rot_dim, layout, scaling, base, factor, original_len, low, high, amplitude, None)
     if frequencies is not None:
         f = [float(x) for x in frequencies]
         if len(f) != rot_dim // 2:
             raise ValueError(f"need {rot_dim // 2} frequencies, got {len(f)}")
         p.frequencies = (ctypes.c_double * len(f))(*f)
-    axes, of_pair = 1, None
+    of_pair = None
     if axis is not None:
         a = [int(x) for x in axis]
         if len(a) != rot_dim // 2:
             raise ValueError(f"need the axis of {rot_dim // 2} pairs, got {len(a)}")
-        axes, of_pair = max(a) + 1, (ctypes.c_int32 * len(a))(*a)
+        if any(abs(x) > 0x7ffffffe for x in a):
+            raise ValueError("axis out of range")
+        of_pair = (ctypes.c_int32 * len(a))(*a)
+    if axes is None:
+        axes = max(a) + 1 if axis is not None else 1
+    if not 0 <= axes <= 0x7fffffff:
+        raise ValueError(f"axes = {axes} out of range")
     h = load_library().tm_rope_create_axes(ctypes.byref(p), axes, of_pair)
     if not h:
         raise TmError(-1, tm_last_error())
