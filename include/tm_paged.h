@@ -95,7 +95,7 @@ typedef struct tm_head_norm {
     const uint16_t* weight;       /* device, fp16 [head_dim], or [heads][head_dim] with a stride; 16-byte aligned; NULL = ones */
     int64_t weight_stride;        /* values from head to head, a multiple of 8; 0 = every head has the same */
     double eps;                   /* >= 1e-300 */
-    double offset;                /* added to every weight: 0, or 1 where a checkpoint keeps weights less one */
+    double offset;                /* added to every weight: 0, or 1 where a checkpoint keeps weights less one; at most 1e150 either way */
     int centred;                  /* 0 or 1 */
 } tm_head_norm;
 

@@ -81,7 +81,7 @@ __device__ __forceinline__ void head_norm(const double (&x)[N], bool any, bool w
                           n.eps);
 }
 
-// (offset + w) * factor; least: offset * factor, finite as the factor is.  (Where offset and w cancel, 2^-53 of `least` is left: a normed value is at most the root of a head's
+// (offset + w) * factor; least: offset * factor, finite as either is at most 1e150.  (Where offset and w cancel, 2^-53 of `least` is left: a normed value is at most the root of a head's
 // dimensions, so nothing that fp16 has.)
 __device__ __forceinline__ double weight_of(_Float16 w, double factor, double least) { return __builtin_fma((double)(float)w, factor, least); }
 

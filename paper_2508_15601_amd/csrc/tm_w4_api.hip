@@ -2127,7 +2127,8 @@ static int check_norm(const char* what, const tm_head_norm* n, int dim, HeadNorm
 {
     *out = HeadNorm{nullptr, 0, 1.0, 0.0, 1.0 / dim, 0, 0};
     if (!n) return TM_OK;
-    if (!(n->eps >= 1e-300) || !isfinite(n->eps) || !isfinite(n->offset)) return fail(TM_EINVAL, "%s: need eps >= 1e-300 and a finite offset (got %g, %g)", what, n->eps, n->offset);
+    if (!(n->eps >= 1e-300) || !isfinite(n->eps) || !(fabs(n->offset) <= 1e150))         // (an offset times 1 / sqrt(eps) has to be finite: a head of zeros is 0)
+        return fail(TM_EINVAL, "%s: need a finite eps >= 1e-300 and an offset of at most 1e150 (got %g, %g)", what, n->eps, n->offset);
     if (n->centred != 0 && n->centred != 1) return fail(TM_EINVAL, "%s: centred = %d", what, n->centred);
     if ((uintptr_t)n->weight & 15) return fail(TM_EINVAL, "%s: weight must be 16-byte aligned", what);
     if (n->weight_stride && (n->weight_stride % 8 || n->weight_stride < dim || n->weight_stride >= (int64_t(1) << 31)))
