@@ -78,14 +78,14 @@ auto pick(int mode, bool interleaved)
 
 }  // namespace
 
-hipError_t launch_heads(const HeadRows& q, const HeadRows& k, const int32_t* positions, const RopePlan& r, int tokens, int dim, hipStream_t stream)
+hipError_t launch_heads(const HeadRows& q, const HeadRows& k, const int32_t* positions, const RopePlan& r, int tokens, int dim, int num_cu, hipStream_t stream)
 {
     const int lanes = dim <= 16 ? 1 : dim <= 32 ? 2 : dim <= 64 ? 4 : dim <= 128 ? 8 : 16, at_once = 64 / lanes;
     const int all = (q.heads + at_once - 1) / at_once + (k.heads + at_once - 1) / at_once;
-    // Rounds a wave takes, which work out the token's angles once but follow one another.  Measured with 1, 2, 3 and 5 (us; heads of 128): 32 / 8 heads, 5 rounds a token: 512 tokens 4.8, 5.3, 5.3,
+    // Rounds a wave takes, which work out the token's angles once but follow one another: by the waves a compute unit would have of one each.  Measured with 1, 2, 3 and 5 (us; heads of 128): 32 / 8 heads, 5 rounds a token: 512 tokens 4.8, 5.3, 5.3,
     // 6.7; 1024 7.1, 7.2, 7.2, 7.7; 1500 9.9, 9.6, 8.8, 9.6; 2048 11.8, 11.1, 10.2, 10.1; 3000 15.4, 14.6, 13.3, 12.2; 8192 41.8, 36.3, 34.2, 34.6.  64 / 4 heads, 9 rounds: 1024 10.7, 9.6, 9.1,
     // 9.6, 2048 18.2, 15.9, 14.4, 13.8, and 15.4 with all nine.
-    const long total = (long)tokens * all, least_parts = total < 6144 ? all : total < 12288 ? (all + 2) / 3 : (all + 4) / 5;
+    const long total = (long)tokens * all, least_parts = total < 24L * num_cu ? all : total < 48L * num_cu ? (all + 2) / 3 : (all + 4) / 5;
     const int rounds = (int)((all + least_parts - 1) / least_parts);
     const long parts = (all + rounds - 1) / rounds, most = 4 * most_ctas(256) / parts;       // tokens of a launch
     const auto of = lanes == 1 ? pick<1> : lanes == 2 ? pick<2> : lanes == 4 ? pick<4> : lanes == 8 ? pick<8> : pick<16>;

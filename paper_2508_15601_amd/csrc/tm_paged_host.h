@@ -67,7 +67,7 @@ inline long most_runs(const PagedSeqs& s)
 
 hipError_t launch_rope(const uint16_t* X, long x_stride, const int32_t* positions, const RopePlan& r, uint16_t* Y, long y_stride, int tokens, int heads,
                        int dim, hipStream_t stream);
-hipError_t launch_heads(const HeadRows& q, const HeadRows& k, const int32_t* positions, const RopePlan& r, int tokens, int dim, hipStream_t stream);
+hipError_t launch_heads(const HeadRows& q, const HeadRows& k, const int32_t* positions, const RopePlan& r, int tokens, int dim, int num_cu, hipStream_t stream);
 hipError_t launch_assign(const AssignJob& j, int num_cu, void* workspace, hipStream_t stream);
 hipError_t launch_release(const ReleaseJob& j, void* workspace, hipStream_t stream);
 // q.p == nullptr: keys and values only; rope == nullptr: not turned; heads == nullptr: no norms, and the sequences' positions

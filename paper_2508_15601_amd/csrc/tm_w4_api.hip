@@ -2166,7 +2166,7 @@ int tm_heads_apply(const tm_head_rows* q, const tm_head_rows* k, const int32_t* 
     const int rc = check_device(&dev);
     if (rc != TM_OK) return rc;
     if (rope && dev != rope->device) return fail(TM_EINVAL, "rope lives on device %d, current device is %d", rope->device, dev);
-    const hipError_t e = launch_heads(rows[0], rows[1], positions, rope_plan(rope), tokens, head_dim, (hipStream_t)stream);
+    const hipError_t e = launch_heads(rows[0], rows[1], positions, rope_plan(rope), tokens, head_dim, g_dev[dev].num_cu, (hipStream_t)stream);
     if (e != hipSuccess) return fail_hip(e, "heads launch");
     return TM_OK;
 }
