@@ -57,8 +57,8 @@ PagedForm paged_form(const PagedPool& pool, const PagedSeqs& seqs, int q_heads, 
     const int reach = windowed ? (int)std::min((long)len, (long)seqs.window + seqs.sinks + most / G) : len;
     f.columns = most > 64 ? G <= 8 ? 8 : 16 : most <= 8 ? 8 : most <= 16 ? 16 : 32;
     f.column_rows = most <= 64 ? 64 : seqs.batch > 1 ? 16 : 0;
-    // (a sequence of the call has a token: 10 of 8000 in a table of 256 rows, 8-bit, 39 us with a segment counted for every row, 34 like this)
-    const long segments = std::min((long)seqs.batch, (long)seqs.tokens) * pool.heads * (most <= 64 ? (most + f.columns - 1) / f.columns : 1);
+    // Where the call has tokens for less than half of the table's rows, the others are not in it (10 of 8000 in a table of 256 rows, 8-bit: 39 us with a segment counted for every row, 34 like this).
+    const long segments = (2L * seqs.tokens < seqs.batch ? (long)seqs.tokens : (long)seqs.batch) * pool.heads * (most <= 64 ? (most + f.columns - 1) / f.columns : 1);
     const double most_units = ((double)seqs.tokens * G / 8 + seqs.batch) * pool.heads * (seqs.cap / 32 + 3);      // blocks and starts, were every context as long as the table
     f.alone = (pool.bits == 4 ? segments > num_cu : f.columns < 32 && segments >= 4L * num_cu) && most_units < 2147483648.0;      // (counted in 32 bits)
     if (f.alone && f.columns == 32) f.columns = 16;

@@ -75,8 +75,8 @@ def test_rows_without_new_tokens_do_not_decode(form, bits, decoding, chunk, past
 @pytest.mark.parametrize("bits, page_runs", [(8, 1), (4, 0), (4, 2)])
 @pytest.mark.parametrize("active, window", [(10, 1 << 30), (32, 1 << 30), (32, 2048), (40, 300)])
 def test_segments_are_those_of_sequences_with_tokens(form, bits, page_runs, active, window):
-    """A decoding step takes the form of its own sequences, not of the table's rows."""
-    forms = form([_call(rows, active, 1, 8000, bits, window=window, run_log=page_runs) for rows in (active, active + 1, 300, 5000)])
+    """A decoding step takes the form of its own sequences, not of the table's rows, where more than half of them are not in it."""
+    forms = form([_call(rows, active, 1, 8000, bits, window=window, run_log=page_runs) for rows in (active, 2 * active + 1, 300, 5000)])
     assert all(f == forms[0] for f in forms), forms
 
 
