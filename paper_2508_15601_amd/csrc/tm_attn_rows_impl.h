@@ -95,7 +95,9 @@ __device__ __forceinline__ void attn_rows(const RowsJob& job, const uint8_t* kco
     constexpr int kChunks = BITS == 8 ? 256 : 128;                                  // of 16 bytes a run
     const int mine = (BITS == 8 ? wave >> 2 : wave >> 1) & 1;
     // The table's entries are scalar loads, requested a stage before they are looked at: as vector loads they would stand in line with the codes and pairs, and a wait for them would be
-    // one for those.
+    // one for those.  Scalar loads share their counter with LDS, out of order, so a wait for LDS is one for them: they go out with the stage's first products, from where the compiler moves
+    // them in front of the barrier, at which waves wait for each other anyway.  In front of the products every stage's first one waited for them (4-bit: four prompts 820 us, like this 797; chunks of
+    // 1500 and 750 92.1 and 88.5, 90.5 as vector loads).
     struct StageEntries {
         int id[2];
     };
@@ -330,7 +332,6 @@ __device__ __forceinline__ void attn_rows(const RowsJob& job, const uint8_t* kco
             run0 = run1;
             note(st + 3, run0);                            // (stage st - 1 has been scored)
             run1 = runs_of(st + 4, next);
-            next = entries_of(st + 5);
         }
 #pragma unroll
         for (int sub = 0; sub < NB; ++sub) {
@@ -351,6 +352,7 @@ __device__ __forceinline__ void attn_rows(const RowsJob& job, const uint8_t* kco
                 // the next scores next to the exponentials of these
                 const int run_n = KS > 1 ? ksg : sub_n;
                 const f32x16 s = multiply_k(kbase + (st_n & 1) * kStageBytes + run_n * 8192);
+                if (PAGED && sub == 0) next = entries_of(st + 5);
                 f16x8 p[2];
 #pragma unroll
                 for (int e = 0; e < 16; ++e) {
@@ -380,6 +382,8 @@ __device__ __forceinline__ void attn_rows(const RowsJob& job, const uint8_t* kco
                     }
                 }
                 scale_scores(s, m_run, at_edge(t_n) || !there, t_n, there);
+            } else if (PAGED && sub == 0) {
+                next = entries_of(st + 5);
             }
         }
     }
