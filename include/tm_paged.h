@@ -147,7 +147,8 @@ typedef struct tm_paged_batch {
     int max_pages;                /* entries of a table row; max_pages * page_tokens < 2^30 */
     int tokens;                   /* rows of the packed arrays */
     int max_count;                /* host hints, 0 = unknown: most new tokens of a sequence, and most tokens of one (cached and new).  They choose between */
-    int max_len;                  /* kernels and launch shapes; results do not depend on them beyond rounding. */
+    int max_len;                  /* kernels and launch shapes; results do not depend on them beyond rounding.  Without max_count a call of no more tokens than
+                                     sequences is launched as a decoding step: give it where prompts come beside rows that have no new tokens. */
 } tm_paged_batch;
 
 /*

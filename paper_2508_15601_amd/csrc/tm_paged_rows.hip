@@ -8,10 +8,10 @@
 //     the pieces are every CTA works out by itself from the sequences' lengths (piece_stages), which the host does not know.  A second kernel puts a row's pieces together in
 //     their order, so results do not depend on which is done first.
 //
-// Measured (32 / 8 heads): prompts of 6000, 5000, 4000 and 3000 tokens, 8-bit: 840 us (0.84 PFLOP/s), 4-bit 845; 512 tokens after 30000, 4-bit: 285 us (0.89 PFLOP/s), 1024 without
-// pieces; 100 after 8000, 8-bit: 41 us, 259 without pieces; one prompt of 4000: 162.  (Calls in a row; after an idle time, until the clock is up, a sixth more.)  What bounds it is the issue of
-// vector and matrix instructions (tm_attn_prefill.hip); page numbers as vector loads, which made every stage wait for all of its wave's loads, took 295 and 870 us in place of 285 and 855 of the
-// same run; a piece of 256 rows leaves 133 KB in memory.
+// Measured (32 / 8 heads): prompts of 6000, 5000, 4000 and 3000 tokens, 8-bit: 837 us (0.84 PFLOP/s), 4-bit 797 (0.89); 512 tokens after 30000, 4-bit: 283 us (0.90 PFLOP/s), 1024 without
+// pieces; 100 after 8000, 8-bit: 40.5 us, 259 without pieces; one prompt of 4000: 162.  (Calls in a row; after an idle time, until the clock is up, a sixth more.  Cards differ: on another 903, 857, 296, 40.7
+// and 172.)  What bounds it is the issue of vector and matrix instructions (tm_attn_prefill.hip).  How page numbers are loaded counts: as vector loads, which made every stage wait for all of its wave's
+// loads, 863, 830, 296 and 42.3 in the same run; as scalar loads that every stage's first product waited for 846, 820, 287 and 41.1.  A piece of 256 rows leaves 133 KB in memory.
 #include "tm_paged_rows_impl.h"
 
 namespace tmw4 {
@@ -31,7 +31,7 @@ hipError_t paged_rows_setup()
 // 256 x 5 after 1000, whose segments need two column tiles, 183 (152): from four segments a compute unit on.  Below that two CTAs a compute unit hide each other's starts if contexts are
 // short: 48 of 300 10.2 us (13.0 with one), 64 of 500 14.2 (15.3), 64 of 2000 42.8 (45), but 40 of 2000 to 4000 50 (45).
 // Both in one call go in one launch, the columns' CTAs (eight waves) first, on half the compute units, or 11 / 16 where row tiles are few.  With half, 11 / 16 and in two launches (us; 8-bit, then
-// 4-bit; contexts from half of the length given): 40 decoding at 4000 and chunks of 1500 and 750 122, 130, 141 and 113, 122, 131; 64 at 4000 and a chunk of 512 at 4000 116, 136, 141 and 113, 108,
+// 4-bit; contexts from half of the length given; all with page numbers as vector loads; the first with half takes 117 and 103 now): 40 decoding at 4000 and chunks of 1500 and 750 122, 130, 141 and 113, 122, 131; 64 at 4000 and a chunk of 512 at 4000 116, 136, 141 and 113, 108,
 // 118; 128 at 1000 and 512 at 2000 86, 93, 104 and 78, 82, 92; 200 at 2000 and a prompt of 256, where the rule takes 11 / 16, 147, 133, 137 and 90, 80, 90.  Short contexts beside tiles of 128 rows
 // it does not tell apart, and takes half: 60 at 500 and 400 at 500 23, 30 and 24, 29, but 300 at 300 and a prompt of 64 46, 41, 48 and 37, 31, 43.  Behind the row tiles the columns' long
 // pieces stick out: 2 to 8 % more than with half in the first three; on all compute units first 10 to 14 %.
